@@ -71,14 +71,24 @@ extern "C" {
  *                     (layer, KV head) and tensor (K or V): the quotient is the
  *                     correctly rounded fp32 division, rounded to nearest even
  *                     and saturated to +-448, NaN kept (1 byte).
+ *   HWKV_KV_I8        int8 codes with one power-of-two scale for each token
+ *                     row of a KV head, K and V apart, which the library takes
+ *                     from the row itself (1 byte, and 1 scale byte a row): with
+ *                     the row's largest magnitude in [2^(e-127), 2^(e-126)), the
+ *                     code of x is round(x * 2^(133-e)), to nearest even, clamped
+ *                     to +-127, and counts code * 2^(e-133); e = 1 for a row of
+ *                     zeros and subnormals.  A row that holds an infinity or a
+ *                     NaN has e = 255 and codes 0, and all its values are NaN.
  * The value an element contributes to attention is its stored value (times s
- * for fp8). */
+ * for fp8, with the row's scale for int8).  Every other format code is refused. */
 #define HWKV_KV_BF16 0
 #define HWKV_KV_F16 1
 #define HWKV_KV_FP8_E4M3 2
+#define HWKV_KV_I8 4
 
 typedef struct hwkv_policy hwkv_policy;
 typedef struct hwkv_cache hwkv_cache;
+typedef struct hwkv_rope hwkv_rope;
 
 /* Text of the last error raised on the calling thread ("" if none).  The
  * pointer stays valid until the next call on that thread. */
@@ -123,7 +133,8 @@ int hwkv_policy_shape(const hwkv_policy *policy, int32_t *n_layers,
 int hwkv_policy_bytes(const hwkv_policy *policy, int64_t ctx, double *bytes);
 
 /* Eq. nominal-storage under cache format kv_format: r_C(w) * head_dim *
- * (b^K + b^V) per unit and sequence, with b = 2 (bf16, f16) or 1 (fp8). */
+ * (b^K + b^V) per unit and sequence, with b = 2 (bf16, f16) or 1 (fp8, int8);
+ * int8 adds the row's 2 scale bytes: r_C(w) * (2 head_dim + 2). */
 int hwkv_policy_bytes_format(const hwkv_policy *policy, int64_t ctx,
                              int32_t kv_format, double *bytes);
 
@@ -150,7 +161,7 @@ int hwkv_cache_bytes(const hwkv_policy *policy, int32_t batch, int64_t max_ctx,
 
 /* hwkv_cache_bytes for a cache of format kv_format: element size b (2 or 1)
  * in place of 2, and the limit max_ctx (rounded up to 64) * head_dim * b <
- * 2^31.  EINVAL on an unknown format. */
+ * 2^31; int8: and 2 scale bytes per row.  EINVAL on an unknown format. */
 int hwkv_cache_bytes_format(const hwkv_policy *policy, int32_t batch,
                             int64_t max_ctx, int32_t kv_format, size_t *bytes);
 
@@ -166,7 +177,7 @@ int hwkv_cache_alloc(hwkv_cache **out, const hwkv_policy *policy,
 /* hwkv_cache_alloc for a cache of format kv_format (hwkv_cache_alloc is the
  * bf16 case).  k_scale, v_scale: host fp32 [n_layers][n_kv_heads], the fp8
  * scales s of K and V per unit (copied; NULL = all 1.0); each must be
- * positive, finite and normal.  For the 16-bit formats they must be NULL.
+ * positive, finite and normal.  For the other formats they must be NULL.
  * Buffer size rules as for hwkv_cache_alloc with hwkv_cache_bytes_format.
  * EINVAL on an unknown format or a bad scale. */
 int hwkv_cache_alloc_format(hwkv_cache **out, const hwkv_policy *policy,
@@ -175,7 +186,7 @@ int hwkv_cache_alloc_format(hwkv_cache **out, const hwkv_policy *policy,
                             void *dev_buf, size_t buf_bytes);
 
 /* Format of a cache and, if the pointers are non-NULL, its scales (host fp32
- * [n_layers][n_kv_heads] each; all 1.0 for the 16-bit formats). */
+ * [n_layers][n_kv_heads] each; all 1.0 for the other formats). */
 int hwkv_cache_format(const hwkv_cache *cache, int32_t *kv_format,
                       float *k_scale, float *v_scale);
 
@@ -193,7 +204,8 @@ int hwkv_cache_format(const hwkv_cache *cache, int32_t *kv_format,
 
 /* Exact device bytes of a paged cache: the finite units as in
  * hwkv_cache_bytes_format, a pool of n_pages pages of
- * 2 * HWKV_PAGE_TOKENS * head_dim * b bytes, and the page table (4 bytes per
+ * 2 * HWKV_PAGE_TOKENS * head_dim * b bytes (int8: 2 * HWKV_PAGE_TOKENS *
+ * (head_dim + 1)), and the page table (4 bytes per
  * page of every full unit and sequence at max_ctx), each part 256-byte
  * aligned.  n_pages >= 0.  EINVAL as hwkv_cache_bytes_format. */
 int hwkv_cache_bytes_paged(const hwkv_policy *policy, int32_t batch,
@@ -274,13 +286,13 @@ int hwkv_prefill_attn(hwkv_cache *cache, int32_t layer, int32_t seq,
 /* Device workspace bytes hwkv_prefill_attn_ws needs on this cache for chunks
  * of up to n_tokens tokens: 0 for a bf16 cache; for a binary16 cache, the
  * chunk's K and V as stored (2 * n_tokens * n_kv_heads * head_dim * 2
- * bytes); for an fp8 cache, a bf16 image of one sequence's units of the
+ * bytes); for an fp8 or int8 cache, a bf16 image of one sequence's units of the
  * largest layer (K tiles and V rows, the layout of a bf16 cache) plus the
  * chunk's K and V. */
 int hwkv_prefill_attn_workspace_bytes(const hwkv_cache *cache, int64_t n_tokens,
                                       size_t *bytes);
 
-/* hwkv_prefill_attn for every cache format.  With an fp8 or binary16 cache
+/* hwkv_prefill_attn for every cache format.  With an fp8, int8 or binary16 cache
  * the keys and values enter with their stored values -- the cached ones as
  * stored, the chunk's own as the cache will store them -- because a format
  * that changes numerical execution is used by every consumer of the cache
@@ -289,6 +301,8 @@ int hwkv_prefill_attn_workspace_bytes(const hwkv_cache *cache, int64_t n_tokens,
  *        the output by the V scale.  Every E4M3 value is a bf16 value, so
  *        the codes are staged into ws as bf16 (exactly) and the bf16 MFMA
  *        kernel runs on them.
+ *   int8: the values are staged into ws as bf16 (every one is a bf16 value) and
+ *        the bf16 MFMA kernel runs on them.
  *   binary16: the cached rows are read in place and the chunk's rows are
  *        staged into ws as binary16; binary16 MFMA products.  q enters as
  *        binary16 after scaling by a power of two per group of 32
@@ -342,6 +356,77 @@ int hwkv_prefill_attn_split(hwkv_cache *cache, int32_t layer, int32_t seq,
 int hwkv_append(hwkv_cache *cache, int32_t layer, const void *k_new,
                 const void *v_new, void *stream);
 
+/* ------------------------------------------------------------------------ */
+/* Rotary positions: the transform between a model's projections and the      */
+/* cache, whose keys are post-RoPE                                            */
+/* ------------------------------------------------------------------------ */
+
+/* Which channels of the first rot_dim make pair i: i and i + rot_dim / 2, or
+ * 2i and 2i + 1. */
+#define HWKV_ROPE_HALF 0
+#define HWKV_ROPE_PAIRS 1
+
+/* Create a rotation of heads of head_dim channels.  Pair i = (a, b) of the first
+ * rot_dim channels becomes
+ *   (a cos t - b sin t, b cos t + a sin t) * magnitude,
+ *   t = pos[axis[i]] * freq[i] radians;
+ * the channels past rot_dim stay as they are.
+ *   head_dim   64, 128 or 256
+ *   rot_dim    multiple of 16, 16 <= rot_dim <= head_dim
+ *   pairs      HWKV_ROPE_HALF or HWKV_ROPE_PAIRS
+ *   n_axes     positions per token (1 for text; time, height and width for
+ *              video), 1 <= n_axes <= 8
+ *   freq       host double [rot_dim / 2], finite: theta^(-2i / rot_dim), scaled
+ *              as the model scales it
+ *   axis       host int32 [rot_dim / 2], in [0, n_axes): the position that turns
+ *              each pair, blocks or interleaved; NULL = axis 0 for all
+ *   magnitude  finite factor of the turned channels (1 in most models)
+ * Host only; the handle holds no device memory and serves every device, and its
+ * arrays are copied.  EINVAL on any out-of-range value. */
+int hwkv_rope_set(hwkv_rope **out, int32_t head_dim, int32_t rot_dim,
+                  int32_t pairs, int32_t n_axes, const double *freq,
+                  const int32_t *axis, float magnitude);
+
+int hwkv_rope_free(hwkv_rope *rope);
+
+/* Rotate the query and key heads of n_tokens tokens, in one launch.
+ *   pos             device int32 [n_axes][n_tokens], any values
+ *   q, k            device bf16, n_q_heads (n_kv_heads) rows of head_dim
+ *                   contiguous channels per token, the tokens q_stride
+ *                   (k_stride) elements apart: multiples of 8, at least the
+ *                   heads' own elements (slices of a fused projection's rows)
+ *   q_out, k_out    device bf16 [n_tokens][heads][head_dim]; may be q (k)
+ *                   itself where that is contiguous, and must not overlap any
+ *                   input otherwise
+ * Either side may be absent: 0 heads, null pointers.  Angles are exact to fp32's
+ * last place, or 2^-22 of a turn for the farthest positions; fp32 products, one
+ * rounding to bf16 (to nearest even).  Pointers 16-byte aligned (pos 4-byte).
+ * n_tokens == 0 is a no-op.  EINVAL on bad shapes, strides, alignment or
+ * overlap, or n_tokens * head_dim >= 2^35. */
+int hwkv_rope_apply(const hwkv_rope *rope, int64_t n_tokens, int32_t n_q_heads,
+                    int32_t n_kv_heads, const int32_t *pos, const void *q,
+                    int64_t q_stride, const void *k, int64_t k_stride,
+                    void *q_out, void *k_out, void *stream);
+
+/* hwkv_append with the rotation on the way: the new token's key is rotated,
+ * rounded to bf16 and stored in the cache's format, its value stored, and its
+ * query rotated into q_out for the hwkv_decode_attn that follows.  The results
+ * are those of hwkv_rope_apply and hwkv_append, bit for bit, in one launch (one
+ * for every 192 sequences and 32 KV heads).
+ *   pos                  device int32 [n_axes][batch]: a sequence's positions
+ *                        (which need not be its length)
+ *   k_new, v_new         device bf16, n_kv_heads rows of head_dim per sequence,
+ *                        the sequences k_stride (v_stride) elements apart
+ *   q, q_out             device bf16, n_q_heads rows per sequence, q_stride
+ *                        elements apart; q_out [batch][n_q_heads][head_dim], as
+ *                        in hwkv_rope_apply.  Both may be NULL.
+ * Errors as hwkv_append, and EINVAL on a rotation of another head_dim, bad
+ * strides, alignment or overlap. */
+int hwkv_append_rope(hwkv_cache *cache, int32_t layer, const hwkv_rope *rope,
+                     const int32_t *pos, const void *k_new, int64_t k_stride,
+                     const void *v_new, int64_t v_stride, const void *q,
+                     int64_t q_stride, void *q_out, void *stream);
+
 /* Workspace bytes hwkv_decode_attn / hwkv_append_decode_attn need for any
  * layer at any length up to max_ctx (split partials). */
 int hwkv_decode_workspace_bytes(const hwkv_cache *cache, size_t *bytes);
@@ -361,7 +446,11 @@ int hwkv_decode_workspace_bytes(const hwkv_cache *cache, size_t *bytes);
  * the decoded codes and multiplied by the K scale, and the output by the V
  * scale, and the softmax weights enter the value product in fp32, or as two
  * bf16 terms (round(p) and round(p - round(p))) that carry each weight to
- * 2^-18 of itself, depending on the sizes; for binary16, q enters q.k as binary16 after a power-of-two scaling
+ * 2^-18 of itself, depending on the sizes; for int8, q enters q.k as an integer of 22
+ * bits and a sign under a power-of-two scaling per query head (exact for every
+ * component within a factor 2^14 of the head's largest |q|, the others to 2^-22 of
+ * that; the products and sums over 64 channels and more are exact), and the weights
+ * the value product as two bf16 terms; for binary16, q enters q.k as binary16 after a power-of-two scaling
  * per query head, exact for every component within a factor 2^31 of the
  * head's largest |q| (the products are exact, the sums fp32). */
 int hwkv_decode_attn(hwkv_cache *cache, int32_t layer, const void *q,
@@ -453,7 +542,7 @@ int hwkv_calib_replay(int32_t n_kv_heads, int32_t n_q_heads, int32_t head_dim,
                       size_t ws_bytes, void *stream);
 
 /* hwkv_calib_workspace_bytes for hwkv_calib_replay_format: the same, plus
- * for an fp8 format the trace's K and V staged as bf16 code values
+ * for the fp8 and int8 formats the trace's K and V staged as bf16
  * (2 * n_hist * n_kv_heads * head_dim * 2 bytes). */
 int hwkv_calib_workspace_bytes_format(int32_t n_kv_heads, int32_t n_q_heads,
                                       int32_t head_dim, int32_t n_sinks,
@@ -466,7 +555,7 @@ int hwkv_calib_workspace_bytes_format(int32_t n_kv_heads, int32_t n_q_heads,
  * nominal-storage): every candidate, the full one included, attends over the
  * trace's keys and values as a cache of that format stores them, code(x / s)
  * with the per-KV-head fp32 scales k_scale, v_scale [n_kv_heads] (NULL =
- * 1.0; fp8 only).  bf16 is hwkv_calib_replay; EINVAL for binary16.  ws of
+ * 1.0; fp8 only), or int8 rows.  bf16 is hwkv_calib_replay; EINVAL for binary16.  ws of
  * at least hwkv_calib_workspace_bytes_format bytes. */
 int hwkv_calib_replay_format(int32_t n_kv_heads, int32_t n_q_heads,
                              int32_t head_dim, int32_t n_sinks,
@@ -544,12 +633,19 @@ int hwkv_decode_timing_read(hwkv_cache *cache, double *split_ms,
 /* Test hook: synchronously copy unit (layer, kv_head) of sequence `seq` to
  * the host after all device work completes.  host_k, host_v receive
  * [capacity][head_dim] stored elements in slot order (bf16 or binary16 bit
- * patterns, 2 bytes each, or E4M3 codes, 1 byte each); *n_valid =
+ * patterns, 2 bytes each, or E4M3 or int8 codes, 1 byte each); *n_valid =
  * min(n, capacity), the number of occupied slots.  Slots >= n_valid hold
  * unspecified values. */
 int hwkv_cache_read_unit(const hwkv_cache *cache, int32_t layer,
                          int32_t kv_head, int32_t seq, void *host_k,
                          void *host_v, int64_t *n_valid);
+
+/* Test hook of int8 caches, as hwkv_cache_read_unit: the scale bytes e of the
+ * unit's K and V rows, [capacity] each, in slot order.  EINVAL on a cache of
+ * another format. */
+int hwkv_cache_read_scales(const hwkv_cache *cache, int32_t layer,
+                           int32_t kv_head, int32_t seq, uint8_t *host_k,
+                           uint8_t *host_v);
 
 #ifdef __cplusplus
 }

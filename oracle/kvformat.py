@@ -19,15 +19,23 @@ an element is stored:
   4 exponent bits of bias 7, 3 mantissa bits; exponent field 0 holds the
   subnormals m * 2^-9).
 
-The value of a stored element is its decoded value, times ``s`` for fp8.
+* ``i8``: int8 code of the element under the power-of-two scale of its row
+  (the head_dim channels of one token in one KV head): with the row's largest
+  magnitude M in [2^k, 2^(k + 1)), k at least -126, the code is the whole number
+  nearest to x / 2^(k - 6), ties to even, clamped to +-127, and the scale byte is
+  k + 127.  A row that is not finite has scale byte 255 and codes 0.
+
+The value of a stored element is its decoded value, times ``s`` for fp8; for
+int8 code * 2^(k - 6), and NaN throughout a row that was not finite.
 ``attend_values`` is decode attention (Eqs. conditional-attention-weight and
 conditional-attention) over such values, with the residency of the sink +
 window rule: a plain fp64 softmax over the retained positions.
 """
 import numpy as np
 
-FORMATS = {"bf16": 0, "f16": 1, "fp8": 2}
-BYTES = {"bf16": 2, "f16": 2, "fp8": 1}
+FORMATS = {"bf16": 0, "f16": 1, "fp8": 2, "i8": 4}
+BYTES = {"bf16": 2, "f16": 2, "fp8": 1, "i8": 1}
+ROW8 = np.dtype([("code", np.int8), ("scale", np.uint8)])   # an int8 element and its row's scale
 
 
 def _e4m3_value(code):
@@ -98,6 +106,26 @@ def f16_values(bits):
     return np.asarray(bits, dtype=np.uint16).view(np.float16).astype(np.float64)
 
 
+def i8_rows(x):
+    """int8 codes and scale bytes of fp64 rows ``x`` [..., d], as ROW8 [..., d]."""
+    x = np.asarray(x, dtype=np.float64)
+    out = np.zeros(x.shape, dtype=ROW8)
+    ok = np.isfinite(x).all(axis=-1, keepdims=True)
+    top = np.where(ok, np.abs(np.where(ok, x, 0.0)).max(axis=-1, keepdims=True), 1.0)
+    k = np.maximum(np.frexp(top)[1] - 1, -126)          # 2^k <= top < 2^(k + 1)
+    k = np.where(top == 0.0, -126, k)
+    code = np.clip(np.rint(np.ldexp(np.where(ok, x, 0.0), 6 - k)), -127, 127)
+    out["code"] = code.astype(np.int8)
+    out["scale"] = np.where(ok, k + 127, 255).astype(np.uint8)
+    return out
+
+
+def i8_values(rows):
+    """fp64 values of ROW8 elements."""
+    v = np.ldexp(rows["code"].astype(np.float64), rows["scale"].astype(np.int64) - 133)
+    return np.where(rows["scale"] == 255, np.nan, v)
+
+
 _ALL_BF16 = np.arange(65536, dtype=np.uint32).astype(np.uint16)
 _TABLES = {}
 
@@ -114,10 +142,13 @@ def _pattern_table(fmt, scale):
 
 def store(bits_bf16, fmt, scale=1.0):
     """Stored elements of bf16 inputs in format ``fmt``: uint16 bf16 bits,
-    uint16 binary16 bits or uint8 E4M3 codes."""
+    uint16 binary16 bits, uint8 E4M3 codes, or int8 codes each with its row's
+    scale (ROW8; the last axis is the row)."""
     bits_bf16 = np.asarray(bits_bf16, dtype=np.uint16)
     if fmt == "bf16":
         return bits_bf16.copy()
+    if fmt == "i8":
+        return i8_rows(bf16_values(bits_bf16))
     if fmt in ("f16", "fp8"):
         return _pattern_table(fmt, scale if fmt == "fp8" else 1.0)[bits_bf16]
     raise ValueError(f"unknown format {fmt!r}")
@@ -131,6 +162,8 @@ def values(stored, fmt, scale=1.0):
         return f16_values(stored)
     if fmt == "fp8":
         return e4m3_values(stored, scale)
+    if fmt == "i8":
+        return i8_values(stored)
     raise ValueError(f"unknown format {fmt!r}")
 
 

@@ -20,8 +20,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["hwkv_api.hip", "decode_kernels.hip", "decode_split_bf16.hip",
-           "decode_split_f16.hip", "decode_split_fp8.hip", "write_kernels.hip",
-           "prefill_attn_kernels.hip", "calib_kernels.hip"]
+           "decode_split_f16.hip", "decode_split_fp8.hip", "decode_i8.hip",
+           "write_kernels.hip", "rope_kernels.hip", "prefill_attn_kernels.hip", "calib_kernels.hip"]
 PROBE_SOURCE = os.path.join("probe", "read_probe.hip")
 PROBE_LIB = os.path.join(LIBDIR, "libhwkv_probe.so")
 

@@ -200,9 +200,9 @@ hipError_t launch_item_merge(int D, int G, const ItemArgs &a, hipStream_t s, hip
 }
 
 int decode_workgroup_target(int fmt, int D, int G) {
-  // at most one workgroup per SIMD slot the register budget holds (the fp8
-  // kernel, on the matrix cores, holds two waves per SIMD)
-  const int per_cu4 = fmt == HWKV_KV_FP8_E4M3
+  // at most one workgroup per SIMD slot the register budget holds (the fp8 and
+  // int8 kernels hold two waves per SIMD)
+  const int per_cu4 = fmt == HWKV_KV_FP8_E4M3 || fmt == HWKV_KV_I8
                           ? std::min(kDecodeWgPerCuX4, 8)
                           : std::min(kDecodeWgPerCuX4, 4 * split_waves_per_eu(D, G, fmt));
   return std::max(1, per_cu4 * device_cus() / 4);
@@ -221,6 +221,8 @@ hipError_t launch_decode_split(int fmt, int D, int G, const DecodeArgs &a,
       return launch_decode_split_fmt<HWKV_KV_F16>(D, G, a, n_splits, s, e0, e1);
     case HWKV_KV_FP8_E4M3:
       return launch_decode_split_fmt<HWKV_KV_FP8_E4M3>(D, G, a, n_splits, s, e0, e1);
+    case HWKV_KV_I8:
+      return launch_decode_i8(D, G, a, n_splits, s, e0, e1);
     default:
       return hipErrorInvalidValue;
   }

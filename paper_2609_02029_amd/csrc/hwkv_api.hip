@@ -37,6 +37,8 @@ struct hwkv_cache {
   std::vector<int64_t> cap_pad;  // rows allocated (multiple of 64)
   std::vector<int64_t> k_off;    // element offset of (u, seq 0); seq stride
   std::vector<int64_t> v_off;    //   is cap_pad * head_dim
+  std::vector<int64_t> s_off;    // int8: byte offset of its scale pairs; seq
+                                 //   stride is cap_pad * kRowScaleBytes
   std::vector<int64_t> n;        // [layer * batch + b] sequence lengths
   int32_t fmt = HWKV_KV_BF16;    // cache format (HWKV_KV_*)
   int32_t elem = 2;              // bytes per stored element
@@ -61,6 +63,11 @@ struct hwkv_cache {
   std::vector<hipEvent_t> ev_pool;   // created events, reused
   size_t ev_used = 0;                // events recorded since the last read
   std::vector<char> ev_merged;       // per launch group since then: has a merge
+};
+
+struct hwkv_rope {
+  int32_t head_dim = 0, n_axes = 0;
+  hwkv::RopeTable table;
 };
 
 namespace {
@@ -91,9 +98,21 @@ int format_bytes(int32_t fmt) {
     case HWKV_KV_BF16: return 2;
     case HWKV_KV_F16: return 2;
     case HWKV_KV_FP8_E4M3: return 1;
+    case HWKV_KV_I8: return 1;
     default: return 0;
   }
 }
+
+// Scale bytes of a token row (its K's and its V's) under a cache format.
+int64_t row_scale_bytes(int32_t fmt) { return fmt == HWKV_KV_I8 ? hwkv::kRowScaleBytes : 0; }
+
+// Elements of one page of a full unit.
+int64_t page_elems(const hwkv_policy &p, int32_t fmt) {
+  return hwkv::kPageTokens * (2 * (int64_t)p.head_dim + row_scale_bytes(fmt));
+}
+
+// Whether prefill attention reads the units from a bf16 image of them.
+bool units_staged(int32_t fmt) { return fmt == HWKV_KV_FP8_E4M3 || fmt == HWKV_KV_I8; }
 
 // Canonical window and capacity of a finite or full unit at max_ctx.
 void unit_shape(const hwkv_policy &p, int32_t u, int64_t max_ctx,
@@ -110,11 +129,12 @@ void unit_shape(const hwkv_policy &p, int32_t u, int64_t max_ctx,
 
 uint64_t round256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Lays out the grouped pools for elements of `elem` bytes; fills per-unit
-// vectors when `c` is non-null.  paged: full units get no region; a pool of
-// n_pages pages and the page table follow the finite units' regions.
-int layout(const hwkv_policy &p, int32_t batch, int64_t max_ctx, int elem,
+// Lays out the grouped pools for format `fmt`; fills per-unit vectors when `c`
+// is non-null.  int8: the units' scale pairs follow their codes.  paged: full
+// units get no region; a pool of n_pages pages and the page table follow.
+int layout(const hwkv_policy &p, int32_t batch, int64_t max_ctx, int32_t fmt,
            bool paged, int64_t n_pages, size_t *bytes, hwkv_cache *c) {
+  const int elem = format_bytes(fmt);
   if (batch < 1) return fail(HWKV_EINVAL, "batch must be >= 1");
   if (paged && (n_pages < 0 || n_pages > (int64_t)INT32_MAX))
     return fail(HWKV_EINVAL, "n_pages must be in [0, 2^31)");
@@ -127,7 +147,7 @@ int layout(const hwkv_policy &p, int32_t batch, int64_t max_ctx, int elem,
                              "or V)");
   const int32_t U = p.n_layers * p.n_kv_heads;
   const uint64_t D = (uint64_t)p.head_dim;
-  std::vector<int64_t> win(U), cap(U), capp(U), koff(U), voff(U);
+  std::vector<int64_t> win(U), cap(U), capp(U), koff(U), voff(U), soff(U, -1);
   for (int32_t u = 0; u < U; ++u) {
     unit_shape(p, u, max_ctx, &win[u], &cap[u]);
     capp[u] = round_tile(cap[u]);
@@ -160,14 +180,22 @@ int layout(const hwkv_policy &p, int32_t batch, int64_t max_ctx, int elem,
     }
   }
   uint64_t total = off * (uint64_t)elem;
+  for (int32_t u = 0; u < U && row_scale_bytes(fmt) > 0; ++u) {
+    if (fidx[u] >= 0) continue;
+    soff[u] = (int64_t)total;
+    uint64_t pairs;
+    if (!mul_ok((uint64_t)(capp[u] * row_scale_bytes(fmt)), (uint64_t)batch, &pairs) ||
+        __builtin_add_overflow(total, pairs, &total) || total > (uint64_t)INT64_MAX / 4)
+      return fail(HWKV_EINVAL, "cache size overflows");
+  }
   const int64_t max_pages = (max_ctx + hwkv::kPageTokens - 1) / hwkv::kPageTokens;
   uint64_t pool_off = 0, table_off = 0;
   if (paged) {
-    // pool: page i at element pool_off + i * 2 * kPageTokens * D
+    // pool: page i at element pool_off + i * page_elems
     total = round256(total);
     pool_off = total / (uint64_t)elem;
     uint64_t pool, tab;
-    if (!mul_ok((uint64_t)n_pages, 2ull * hwkv::kPageTokens * D * (uint64_t)elem, &pool) ||
+    if (!mul_ok((uint64_t)n_pages, (uint64_t)page_elems(p, fmt) * (uint64_t)elem, &pool) ||
         __builtin_add_overflow(total, pool, &total))
       return fail(HWKV_EINVAL, "cache size overflows");
     // table: int32 [full unit][seq][max_pages]; offsets into it are int32
@@ -185,6 +213,7 @@ int layout(const hwkv_policy &p, int32_t batch, int64_t max_ctx, int elem,
     c->cap_pad = capp;
     c->k_off = koff;
     c->v_off = voff;
+    c->s_off = soff;
     c->paged = paged;
     if (paged) {
       c->n_pages = n_pages;
@@ -284,6 +313,45 @@ int check_device(hipError_t e, const char *what) {
   return fail(HWKV_EDEVICE, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+// A range of device memory that a call reads or writes.
+struct RowSpan {
+  const void *at;
+  int64_t bytes;
+};
+
+bool overlap(const RowSpan &x, const RowSpan &y) {
+  const uintptr_t a = (uintptr_t)x.at, b = (uintptr_t)y.at;
+  return x.bytes > 0 && y.bytes > 0 && a < b + (uintptr_t)y.bytes && b < a + (uintptr_t)x.bytes;
+}
+
+// Checks n rows of `elems` bf16 elements, `stride` apart, and their output (0
+// elements: the side is absent); *span receives what the rows cover.
+int check_rows(const char *name, const void *in, int64_t stride, const void *out, int64_t n,
+               int64_t elems, RowSpan *span) {
+  *span = {nullptr, 0};
+  if (elems == 0) return HWKV_OK;
+  if (!in || !out) return fail(HWKV_EINVAL, std::string(name) + " and its output must be non-null");
+  if ((uintptr_t)in % 16 != 0 || (uintptr_t)out % 16 != 0)
+    return fail(HWKV_EINVAL, std::string(name) + " must be 16-byte aligned");
+  if (stride % 8 != 0 || stride < elems || stride > ((int64_t)1 << 31) || (n - 1) > ((int64_t)1 << 58) / stride)
+    return fail(HWKV_EINVAL, std::string(name) + " stride must be a multiple of 8 elements, at "
+                                                 "least a row's, and at most 2^31");
+  *span = {in, ((n - 1) * stride + elems) * 2};
+  return HWKV_OK;
+}
+
+// Whether an output of `elems` elements is its own input, in place, or apart
+// from every range the call reads.
+int check_apart(const char *name, const void *out, const void *in, int64_t elems, bool contiguous,
+                const RowSpan *reads, int n) {
+  for (int i = 0; i < n; ++i) {
+    if (out == in && contiguous && reads[i].at == in) continue;
+    if (overlap({out, elems * 2}, reads[i]))
+      return fail(HWKV_EINVAL, std::string(name) + " overlaps an input");
+  }
+  return HWKV_OK;
+}
+
 // The next timing event of the cache (created on first use, then reused);
 // the launch it is handed to records it.
 int next_event(hwkv_cache *c, hipEvent_t *e) {
@@ -344,9 +412,9 @@ int take_pages(hwkv_cache *c, int32_t layer,
 }
 
 // Element offsets (2-byte elements) of the prefill-attention staging area:
-// for an fp8 cache, per kv head of the layer its K tiles and V rows widened
-// to bf16 in the bf16 cache layout (cap_pad rows each); then, for fp8 and
-// binary16 caches, the chunk's K and V ([n_tokens][Hkv][D]) as the cache will
+// for an fp8 or int8 cache, per kv head of the layer its K tiles and V rows
+// widened to bf16 in the bf16 cache layout (cap_pad rows each); then, for these
+// and binary16 caches, the chunk's K and V ([n_tokens][Hkv][D]) as the cache will
 // store them.  Returns the bytes (0 for a bf16 cache).
 struct StageLayout {
   std::vector<int64_t> k_img, v_img;
@@ -361,7 +429,7 @@ size_t stage_layout(const hwkv_cache *c, int32_t layer, int64_t n_tokens, StageL
     if (out) *out = L;
     return 0;
   }
-  for (int32_t h = 0; h < p.n_kv_heads && c->fmt == HWKV_KV_FP8_E4M3; ++h) {
+  for (int32_t h = 0; h < p.n_kv_heads && units_staged(c->fmt); ++h) {
     const int32_t u = layer * p.n_kv_heads + h;
     L.k_img.push_back(off);
     off += c->cap_pad[u] * D;
@@ -453,9 +521,9 @@ int prefill_attn_impl(hwkv_cache *c, int32_t layer, int32_t seq, int64_t pos0,
                       float scale, void *out, void *ws, size_t ws_bytes, void *parts,
                       size_t part_bytes, void *stream) {
   if (!c) return fail(HWKV_EINVAL, "cache is null");
-  // fp8: the units are staged as bf16 code values; fp8 and binary16: the
+  // fp8 and int8: the units are staged as bf16; these and binary16: the
   // chunk's own keys and values are staged as the cache will store them
-  const bool staged = c->fmt == HWKV_KV_FP8_E4M3;
+  const bool staged = units_staged(c->fmt);
   const bool chunk_staged = c->fmt != HWKV_KV_BF16;
   const hwkv_policy &p = c->pol;
   if (layer < 0 || layer >= p.n_layers || seq < 0 || seq >= c->batch)
@@ -555,6 +623,7 @@ int prefill_attn_impl(hwkv_cache *c, int32_t layer, int32_t seq, int64_t pos0,
       hwkv::StageUnit &su = sa.unit[h];
       su.src_k_off = c->k_off[u] + seq_off;
       su.src_v_off = c->v_off[u] + seq_off;
+      su.src_s_off = c->s_off[u] + (int64_t)seq * c->cap_pad[u] * hwkv::kRowScaleBytes;
       su.dst_k_off = SL.k_img[h];
       su.dst_v_off = SL.v_img[h];
       su.pto = page_tab_off(c, u, seq);
@@ -569,7 +638,7 @@ int prefill_attn_impl(hwkv_cache *c, int32_t layer, int32_t seq, int64_t pos0,
     sa.max_chunks = (int32_t)max_chunks;
     int rc;
     if (max_chunks > 0 &&
-        (rc = check_device(hwkv::launch_stage_units((int)D, sa, st), "stage launch")) != HWKV_OK)
+        (rc = check_device(hwkv::launch_stage_units(c->fmt, (int)D, sa, st), "stage launch")) != HWKV_OK)
       return rc;
     a.cache = img;
   } else {
@@ -922,7 +991,8 @@ int decode_impl(hwkv_cache *c, int32_t layer, const void *k_new,
   ItemLaunch one;                   // (a batch of one launch: nothing from the heap)
   std::vector<ItemLaunch> several(B > hwkv::kItemSeqs ? (B - 1) / hwkv::kItemSeqs + 1 : 0);
   ItemLaunch *const launches = several.empty() ? &one : several.data();
-  if (decode_by_item(c, layer, tiles, order, fused, total_splits, launches)) {
+  if (c->fmt != HWKV_KV_I8 &&
+      decode_by_item(c, layer, tiles, order, fused, total_splits, launches)) {
     const int rc = launch_items(c, layer, order, launches, k_new, v_new, q, scale, out,
                                 static_cast<float *>(ws), fused, s);
     if (rc != HWKV_OK) return rc;
@@ -948,8 +1018,12 @@ int decode_impl(hwkv_cache *c, int32_t layer, const void *k_new,
       a.it.new_slot[j] = nslot[i];
       a.it.q_row[j] = b * p.n_q_heads + h * G;
       a.it.kv_row[j] = b * H + h;
-      a.it.k_scale[j] = c->k_scale[u];
-      a.it.v_scale[j] = c->v_scale[u];
+      if (c->fmt == HWKV_KV_I8) {
+        a.it.s_off[j] = c->s_off[u] + (int64_t)b * c->cap_pad[u] * hwkv::kRowScaleBytes;
+      } else {
+        a.it.k_scale[j] = c->k_scale[u];
+        a.it.v_scale[j] = c->v_scale[u];
+      }
       a.it.pto[j] = page_tab_off(c, u, b);
       a.it.split_begin[j] = splits;
       splits += nwg[i];
@@ -1074,7 +1148,8 @@ int hwkv_policy_bytes_format(const hwkv_policy *p, int64_t ctx,
   const int b = format_bytes(kv_format);
   if (b == 0) return fail(HWKV_EINVAL, "unknown cache format");
   double tot = 0.0;
-  const double row = (double)p->head_dim * (double)(b + b);  // d^K b^K + d^V b^V
+  // d^K b^K + d^V b^V, and an int8 row's scale bytes
+  const double row = (double)p->head_dim * (double)(b + b) + (double)row_scale_bytes(kv_format);
   for (int32_t lv : p->level_of_unit) {
     const int64_t w = p->level_window[lv];
     const int64_t r = (w == 0) ? ctx : std::min<int64_t>(p->n_sinks + w, ctx);
@@ -1103,18 +1178,16 @@ int hwkv_cache_bytes(const hwkv_policy *p, int32_t batch, int64_t max_ctx,
 int hwkv_cache_bytes_format(const hwkv_policy *p, int32_t batch,
                             int64_t max_ctx, int32_t kv_format, size_t *bytes) {
   if (!p || !bytes) return fail(HWKV_EINVAL, "null argument");
-  const int elem = format_bytes(kv_format);
-  if (elem == 0) return fail(HWKV_EINVAL, "unknown cache format");
-  const int rc = layout(*p, batch, max_ctx, elem, false, 0, bytes, nullptr);
+  if (format_bytes(kv_format) == 0) return fail(HWKV_EINVAL, "unknown cache format");
+  const int rc = layout(*p, batch, max_ctx, kv_format, false, 0, bytes, nullptr);
   return rc == HWKV_OK ? ok() : rc;
 }
 
 int hwkv_cache_bytes_paged(const hwkv_policy *p, int32_t batch, int64_t max_ctx,
                            int32_t kv_format, int64_t n_pages, size_t *bytes) {
   if (!p || !bytes) return fail(HWKV_EINVAL, "null argument");
-  const int elem = format_bytes(kv_format);
-  if (elem == 0) return fail(HWKV_EINVAL, "unknown cache format");
-  const int rc = layout(*p, batch, max_ctx, elem, true, n_pages, bytes, nullptr);
+  if (format_bytes(kv_format) == 0) return fail(HWKV_EINVAL, "unknown cache format");
+  const int rc = layout(*p, batch, max_ctx, kv_format, true, n_pages, bytes, nullptr);
   return rc == HWKV_OK ? ok() : rc;
 }
 
@@ -1173,7 +1246,7 @@ int alloc_impl(hwkv_cache **out, const hwkv_policy *p, int32_t batch, int64_t ma
     if (k_scale) c->k_scale.assign(k_scale, k_scale + n_units);
     if (v_scale) c->v_scale.assign(v_scale, v_scale + n_units);
     size_t bytes = 0;
-    int rc = layout(*p, batch, max_ctx, elem, paged, n_pages, &bytes, c);
+    int rc = layout(*p, batch, max_ctx, kv_format, paged, n_pages, &bytes, c);
     if (rc != HWKV_OK) {
       delete c;
       return rc;
@@ -1343,8 +1416,12 @@ int hwkv_prefill_write(hwkv_cache *c, int32_t layer, int32_t seq, int64_t pos0,
     wh.v_off = c->v_off[u] + seq_off;
     wh.window = (int32_t)w;
     wh.pto = page_tab_off(c, u, seq);
-    wh.k_scale = c->k_scale[u];
-    wh.v_scale = c->v_scale[u];
+    if (c->fmt == HWKV_KV_I8) {
+      wh.s_off = c->s_off[u] + (int64_t)seq * c->cap_pad[u] * hwkv::kRowScaleBytes;
+    } else {
+      wh.k_scale = c->k_scale[u];
+      wh.v_scale = c->v_scale[u];
+    }
     // slot ranges [lo, hi) written by this chunk
     std::vector<std::pair<int64_t, int64_t>> sr;
     if (w == 0) {
@@ -1408,7 +1485,7 @@ int hwkv_prefill_attn(hwkv_cache *c, int32_t layer, int32_t seq, int64_t pos0,
                       const void *v, float scale, void *out, void *stream) {
   if (c && c->fmt != HWKV_KV_BF16)
     return fail(HWKV_EINVAL, "prefill attention needs a bf16 cache here "
-                             "(hwkv_prefill_attn_ws takes fp8 and binary16 caches)");
+                             "(hwkv_prefill_attn_ws takes every format)");
   return prefill_attn_impl(c, layer, seq, pos0, n_tokens, q, k, v, scale, out,
                            nullptr, 0, nullptr, 0, stream);
 }
@@ -1544,14 +1621,14 @@ int hwkv_calib_workspace_bytes_format(int32_t n_kv_heads, int32_t n_q_heads,
                                       int32_t head_dim, int32_t n_sinks, int64_t n_hist,
                                       int64_t n_rows, int32_t kv_format, size_t *bytes) {
   if (!bytes) return fail(HWKV_EINVAL, "bytes is null");
-  if (kv_format != HWKV_KV_BF16 && kv_format != HWKV_KV_FP8_E4M3)
-    return fail(HWKV_EINVAL, "the replay takes bf16 or fp8 formats");
+  if (kv_format != HWKV_KV_BF16 && !units_staged(kv_format))
+    return fail(HWKV_EINVAL, "the replay takes bf16, fp8 or int8 formats");
   if (n_kv_heads < 1 || n_kv_heads > hwkv::kMaxItems)
     return fail(HWKV_EINVAL, "n_kv_heads must be in [1, 64]");
   size_t base = 0;
   const int rc = hwkv_calib_workspace_bytes(n_q_heads, head_dim, n_sinks, n_hist, n_rows, &base);
   if (rc != HWKV_OK) return rc;
-  if (kv_format == HWKV_KV_FP8_E4M3)       // the staged trace, 256-byte aligned
+  if (units_staged(kv_format))             // the staged trace, 256-byte aligned
     base = (base + 255) / 256 * 256 +
            2 * (size_t)n_hist * (size_t)n_kv_heads * (size_t)head_dim * 2;
   *bytes = base;
@@ -1603,11 +1680,11 @@ int hwkv_calib_replay_format(int32_t n_kv_heads, int32_t n_q_heads, int32_t head
     return fail(HWKV_EINVAL, "k, v, q, outs, ws (and scores, means) must be non-null");
   if ((ref_full == nullptr) != (check == nullptr))
     return fail(HWKV_EINVAL, "check is required exactly when ref_full is given");
-  if (kv_format != HWKV_KV_BF16 && kv_format != HWKV_KV_FP8_E4M3)
-    return fail(HWKV_EINVAL, "the replay takes bf16 or fp8 formats (binary16 values are "
-                             "not bf16 values)");
-  const bool staged = kv_format == HWKV_KV_FP8_E4M3;
-  if (!staged && (k_scale || v_scale))
+  if (kv_format != HWKV_KV_BF16 && !units_staged(kv_format))
+    return fail(HWKV_EINVAL, "the replay takes bf16, fp8 or int8 formats (binary16 values "
+                             "are not bf16 values)");
+  const bool staged = units_staged(kv_format);
+  if (kv_format != HWKV_KV_FP8_E4M3 && (k_scale || v_scale))
     return fail(HWKV_EINVAL, "scales are for fp8 only");
   for (const float *sc : {k_scale, v_scale}) {
     if (!sc) continue;
@@ -1646,8 +1723,8 @@ int hwkv_calib_replay_format(int32_t n_kv_heads, int32_t n_q_heads, int32_t head
   const size_t vec = (size_t)n_rows * n_q_heads * head_dim;
   float *part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) +
                                           replay_rows_bytes(n_rows));
-  // fp8: the trace's keys and values as a cache of that format stores them,
-  // staged after the partials as bf16 code values
+  // fp8 and int8: the trace's keys and values as a cache of that format stores
+  // them, staged after the partials as bf16 (fp8: code values)
   const void *k_src = k, *v_src = v;
   if (staged) {
     size_t base = 0;
@@ -1657,7 +1734,7 @@ int hwkv_calib_replay_format(int32_t n_kv_heads, int32_t n_q_heads, int32_t head
     uint16_t *vst = kst + (size_t)n_hist * n_kv_heads * head_dim;
     hwkv::StageChunkArgs ca;
     std::memset(&ca, 0, sizeof ca);
-    ca.fmt = HWKV_KV_FP8_E4M3;
+    ca.fmt = kv_format;
     ca.k = static_cast<const uint16_t *>(k);
     ca.v = static_cast<const uint16_t *>(v);
     ca.k_out = kst;
@@ -2064,8 +2141,12 @@ int hwkv_append(hwkv_cache *c, int32_t layer, const void *k_new,
       a.v_off[j] = c->v_off[u] + seq_off;
       a.slot[j] = (int32_t)slot_of(c, u, seq_len(c, layer, b));
       a.kv_row[j] = b * H + h;
-      a.k_scale[j] = c->k_scale[u];
-      a.v_scale[j] = c->v_scale[u];
+      if (c->fmt == HWKV_KV_I8) {
+        a.s_off[j] = c->s_off[u] + (int64_t)b * c->cap_pad[u] * hwkv::kRowScaleBytes;
+      } else {
+        a.k_scale[j] = c->k_scale[u];
+        a.v_scale[j] = c->v_scale[u];
+      }
       a.pto[j] = page_tab_off(c, u, b);
     }
     a.n_items = cnt;
@@ -2078,6 +2159,168 @@ int hwkv_append(hwkv_cache *c, int32_t layer, const void *k_new,
         hwkv::launch_append(c->fmt, p.head_dim, a, (hipStream_t)stream),
         "append launch");
     if (rc != HWKV_OK) return rc;
+  }
+  for (int32_t b = 0; b < B; ++b) seq_len(c, layer, b) += 1;
+  return ok();
+}
+
+int hwkv_rope_set(hwkv_rope **out, int32_t head_dim, int32_t rot_dim, int32_t pairs,
+                  int32_t n_axes, const double *freq, const int32_t *axis, float magnitude) {
+  if (!out) return fail(HWKV_EINVAL, "out is null");
+  *out = nullptr;
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256)
+    return fail(HWKV_EINVAL, "head_dim must be 64, 128 or 256");
+  if (rot_dim < 16 || rot_dim > head_dim || rot_dim % 16 != 0)
+    return fail(HWKV_EINVAL, "rot_dim must be a multiple of 16 in [16, head_dim]");
+  if (pairs != HWKV_ROPE_HALF && pairs != HWKV_ROPE_PAIRS)
+    return fail(HWKV_EINVAL, "pairs must be HWKV_ROPE_HALF or HWKV_ROPE_PAIRS");
+  if (n_axes < 1 || n_axes > 8) return fail(HWKV_EINVAL, "n_axes must be in [1, 8]");
+  if (!freq) return fail(HWKV_EINVAL, "freq is null");
+  if (!std::isfinite(magnitude)) return fail(HWKV_EINVAL, "magnitude must be finite");
+  for (int32_t i = 0; i < rot_dim / 2; ++i) {
+    // (a position has 31 bits, and the product keeps its fraction up to 2^52 turns)
+    if (!(std::fabs(freq[i]) <= 1e6)) return fail(HWKV_EINVAL, "freq must be finite, at most 1e6");
+    if (axis && (axis[i] < 0 || axis[i] >= n_axes))
+      return fail(HWKV_EINVAL, "axis must be in [0, n_axes)");
+  }
+  hwkv_rope *r = new (std::nothrow) hwkv_rope;
+  if (!r) return fail(HWKV_ENOMEM, "host allocation failed");
+  std::memset(&r->table, 0, sizeof r->table);
+  r->head_dim = head_dim;
+  r->n_axes = n_axes;
+  r->table.rot_dim = rot_dim;
+  r->table.pairs = pairs;
+  r->table.magnitude = magnitude;
+  for (int32_t i = 0; i < rot_dim / 2; ++i) {
+    r->table.turns[i] = (double)((long double)freq[i] / 6.283185307179586476925286766559L);
+    r->table.axis[i] = (uint8_t)(axis ? axis[i] : 0);
+  }
+  *out = r;
+  return ok();
+}
+
+int hwkv_rope_free(hwkv_rope *rope) {
+  delete rope;
+  return ok();
+}
+
+int hwkv_rope_apply(const hwkv_rope *rope, int64_t n_tokens, int32_t n_q_heads,
+                    int32_t n_kv_heads, const int32_t *pos, const void *q, int64_t q_stride,
+                    const void *k, int64_t k_stride, void *q_out, void *k_out, void *stream) {
+  if (!rope) return fail(HWKV_EINVAL, "rope is null");
+  const int64_t D = rope->head_dim;
+  if (n_tokens < 0 || n_tokens >= ((int64_t)1 << 35) / D)
+    return fail(HWKV_EINVAL, "n_tokens must be >= 0 and n_tokens * head_dim below 2^35");
+  if (n_q_heads < 0 || n_kv_heads < 0 || n_q_heads > 65536 || n_kv_heads > 65536)
+    return fail(HWKV_EINVAL, "head counts must be in [0, 65536]");
+  if (n_tokens == 0 || n_q_heads + n_kv_heads == 0) return ok();
+  if (!pos || (uintptr_t)pos % 4 != 0) return fail(HWKV_EINVAL, "pos must be non-null, 4-byte aligned");
+  RowSpan span[3] = {{pos, rope->n_axes * n_tokens * 4}};
+  int rc = check_rows("q", q, q_stride, q_out, n_tokens, n_q_heads * D, &span[1]);
+  if (rc == HWKV_OK) rc = check_rows("k", k, k_stride, k_out, n_tokens, n_kv_heads * D, &span[2]);
+  if (rc == HWKV_OK && n_q_heads > 0) rc = check_apart("q_out", q_out, q, n_tokens * n_q_heads * D, q_stride == n_q_heads * D, span, 3);
+  if (rc == HWKV_OK && n_kv_heads > 0) rc = check_apart("k_out", k_out, k, n_tokens * n_kv_heads * D, k_stride == n_kv_heads * D, span, 3);
+  if (rc == HWKV_OK && n_q_heads > 0 && n_kv_heads > 0 &&
+      overlap({q_out, n_tokens * n_q_heads * D * 2}, {k_out, n_tokens * n_kv_heads * D * 2}))
+    rc = fail(HWKV_EINVAL, "q_out and k_out overlap");
+  if (rc != HWKV_OK) return rc;
+  hwkv::RopeArgs a;
+  a.rope = rope->table;
+  a.pos = pos;
+  a.q = static_cast<const uint16_t *>(q);
+  a.k = static_cast<const uint16_t *>(k);
+  a.q_out = static_cast<uint16_t *>(q_out);
+  a.k_out = static_cast<uint16_t *>(k_out);
+  a.n = n_tokens;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.n_q = n_q_heads;
+  a.n_k = n_kv_heads;
+  a.heads_per = 4;
+  rc = check_device(hwkv::launch_rope((int)D, a, (hipStream_t)stream), "rope launch");
+  return rc == HWKV_OK ? ok() : rc;
+}
+
+int hwkv_append_rope(hwkv_cache *c, int32_t layer, const hwkv_rope *rope, const int32_t *pos,
+                     const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                     const void *q, int64_t q_stride, void *q_out, void *stream) {
+  if (!c || !rope) return fail(HWKV_EINVAL, "cache and rope must be non-null");
+  const hwkv_policy &p = c->pol;
+  if (layer < 0 || layer >= p.n_layers) return fail(HWKV_EINVAL, "layer out of range");
+  if (rope->head_dim != p.head_dim)
+    return fail(HWKV_EINVAL, "the rotation's head_dim is not the cache's");
+  if (!pos || (uintptr_t)pos % 4 != 0) return fail(HWKV_EINVAL, "pos must be non-null, 4-byte aligned");
+  if ((q == nullptr) != (q_out == nullptr))
+    return fail(HWKV_EINVAL, "q and q_out are given together");
+  const int32_t H = p.n_kv_heads, B = c->batch;
+  const int64_t D = p.head_dim, G = group_size(p), n_q = q ? p.n_q_heads : 0;
+  RowSpan span[5] = {{pos, (int64_t)rope->n_axes * B * 4}, {c->base, (int64_t)c->bytes}};
+  int rc = check_rows("k_new", k_new, k_stride, k_new, B, H * D, &span[2]);
+  if (rc == HWKV_OK) rc = check_rows("v_new", v_new, v_stride, v_new, B, H * D, &span[3]);
+  if (rc == HWKV_OK) rc = check_rows("q", q, q_stride, q_out, B, n_q * D, &span[4]);
+  if (rc == HWKV_OK && q) rc = check_apart("q_out", q_out, q, B * n_q * D, q_stride == n_q * D, span, 5);
+  if (rc != HWKV_OK) return rc;
+  for (int32_t b = 0; b < B; ++b)
+    for (int32_t h = 0; h < H; ++h) {
+      const int32_t u = layer * H + h;
+      if (c->window[u] == 0 && seq_len(c, layer, b) >= c->cap[u])
+        return fail(HWKV_ECAPACITY, "append past max_ctx on a full unit");
+      if (seq_len(c, layer, b) >= INT32_MAX) return fail(HWKV_ECAPACITY, "sequence too long");
+    }
+  const hipStream_t st = (hipStream_t)stream;
+  if (c->paged) {
+    std::vector<std::pair<int32_t, int64_t>> want;
+    try {
+      for (int32_t b = 0; b < B; ++b) want.push_back({b, seq_len(c, layer, b) + 1});
+    } catch (const std::bad_alloc &) {
+      return fail(HWKV_ENOMEM, "host allocation failed");
+    }
+    rc = take_pages(c, layer, want, st);
+    if (rc != HWKV_OK) return rc;
+  }
+  hwkv::AppendRopeArgs a;
+  a.rope = rope->table;
+  a.cache = c->base;
+  a.page_table = device_page_table(c);
+  a.pool_off = c->pool_off;
+  a.pos_stride = B;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out_stride = n_q * D;
+  a.group = q ? (int32_t)G : 0;
+  a.n_sinks = p.n_sinks;
+  a.max_pages = (int32_t)c->max_pages;
+  for (int32_t h0 = 0; h0 < H; h0 += hwkv::kRopeHeads) {
+    a.n_heads = std::min(hwkv::kRopeHeads, H - h0);
+    for (int32_t b0 = 0; b0 < B; b0 += hwkv::kRopeSeqs) {
+      a.n_seqs = std::min(hwkv::kRopeSeqs, B - b0);
+      for (int32_t j = 0; j < a.n_heads; ++j) {
+        const int32_t u = layer * H + h0 + j;
+        const int64_t rows = (int64_t)b0 * c->cap_pad[u];
+        hwkv::ItemHead &hd = a.head[j];
+        hd.k_off = c->k_off[u] + rows * D;
+        hd.v_off = c->v_off[u] + rows * D;
+        hd.cap = (int32_t)c->cap[u];
+        hd.cap_pad = (int32_t)c->cap_pad[u];
+        hd.window = (int32_t)c->window[u];
+        hd.page0 = page_tab_off(c, u, b0);
+        if (c->fmt == HWKV_KV_I8) {
+          hd.s_off = c->s_off[u] + rows * hwkv::kRowScaleBytes;
+        } else {
+          hd.k_scale = c->k_scale[u];
+          hd.v_scale = c->v_scale[u];
+        }
+      }
+      for (int32_t i = 0; i < a.n_seqs; ++i) a.len[i] = (int32_t)seq_len(c, layer, b0 + i);
+      a.pos = pos + b0;
+      a.q = q ? static_cast<const uint16_t *>(q) + b0 * q_stride + h0 * G * D : nullptr;
+      a.q_out = q ? static_cast<uint16_t *>(q_out) + (b0 * n_q + h0 * G) * D : nullptr;
+      a.k = static_cast<const uint16_t *>(k_new) + b0 * k_stride + h0 * D;
+      a.v = static_cast<const uint16_t *>(v_new) + b0 * v_stride + h0 * D;
+      rc = check_device(hwkv::launch_append_rope(c->fmt, (int)D, a, st), "append rope launch");
+      if (rc != HWKV_OK) return rc;
+    }
   }
   for (int32_t b = 0; b < B; ++b) seq_len(c, layer, b) += 1;
   return ok();
@@ -2183,7 +2426,7 @@ int hwkv_cache_read_unit(const hwkv_cache *c, int32_t layer, int32_t kv_head,
     const int32_t have = c->held[(size_t)(pto / c->max_pages)];
     for (int32_t j = 0; j < have; ++j) {
       const int64_t pg = c->pt_host[(size_t)pto + j];
-      const uint8_t *src = c->base + (c->pool_off + pg * 2 * PT * D) * E;
+      const uint8_t *src = c->base + (c->pool_off + pg * page_elems(p, c->fmt)) * E;
       const int64_t rows = std::min(PT, cap - j * PT);
       rc = check_device(hipMemcpy(tiles.data() + j * PT * D * E, src,
                                   (size_t)(std::min(PT, capp - j * PT) * D * E),
@@ -2214,6 +2457,46 @@ int hwkv_cache_read_unit(const hwkv_cache *c, int32_t layer, int32_t kv_head,
                   tiles.data() + ((t * NC + g) * hwkv::kTile + sl) * LB, (size_t)LB);
   }
   *n_valid = std::min(c->n[(size_t)layer * c->batch + seq], cap);
+  return ok();
+}
+
+int hwkv_cache_read_scales(const hwkv_cache *c, int32_t layer, int32_t kv_head,
+                           int32_t seq, uint8_t *host_k, uint8_t *host_v) {
+  if (!c || !host_k || !host_v) return fail(HWKV_EINVAL, "null argument");
+  const hwkv_policy &p = c->pol;
+  if (layer < 0 || layer >= p.n_layers || kv_head < 0 ||
+      kv_head >= p.n_kv_heads || seq < 0 || seq >= c->batch)
+    return fail(HWKV_EINVAL, "layer, kv_head or seq out of range");
+  if (c->fmt != HWKV_KV_I8) return fail(HWKV_EINVAL, "only int8 caches hold row scales");
+  const int32_t u = layer * p.n_kv_heads + kv_head;
+  const int64_t cap = c->cap[u], B = hwkv::kRowScaleBytes, PT = hwkv::kPageTokens;
+  std::vector<uint8_t> pairs;
+  try {
+    pairs.resize((size_t)(cap * B));
+  } catch (const std::bad_alloc &) {
+    return fail(HWKV_ENOMEM, "host allocation failed");
+  }
+  int rc = check_device(hipDeviceSynchronize(), "synchronize");
+  const int32_t pto = page_tab_off(c, u, seq);
+  if (pto >= 0) {
+    const int32_t have = c->held[(size_t)(pto / c->max_pages)];
+    for (int32_t j = 0; rc == HWKV_OK && j < have; ++j) {
+      const int64_t pg = c->pt_host[(size_t)pto + j];
+      const uint8_t *src = c->base + c->pool_off + pg * page_elems(p, c->fmt) + 2 * PT * p.head_dim;
+      rc = check_device(hipMemcpy(pairs.data() + j * PT * B, src,
+                                  (size_t)(std::min(PT, cap - j * PT) * B), hipMemcpyDeviceToHost),
+                        "copy scale page");
+    }
+  } else if (rc == HWKV_OK) {
+    rc = check_device(hipMemcpy(pairs.data(), c->base + c->s_off[u] + (int64_t)seq * c->cap_pad[u] * B,
+                                (size_t)(cap * B), hipMemcpyDeviceToHost),
+                      "copy scales");
+  }
+  if (rc != HWKV_OK) return rc;
+  for (int64_t j = 0; j < cap; ++j) {
+    host_k[j] = pairs[(size_t)(j * B)];
+    host_v[j] = pairs[(size_t)(j * B + 1)];
+  }
   return ok();
 }
 

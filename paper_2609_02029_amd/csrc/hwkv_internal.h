@@ -20,6 +20,10 @@
 // a pool after the finite units' regions; page j of (unit, sequence) is
 // page_table[pto + j], where pto = (full unit index * batch + sequence) *
 // pages per max_ctx.  A page holds whole decode and prefill key tiles.
+//
+// int8 caches keep a pair of scale bytes per row (kv_rows8.h): s_off below is
+// the byte offset of a (unit, sequence) region's pairs; a page's follow its V
+// rows.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -31,6 +35,7 @@ namespace hwkv {
 constexpr int kTile = 64;        // token slots per K tile (= wavefront width)
 constexpr int kMaxItems = 64;    // (sequence, kv-head) items per launch
 constexpr int kPageTokens = 256; // rows per page of a paged full unit
+constexpr int kRowScaleBytes = 2;  // int8 caches: scale bytes of a token row (K's, V's)
 constexpr int kDecodeWaves = 4;  // waves of a decode split workgroup
 #ifndef HWKV_DECODE_WG_PER_CU_X4
 #define HWKV_DECODE_WG_PER_CU_X4 8
@@ -52,8 +57,13 @@ struct DecodeItems {
   int32_t new_slot[kMaxItems];   // slot taking the appended token, or -1
   int32_t q_row[kMaxItems];      // b * n_q_heads + h * G (first q head)
   int32_t kv_row[kMaxItems];     // b * n_kv_heads + h (row of k_new/v_new)
-  float k_scale[kMaxItems];      // fp8 scales of the item's unit (else 1)
-  float v_scale[kMaxItems];
+  union {
+    struct {
+      float k_scale[kMaxItems];  // fp8 scales of the item's unit (else 1)
+      float v_scale[kMaxItems];
+    };
+    int64_t s_off[kMaxItems];    // int8: scale pairs of the item
+  };
   int32_t pto[kMaxItems];        // page-table offset of a paged unit, or -1
   int32_t split_begin[kMaxItems + 1];
   int32_t n_items;
@@ -86,7 +96,12 @@ struct ItemHead {
   int32_t cap, cap_pad;          // rows holding data; rows allocated
   int32_t window;                // 0 = full
   int32_t page0;                 // page-table offset of sequence 0, or -1
-  float k_scale, v_scale;        // fp8 scales of the unit (else 1)
+  union {
+    struct {
+      float k_scale, v_scale;    // fp8 scales of the unit (else 1)
+    };
+    int64_t s_off;               // int8: scale pairs of the unit, sequence 0
+  };
 };
 struct ItemArgs {
   ItemHead head[kMaxItems];
@@ -129,7 +144,12 @@ struct WriteHead {
   int32_t pto;                   // page-table offset of a paged unit, or -1
   int32_t tile0[3];
   int32_t n_tiles[3];
-  float k_scale, v_scale;        // fp8 scales of the unit (else 1)
+  union {
+    struct {
+      float k_scale, v_scale;    // fp8 scales of the unit (else 1)
+    };
+    int64_t s_off;               // int8: scale pairs of the (unit, seq)
+  };
 };
 
 struct WriteArgs {
@@ -149,8 +169,13 @@ struct AppendArgs {
   int64_t v_off[kMaxItems];
   int32_t slot[kMaxItems];
   int32_t kv_row[kMaxItems];
-  float k_scale[kMaxItems];
-  float v_scale[kMaxItems];
+  union {
+    struct {
+      float k_scale[kMaxItems];
+      float v_scale[kMaxItems];
+    };
+    int64_t s_off[kMaxItems];    // int8: scale pairs of the item
+  };
   int32_t pto[kMaxItems];        // page-table offset of a paged unit, or -1
   int32_t n_items;
   void *cache;
@@ -159,6 +184,48 @@ struct AppendArgs {
   const uint16_t *k_new;
   const uint16_t *v_new;
 };
+
+// A rotation of the first rot_dim channels of a head (rope_kernels.hip): pair
+// i turns by pos[axis[i]] * turns[i] whole turns.
+constexpr int kMaxPairs = 128;   // rot_dim / 2 at head_dim 256
+struct RopeTable {
+  double turns[kMaxPairs];       // turns per position, of each pair
+  uint8_t axis[kMaxPairs];
+  int32_t rot_dim;
+  int32_t pairs;                 // HWKV_ROPE_*: which channels make a pair
+  float magnitude;
+};
+
+// Rotation of n tokens' q and k heads: grid x over (token, 16 channels of a
+// head), grid y over the heads in groups of heads_per.
+struct RopeArgs {
+  RopeTable rope;
+  const int32_t *pos;            // [n_axes][n]
+  const uint16_t *q, *k;         // rows of n_q, n_k heads, q_stride / k_stride apart
+  uint16_t *q_out, *k_out;       // [n][heads][D]
+  int64_t n, q_stride, k_stride; // strides in elements
+  int32_t n_q, n_k, heads_per;
+};
+hipError_t launch_rope(int D, const RopeArgs &a, hipStream_t s);
+
+// Append of one token of up to kRopeSeqs sequences to up to kRopeHeads KV heads,
+// rotated on the way.
+constexpr int kRopeHeads = 32, kRopeSeqs = 192;
+struct AppendRopeArgs {
+  RopeTable rope;
+  ItemHead head[kRopeHeads];
+  int32_t len[kRopeSeqs];        // length before the append
+  void *cache;
+  const int32_t *page_table;     // paged caches (else null)
+  int64_t pool_off;
+  const int32_t *pos;            // position of the launch's first sequence
+  int64_t pos_stride;            // between axes
+  const uint16_t *q, *k, *v;     // of the launch's first sequence and head
+  uint16_t *q_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;   // between sequences
+  int32_t n_seqs, n_heads, group, n_sinks, max_pages;
+};
+hipError_t launch_append_rope(int fmt, int D, const AppendRopeArgs &a, hipStream_t s);
 
 // Page-table entries to install (table[idx[i]] = page[i]) before the
 // kernels of a call that took new pages read them.
@@ -252,6 +319,8 @@ template <int F>
 hipError_t launch_decode_split_fmt(int D, int G, const DecodeArgs &a,
                                    int n_splits, hipStream_t s, hipEvent_t e0,
                                    hipEvent_t e1);
+hipError_t launch_decode_i8(int D, int G, const DecodeArgs &a, int n_splits, hipStream_t s,
+                            hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_decode_item(int fmt, int D, int G, const ItemArgs &a, hipStream_t s,
                               hipEvent_t e0 = nullptr, hipEvent_t e1 = nullptr);
 hipError_t launch_item_merge(int D, int G, const ItemArgs &a, hipStream_t s,
@@ -270,30 +339,32 @@ hipError_t launch_prefill_write(int fmt, int D, const WriteArgs &a,
 hipError_t launch_append(int fmt, int D, const AppendArgs &a, hipStream_t s);
 hipError_t launch_page_update(const PageUpdateArgs &a, hipStream_t s);
 
-// Staging of an fp8 cache for prefill attention: rows [0, n_rows) of one
-// (unit, sequence) widened to bf16 code values in the bf16 cache layout, and
-// a chunk's K or V quantised as the cache stores it and widened.
+// Staging of an fp8 or int8 cache for prefill attention: rows [0, n_rows) of
+// one (unit, sequence) widened to bf16 -- fp8 code values, int8 values -- in
+// the bf16 cache layout, and a chunk's K or V quantised as the cache stores it
+// and widened.
 struct StageUnit {
-  int64_t src_k_off, src_v_off;  // fp8 element offsets (unpaged units)
+  int64_t src_k_off, src_v_off;  // element offsets (unpaged units)
+  int64_t src_s_off;             // int8: scale pairs (unpaged units)
   int64_t dst_k_off, dst_v_off;  // bf16 element offsets in the image
   int32_t pto;                   // page-table offset of a paged unit, or -1
   int32_t n_rows;                // occupied slots to stage
 };
 struct StageArgs {
   StageUnit unit[kMaxItems];     // one per kv head of the layer
-  const uint8_t *cache;          // fp8 cache base
+  const uint8_t *cache;          // cache base
   const int32_t *page_table;
   int64_t pool_off;
   uint16_t *image;               // bf16 image base
   int32_t n_units;
   int32_t max_chunks;            // max over units of n_rows * D / 8 (per K or V)
 };
-hipError_t launch_stage_units(int D, const StageArgs &a, hipStream_t s);
+hipError_t launch_stage_units(int fmt, int D, const StageArgs &a, hipStream_t s);
 struct StageChunkArgs {
-  int32_t fmt;                   // HWKV_KV_FP8_E4M3 or HWKV_KV_F16
+  int32_t fmt;                   // HWKV_KV_FP8_E4M3, HWKV_KV_I8 or HWKV_KV_F16
   const uint16_t *k, *v;         // [n_tokens][Hkv][D] bf16 inputs
   uint16_t *k_out, *v_out;       // the same layout: the stored values, as bf16
-                                 // code values (fp8) or binary16 (f16)
+                                 // code values (fp8), bf16 (i8) or binary16 (f16)
   float k_scale[kMaxItems];      // per kv head of the layer
   float v_scale[kMaxItems];
   int64_t n_chunks;              // n_tokens * Hkv * D / 8
@@ -375,6 +446,8 @@ static_assert(sizeof(hwkv::DecodeArgs) <= 4096, "decode kernarg too large");
 static_assert(sizeof(hwkv::ItemArgs) <= 4096, "decode item kernarg too large");
 static_assert(sizeof(hwkv::WriteArgs) <= 4096, "write kernarg too large");
 static_assert(sizeof(hwkv::AppendArgs) <= 4096, "append kernarg too large");
+static_assert(sizeof(hwkv::RopeArgs) <= 4096, "rope kernarg too large");
+static_assert(sizeof(hwkv::AppendRopeArgs) <= 4096, "append rope kernarg too large");
 static_assert(sizeof(hwkv::PageUpdateArgs) <= 4096, "page update kernarg too large");
 static_assert(sizeof(hwkv::StageArgs) <= 4096, "stage kernarg too large");
 static_assert(sizeof(hwkv::StageChunkArgs) <= 4096, "stage chunk kernarg too large");

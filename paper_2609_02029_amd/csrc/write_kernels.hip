@@ -16,6 +16,7 @@
 
 #include "hwkv_internal.h"
 #include "kv_format.h"
+#include "kv_rows8.h"
 
 namespace hwkv {
 namespace {
@@ -27,6 +28,7 @@ __global__ __launch_bounds__(256) void prefill_write(WriteArgs a) {
   constexpr int EB = KvFormat<F>::kBytes;
   constexpr int LB = 8 * EB;
   __shared__ int64_t src_row[kTile];  // source row of each slot, or -1
+  __shared__ uint32_t k_exp[F == HWKV_KV_I8 ? kTile : 1];   // scale of each slot's K row
   const int h = blockIdx.y;
   const WriteHead &wh = a.head[h];
   int x = blockIdx.x, tile = -1;
@@ -61,17 +63,44 @@ __global__ __launch_bounds__(256) void prefill_write(WriteArgs a) {
 
   uint8_t *const cache = static_cast<uint8_t *>(a.cache);
   uint8_t *kt, *vt;     // this tile's K tile and its first V row
+  uint8_t *st = nullptr;  // and its scale pairs (int8)
   if (wh.pto >= 0) {    // paged: tile `tile % 4` of page tile / 4
     constexpr int TPP = kPageTokens / kTile;
     const int64_t pg = a.page_table[wh.pto + tile / TPP];
-    const int64_t base = a.pool_off + pg * 2 * kPageTokens * D;
+    const int64_t base = a.pool_off + pg * page_elems<F>(D);
     kt = cache + (base + (int64_t)(tile % TPP) * kTile * D) * EB;
     vt = cache + (base + (int64_t)kPageTokens * D + (int64_t)(tile % TPP) * kTile * D) * EB;
+    st = cache + base + (int64_t)2 * kPageTokens * D + tile % TPP * (kTile * kRowScaleBytes);
   } else {
     kt = cache + (wh.k_off + (size_t)tile * kTile * D) * EB;
     vt = cache + (wh.v_off + (size_t)tile * kTile * D) * EB;
+    if constexpr (F == HWKV_KV_I8) st = cache + wh.s_off + (size_t)tile * kTile * kRowScaleBytes;
   }
   const size_t row_stride = (size_t)a.n_kv_heads * D;
+  if constexpr (F == HWKV_KV_I8) {
+    // V rows and their scales, NC lanes to a row; the scales of K
+    for (int e = threadIdx.x; e < kTile * NC; e += 256) {
+      const int sl = e / NC, g = e % NC;
+      const int64_t r = src_row[sl];
+      const size_t at = max(r, (int64_t)0) * row_stride + h * D + g * 8;
+      const uint4 k = *reinterpret_cast<const uint4 *>(a.k + at);
+      const uint4 v = *reinterpret_cast<const uint4 *>(a.v + at);
+      const uint32_t ke = row_scale(group_max<NC>(top8(k)));
+      const uint32_t ve = row_scale(group_max<NC>(top8(v)));
+      if (g == 0) k_exp[sl] = ke;
+      if (r < 0) continue;
+      if (g == 0) *reinterpret_cast<uint16_t *>(st + sl * kRowScaleBytes) = (uint16_t)(ke | ve << 8);
+      store_chunk<F>(vt + (size_t)sl * D + g * LB, encode8_row(v, ve));
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < kTile * NC; e += 256) {
+      const int sl = e & (kTile - 1), g = e >> 6;
+      const int64_t r = src_row[sl];
+      if (r < 0) continue;
+      const uint4 k = *reinterpret_cast<const uint4 *>(a.k + r * row_stride + h * D + g * 8);
+      store_chunk<F>(kt + ((size_t)g * kTile + sl) * LB, encode8_row(k, k_exp[sl]));
+    }
+  } else {
   // K: thread -> (chunk g, slot), slot fastest: coalesced tile stores
   for (int e = threadIdx.x; e < kTile * NC; e += 256) {
     const int sl = e & (kTile - 1), g = e >> 6;
@@ -90,6 +119,7 @@ __global__ __launch_bounds__(256) void prefill_write(WriteArgs a) {
         *reinterpret_cast<const uint4 *>(a.v + r * row_stride + h * D + g * 8);
     store_chunk<F>(vt + (size_t)sl * D * EB + g * LB, encode8<F>(val, wh.v_scale));
   }
+  }
 }
 
 // One workgroup of 64 lanes per (sequence, kv head): lanes [0, NC) copy K
@@ -105,18 +135,32 @@ __global__ __launch_bounds__(64) void append_token(AppendArgs a) {
   const size_t src = (size_t)a.kv_row[i] * D;
   uint8_t *const cache = static_cast<uint8_t *>(a.cache);
   // the K region and V region holding `slot`, and its row r in them
-  int64_t koff, voff;
+  int64_t koff, voff, soff = 0;
   int r = slot;
   if (a.pto[i] >= 0) {  // paged: row slot % 256 of page slot / 256
     const int64_t pg = a.page_table[a.pto[i] + slot / kPageTokens];
-    koff = a.pool_off + pg * 2 * kPageTokens * D;
+    koff = a.pool_off + pg * page_elems<F>(D);
     voff = koff + (int64_t)kPageTokens * D;
+    soff = voff + (int64_t)kPageTokens * D;
     r = slot % kPageTokens;
   } else {
     koff = a.k_off[i];
     voff = a.v_off[i];
+    if constexpr (F == HWKV_KV_I8) soff = a.s_off[i];
   }
-  if (t < NC) {
+  if constexpr (F == HWKV_KV_I8) {
+    const int g = t % NC;
+    const uint16_t *from = (t < NC ? a.k_new : a.v_new) + src + g * 8;
+    uint4 val = make_uint4(0u, 0u, 0u, 0u);
+    if (t < 2 * NC) val = *reinterpret_cast<const uint4 *>(from);
+    const uint32_t e = row_scale(group_max<NC>(top8(val)));
+    if (t < 2 * NC) {
+      uint8_t *const to = t < NC ? cache + koff + (size_t)(r / kTile) * kTile * D + ((size_t)g * kTile + r % kTile) * LB
+                                 : cache + voff + (size_t)r * D + g * LB;
+      store_chunk<F>(to, encode8_row(val, e));
+      if (g == 0) cache[soff + (size_t)r * kRowScaleBytes + t / NC] = (uint8_t)e;
+    }
+  } else if (t < NC) {
     uint8_t *kt = cache + (koff + (size_t)(r / kTile) * kTile * D) * EB;
     const uint4 val = *reinterpret_cast<const uint4 *>(a.k_new + src + t * 8);
     store_chunk<F>(kt + ((size_t)t * kTile + r % kTile) * LB,
@@ -144,12 +188,13 @@ __device__ __forceinline__ uint4 widen_fp8x8(uint2 c) {
   return make_uint4(w(c.x, false), w(c.x, true), w(c.y, false), w(c.y, true));
 }
 
-// Staging of an fp8 cache for prefill attention: the occupied rows of each
-// (unit, sequence) of a layer widened to bf16 code values, in the layout of
-// a bf16 cache (K tiles chunk for chunk, V rows), into an image the bf16
-// kernel reads.  blockIdx.y: the unit; blockIdx.z: 0 = K, 1 = V.  Whole K
-// tiles are staged (rows past the occupied ones are never read).
-template <int D>
+// Staging of an fp8 or int8 cache for prefill attention: the occupied rows of
+// each (unit, sequence) of a layer widened to bf16 (fp8 code values; int8
+// values, with their row's scale), in the layout of a bf16 cache (K tiles chunk
+// for chunk, V rows), into an image the bf16 kernel reads.  blockIdx.y: the
+// unit; blockIdx.z: 0 = K, 1 = V.  Whole K tiles are staged (rows past the
+// occupied ones are never read).
+template <int D, int F>
 __global__ __launch_bounds__(256) void stage_units(StageArgs a) {
   constexpr int NC = D / 8;
   constexpr int TPP = kPageTokens / kTile;
@@ -159,27 +204,37 @@ __global__ __launch_bounds__(256) void stage_units(StageArgs a) {
                         : (int64_t)((su.n_rows + kTile - 1) / kTile) * kTile * NC;
   for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n;
        c += (int64_t)gridDim.x * 256) {
-    int64_t src;
+    // K chunk c: position r of tile t; V chunk c: chunk g of row j
+    const int64_t row = isv ? c / NC : c / (kTile * NC) * kTile + c % kTile;
+    int64_t src, sc = 0;        // the codes, and the row's scale byte (int8)
     if (su.pto < 0) {
       src = (isv ? su.src_v_off : su.src_k_off) + c * 8;
-    } else if (!isv) {          // K chunk c: tile t, position r in the tile
+      sc = su.src_s_off + row * kRowScaleBytes + (isv ? 1 : 0);
+    } else if (!isv) {
       const int64_t t = c / (kTile * NC), r = c % (kTile * NC);
       const int64_t pg = a.page_table[su.pto + t / TPP];
-      src = a.pool_off + pg * 2 * kPageTokens * D + (t % TPP) * kTile * D + r * 8;
-    } else {                    // V chunk c: row j, chunk g
+      src = a.pool_off + pg * page_elems<F>(D) + (t % TPP) * kTile * D + r * 8;
+      sc = a.pool_off + pg * page_elems<F>(D) + 2 * kPageTokens * D + row % kPageTokens * kRowScaleBytes;
+    } else {
       const int64_t j = c / NC, g = c % NC;
       const int64_t pg = a.page_table[su.pto + j / kPageTokens];
-      src = a.pool_off + pg * 2 * kPageTokens * D + (int64_t)kPageTokens * D +
+      src = a.pool_off + pg * page_elems<F>(D) + (int64_t)kPageTokens * D +
             (j % kPageTokens) * D + g * 8;
+      sc = a.pool_off + pg * page_elems<F>(D) + 2 * kPageTokens * D + row % kPageTokens * kRowScaleBytes + 1;
     }
     const uint2 codes = *reinterpret_cast<const uint2 *>(a.cache + src);
-    *reinterpret_cast<uint4 *>(a.image + (isv ? su.dst_v_off : su.dst_k_off) + c * 8) =
-        widen_fp8x8(codes);
+    uint4 *const to = reinterpret_cast<uint4 *>(a.image + (isv ? su.dst_v_off : su.dst_k_off) + c * 8);
+    if constexpr (F == HWKV_KV_I8)
+      *to = widen8_row(codes, a.cache[sc]);
+    else
+      *to = widen_fp8x8(codes);
   }
 }
 
 // The chunk's own K and V as the cache will store them: fp8 codes (code(x /
-// s) of the unit's scale) widened to bf16 code values, or binary16 values.
+// s) of the unit's scale) widened to bf16 code values, int8 codes widened to
+// their values, or binary16 values.  (The NC chunks of a row are NC lanes of one
+// wavefront, and in or out of range together.)
 template <int D, int F>
 __global__ __launch_bounds__(256) void stage_chunk(StageChunkArgs a) {
   constexpr int NC = D / 8;
@@ -191,6 +246,11 @@ __global__ __launch_bounds__(256) void stage_chunk(StageChunkArgs a) {
     if constexpr (F == HWKV_KV_F16) {
       *reinterpret_cast<uint4 *>(a.k_out + c * 8) = encode8<HWKV_KV_F16>(k, 1.0f);
       *reinterpret_cast<uint4 *>(a.v_out + c * 8) = encode8<HWKV_KV_F16>(v, 1.0f);
+    } else if constexpr (F == HWKV_KV_I8) {
+      const uint32_t ke = row_scale(group_max<NC>(top8(k)));
+      const uint32_t ve = row_scale(group_max<NC>(top8(v)));
+      *reinterpret_cast<uint4 *>(a.k_out + c * 8) = widen8_row(encode8_row(k, ke), ke);
+      *reinterpret_cast<uint4 *>(a.v_out + c * 8) = widen8_row(encode8_row(v, ve), ve);
     } else {
       *reinterpret_cast<uint4 *>(a.k_out + c * 8) =
           widen_fp8x8(encode8<HWKV_KV_FP8_E4M3>(k, a.k_scale[h]));
@@ -208,6 +268,7 @@ hipError_t dispatch_df(int fmt, int D, Args &&...args) {
     case HWKV_KV_BF16: return L<DD, HWKV_KV_BF16>::run(args...);          \
     case HWKV_KV_F16: return L<DD, HWKV_KV_F16>::run(args...);            \
     case HWKV_KV_FP8_E4M3: return L<DD, HWKV_KV_FP8_E4M3>::run(args...);  \
+    case HWKV_KV_I8: return L<DD, HWKV_KV_I8>::run(args...);              \
     default: return hipErrorInvalidValue;                                 \
   }
   switch (D) {
@@ -247,35 +308,42 @@ hipError_t launch_append(int fmt, int D, const AppendArgs &a, hipStream_t s) {
   return dispatch_df<AppendLaunch>(fmt, D, a, s);
 }
 
-hipError_t launch_stage_units(int D, const StageArgs &a, hipStream_t s) {
+hipError_t launch_stage_units(int fmt, int D, const StageArgs &a, hipStream_t s) {
   const int64_t per = 256;
   const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((a.max_chunks + per - 1) / per, 2048)),
                   (unsigned)a.n_units, 2);
+#define HWKV_SU(DD)                                                                    \
+  if (fmt == HWKV_KV_I8)                                                               \
+    hipLaunchKernelGGL((stage_units<DD, HWKV_KV_I8>), grid, dim3(256), 0, s, a);       \
+  else if (fmt == HWKV_KV_FP8_E4M3)                                                    \
+    hipLaunchKernelGGL((stage_units<DD, HWKV_KV_FP8_E4M3>), grid, dim3(256), 0, s, a); \
+  else                                                                                 \
+    return hipErrorInvalidValue
   switch (D) {
-    case 64: hipLaunchKernelGGL(stage_units<64>, grid, dim3(256), 0, s, a); break;
-    case 128: hipLaunchKernelGGL(stage_units<128>, grid, dim3(256), 0, s, a); break;
-    case 256: hipLaunchKernelGGL(stage_units<256>, grid, dim3(256), 0, s, a); break;
+    case 64: HWKV_SU(64); break;
+    case 128: HWKV_SU(128); break;
+    case 256: HWKV_SU(256); break;
     default: return hipErrorInvalidValue;
   }
+#undef HWKV_SU
   return hipGetLastError();
 }
 
+template <int D, int F>
+struct StageChunkLaunch {
+  static hipError_t run(const StageChunkArgs &a, dim3 grid, hipStream_t s) {
+    if constexpr (F == HWKV_KV_BF16) {
+      return hipErrorInvalidValue;
+    } else {
+      hipLaunchKernelGGL((stage_chunk<D, F>), grid, dim3(256), 0, s, a);
+      return hipGetLastError();
+    }
+  }
+};
+
 hipError_t launch_stage_chunk(int D, const StageChunkArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((a.n_chunks + 255) / 256, 4096)));
-  if (a.fmt != HWKV_KV_F16 && a.fmt != HWKV_KV_FP8_E4M3) return hipErrorInvalidValue;
-#define HWKV_SC(DD)                                                                   \
-  if (a.fmt == HWKV_KV_F16)                                                           \
-    hipLaunchKernelGGL((stage_chunk<DD, HWKV_KV_F16>), grid, dim3(256), 0, s, a);     \
-  else                                                                                \
-    hipLaunchKernelGGL((stage_chunk<DD, HWKV_KV_FP8_E4M3>), grid, dim3(256), 0, s, a)
-  switch (D) {
-    case 64: HWKV_SC(64); break;
-    case 128: HWKV_SC(128); break;
-    case 256: HWKV_SC(256); break;
-    default: return hipErrorInvalidValue;
-  }
-#undef HWKV_SC
-  return hipGetLastError();
+  return dispatch_df<StageChunkLaunch>(a.fmt, D, a, grid, s);
 }
 
 hipError_t launch_page_update(const PageUpdateArgs &a, hipStream_t s) {

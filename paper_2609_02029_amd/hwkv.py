@@ -16,7 +16,7 @@ LIB_PATH = os.environ.get("HWKV_LIBRARY") or os.path.join(_HERE, "_lib", "libhwk
 
 OK, EINVAL, ENOMEM, ECAPACITY, ESTATE, EDEVICE = 0, 1, 2, 3, 4, 5
 # cache formats (HWKV_KV_*): name -> (code, bytes per element)
-KV_FORMATS = {"bf16": (0, 2), "f16": (1, 2), "fp8": (2, 1)}
+KV_FORMATS = {"bf16": (0, 2), "f16": (1, 2), "fp8": (2, 1), "i8": (4, 1)}
 PAGE_TOKENS = 256   # rows per page of a paged cache's full units
 _NAMES = {EINVAL: "EINVAL", ENOMEM: "ENOMEM", ECAPACITY: "ECAPACITY",
           ESTATE: "ESTATE", EDEVICE: "EDEVICE"}
@@ -72,6 +72,13 @@ SYMBOLS = {
     "hwkv_decode_attn": ([_vp, _i32, _vp, _flt, _vp, _vp, _sz, _vp], ctypes.c_int),
     "hwkv_append_decode_attn": ([_vp, _i32, _vp, _vp, _vp, _flt, _vp, _vp, _sz, _vp], ctypes.c_int),
     "hwkv_append_decode_attn_noalloc": ([_vp, _i32, _vp, _vp, _vp, _flt, _vp, _vp], ctypes.c_int),
+    "hwkv_cache_read_scales": ([_vp, _i32, _i32, _i32, _vp, _vp], ctypes.c_int),
+    "hwkv_rope_set": ([_P(_vp), _i32, _i32, _i32, _i32, _vp, _vp, _flt], ctypes.c_int),
+    "hwkv_rope_free": ([_vp], ctypes.c_int),
+    "hwkv_rope_apply": ([_vp, _i64, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp],
+                        ctypes.c_int),
+    "hwkv_append_rope": ([_vp, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp],
+                         ctypes.c_int),
     "hwkv_cache_read_unit": ([_vp, _i32, _i32, _i32, _vp, _vp, _P(_i64)], ctypes.c_int),
     "hwkv_decode_timing": ([_vp, _i32], ctypes.c_int),
     "hwkv_decode_timing_read": ([_vp, _P(_dbl), _P(_dbl), _P(_i64)], ctypes.c_int),
@@ -240,7 +247,7 @@ def _scales(policy, x):
 def cache_alloc(policy, batch, max_ctx, dev_buf=None, kv_format="bf16", k_scale=None,
                 v_scale=None, n_pages=None):
     """``dev_buf``: optional uint8 device tensor to adopt (kept alive).
-    ``kv_format``: "bf16", "f16" or "fp8"; ``k_scale``/``v_scale``: fp8 scales,
+    ``kv_format``: "bf16", "f16", "fp8" or "i8"; ``k_scale``/``v_scale``: fp8 scales,
     a scalar or ``[n_layers, n_kv_heads]`` (None = 1.0).  ``n_pages`` (not
     None): full units are paged from a pool of that many pages."""
     h = _vp()
@@ -308,10 +315,10 @@ def cache_unit_info(cache, layer, kv_head):
 
 def cache_read_unit(cache, layer, kv_head, seq):
     """Returns (k, v, n_valid): numpy [capacity, head_dim] stored elements --
-    uint16 bit patterns (bf16, f16) or uint8 E4M3 codes (fp8)."""
+    uint16 bit patterns (bf16, f16), uint8 E4M3 codes (fp8) or int8 codes (i8)."""
     import numpy as np
     cap, _ = cache_unit_info(cache, layer, kv_head)
-    dt = np.uint8 if getattr(cache, "kv_format", "bf16") == "fp8" else np.uint16
+    dt = {"fp8": np.uint8, "i8": np.int8}.get(getattr(cache, "kv_format", "bf16"), np.uint16)
     k = np.empty((cap, cache.head_dim), dtype=dt)
     v = np.empty((cap, cache.head_dim), dtype=dt)
     nv = _i64()
@@ -319,6 +326,99 @@ def cache_read_unit(cache, layer, kv_head, seq):
                                      k.ctypes.data_as(_vp), v.ctypes.data_as(_vp),
                                      ctypes.byref(nv)))
     return k, v, nv.value
+
+
+def cache_read_scales(cache, layer, kv_head, seq):
+    """Scale bytes (k, v) of an "i8" cache's rows: numpy uint8 [capacity] each,
+    in slot order."""
+    import numpy as np
+    cap, _ = cache_unit_info(cache, layer, kv_head)
+    k, v = np.empty(cap, dtype=np.uint8), np.empty(cap, dtype=np.uint8)
+    _check(_lib.hwkv_cache_read_scales(cache.handle, layer, kv_head, seq, k.ctypes.data_as(_vp),
+                                       v.ctypes.data_as(_vp)))
+    return k, v
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+class Rope:
+    """Owns an ``hwkv_rope*``."""
+
+    _free = _lib.hwkv_rope_free
+
+    def __init__(self, handle, head_dim, n_axes):
+        self.handle, self.head_dim, self.n_axes = handle, head_dim, n_axes
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            self._free(self.handle)
+            self.handle = None
+
+
+ROPE_PAIRS = {"half": 0, "pairs": 1}
+
+
+def rope_set(head_dim, freq, axis=None, n_axes=1, pairing="half", magnitude=1.0):
+    """A rotation of the first ``2 * len(freq)`` channels of each head: pair i
+    turns by ``pos[axis[i]] * freq[i]`` radians.  ``pairing``: "half" (channels i
+    and i + rot_dim / 2) or "pairs" (2i and 2i + 1)."""
+    import numpy as np
+    if pairing not in ROPE_PAIRS:
+        raise ValueError(f"pairing must be one of {sorted(ROPE_PAIRS)}")
+    f = np.ascontiguousarray(freq, dtype=np.float64)
+    a = None if axis is None else np.ascontiguousarray(axis, dtype=np.int32)
+    if f.ndim != 1 or (a is not None and a.shape != f.shape):
+        raise ValueError("freq and axis must hold one entry per pair")
+    h = _vp()
+    _check(_lib.hwkv_rope_set(ctypes.byref(h), head_dim, 2 * f.size, ROPE_PAIRS[pairing], n_axes,
+                              f.ctypes.data_as(_vp), None if a is None else a.ctypes.data_as(_vp),
+                              float(magnitude)))
+    return Rope(h, head_dim, n_axes)
+
+
+def rope_free(rope):
+    if rope.handle:
+        _check(_lib.hwkv_rope_free(rope.handle))
+        rope.handle = None
+
+
+def _rows(t, heads, head_dim, what):
+    """(address, tokens, elements between tokens) of bf16 [n, heads, head_dim]
+    rows, whose tokens may lie apart (a slice of a wider row)."""
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError(f"{what} must be a bfloat16 device tensor")
+    if t.dim() != 3 or t.shape[2] != head_dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{what} must be [n, heads, head_dim]")
+    n, h, d = t.shape
+    if t.numel() and (t.stride(2) != 1 or (h > 1 and t.stride(1) != d)):
+        raise ValueError(f"{what}: the heads of a token must be contiguous")
+    return t.data_ptr(), n, t.stride(0) if n > 1 else h * d
+
+
+def rope_apply(rope, pos, q, k, q_out, k_out, stream=None):
+    """Rotates q [n, n_q_heads, head_dim] and k [n, n_kv_heads, head_dim] (bf16,
+    tokens any multiple of 8 elements apart) into the contiguous ``q_out`` and
+    ``k_out``, which may be q and k themselves.  ``pos``: int32 [n_axes, n], or
+    [n] for one axis, device.  Either side may be None with its output."""
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("an input and its output are given together")
+    if q is None and k is None:
+        raise ValueError("q or k must be given")
+    args, n = [], (q if q is not None else k).shape[0]
+    for t, o, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if t is None:
+            args.append((0, None, 0, None))
+            continue
+        ptr, rows, stride = _rows(t, None, rope.head_dim, what)
+        if rows != n or tuple(o.shape) != tuple(t.shape):
+            raise ValueError("q, k and their outputs must hold the same tokens")
+        args.append((t.shape[1], ptr, stride, _dev(o, "bfloat16", what + "_out")))
+    if tuple(pos.shape) != (rope.n_axes, n) and not (rope.n_axes == 1 and tuple(pos.shape) == (n,)):
+        raise ValueError("pos must be [n_axes, n]")
+    (hq, qp, qs, qo), (hk, kp, ks, ko) = args
+    _check(_lib.hwkv_rope_apply(rope.handle, n, hq, hk, _dev(pos, "int32", "pos"), qp, qs, kp, ks,
+                                qo, ko, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------
@@ -413,6 +513,30 @@ def append(cache, layer, k_new, v_new, stream=None):
         raise ValueError("k_new and v_new must be [batch, n_kv_heads, head_dim]")
     _check(_lib.hwkv_append(cache.handle, layer, _dev(k_new, "bfloat16", "k_new"),
                             _dev(v_new, "bfloat16", "v_new"), _stream(stream)))
+
+
+def append_rope(cache, layer, rope, pos, k_new, v_new, q=None, q_out=None, stream=None):
+    """``append`` with the new keys rotated on the way and the queries into
+    ``q_out``: k_new, v_new [batch, n_kv_heads, head_dim], q [batch, n_q_heads,
+    head_dim] (bf16, sequences any multiple of 8 elements apart), ``pos`` int32
+    [n_axes, batch] (or [batch] for one axis), ``q_out`` like q, contiguous."""
+    kp, nk, ks = _rows(k_new, cache.n_kv_heads, cache.head_dim, "k_new")
+    vp, nv, vs = _rows(v_new, cache.n_kv_heads, cache.head_dim, "v_new")
+    if nk != cache.batch or nv != cache.batch:
+        raise ValueError("k_new and v_new must be [batch, n_kv_heads, head_dim]")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out are given together")
+    qp, qs, qo = None, 0, None
+    if q is not None:
+        qp, nq, qs = _rows(q, cache.n_q_heads, cache.head_dim, "q")
+        if nq != cache.batch or tuple(q_out.shape) != tuple(q.shape):
+            raise ValueError("q and q_out must be [batch, n_q_heads, head_dim]")
+        qo = _dev(q_out, "bfloat16", "q_out")
+    if (tuple(pos.shape) != (rope.n_axes, cache.batch)
+            and not (rope.n_axes == 1 and tuple(pos.shape) == (cache.batch,))):
+        raise ValueError("pos must be [n_axes, batch]")
+    _check(_lib.hwkv_append_rope(cache.handle, layer, rope.handle, _dev(pos, "int32", "pos"), kp, ks,
+                                 vp, vs, qp, qs, qo, _stream(stream)))
 
 
 def decode_workspace_bytes(cache):
