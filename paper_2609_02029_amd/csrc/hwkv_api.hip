@@ -738,7 +738,11 @@ int64_t item_splits(const hwkv_cache *c, int32_t u, int32_t len, int64_t T) {
 // Plans the launch of sequences [b0, b0 + n), heads in `order` (by capacity),
 // with room for the partials of `parts` workgroups, and estimates its time.
 //
-// T is a quarter above an even share of the CUs (48 ragged sequences of
+// int8 (decode_i8, two to four workgroups per CU): T is an even share of two
+// workgroups per CU, and at least 8 tiles (the 48 sequences below 41 us; 0.5 / 0.75
+// / 1.5 shares 42.5 / 40.5 / 44.5; 16 sequences of 1,000 tokens, 8 KV heads, with at
+// least 2 / 4 / 8 tiles 19.8 / 15.6 / 15.1).
+// The others: T is a quarter above an even share of the CUs (48 ragged sequences of
 // 200-6,000 tokens, 8 KV heads: 84 us a layer with whole items, 78 / 77 at 1.0 /
 // 1.5 shares, 81 / 85 at 0.5 / 0.3), and at least one tile for each of 16 waves.
 //
@@ -767,6 +771,7 @@ void plan_item_launch(const hwkv_cache *c, int32_t layer, const int32_t *order, 
   const int64_t longest =
       std::max<int64_t>(1, tiles_for(std::min<int64_t>(L->len[0], c->cap[layer * H + order[0]])));
   int64_t T = std::max<int64_t>(16, total * 5 / (4 * cus) + 1);
+  if (c->fmt == HWKV_KV_I8) T = std::max<int64_t>(8, total / (2 * cus) + 1);
   if (longest <= T + T / 4) T = longest;
   int64_t runs = 0;
   for (int32_t h = 0; h < H; ++h) runs += item_splits(c, layer * H + h, L->len[0], T);
@@ -785,6 +790,7 @@ void plan_item_launch(const hwkv_cache *c, int32_t layer, const int32_t *order, 
     L->us = HUGE_VAL;
     return;
   }
+  if (c->fmt == HWKV_KV_I8) return;   // (decode_by_item asks the sizes alone)
   const bool fp8 = c->fmt == HWKV_KV_FP8_E4M3;
   const double dg = (double)(D * G), waves = hwkv::decode_item_waves((int)D, (int)G);
   const double start = fp8 ? 5.1 : 2.2, own = fp8 ? 1.2 * G + 0.0021 * dg : 1.3 * G + 0.0004 * dg;
@@ -823,13 +829,22 @@ double estimate_split(const hwkv_cache *c, const std::vector<int64_t> &tiles) {
 // to 1,024 items, alike, ragged over up to two powers of ten, or a few long ones
 // among many short.  Of 2,880 such calls all but 10 take at most 3 % longer
 // than split, those up to 7 %; on average 0.5 % more than the better side.
+// int8 caches, whose two sides run the same kernel, go by item where split takes
+// several launch pairs, or every item is so short that one workgroup has it done
+// before a merge: 16 sequences of 1,000 tokens, 8 KV heads, 128 x 4: 15.1 us against
+// 25.6, 64 of them 27 against 107, one of 300 8.2 against 9.2; but 8 of 1,000 13.1
+// against 12.7, one of 2,000 13.0 against 9.9, of 114,688 (256 x 6) 36 against 25.
 // bf16, 256 x 1, us a layer by item / split: 8 items of 2,048 slots 25.7 / 10.3, 128 of
 // 512 17.7 / 27.3, 512 of 512 52 / 110; 64 x 8, 16 sequences of 64-4,000, 8 KV heads:
 // 25.8 / 32.7.
 bool decode_by_item(const hwkv_cache *c, int32_t layer, const std::vector<int64_t> &tiles,
                     const int32_t *order, bool fused, int64_t parts,
                     ItemLaunch *launches) {
-  const double most = 0.95 * estimate_split(c, tiles);
+  double most = 0.95 * estimate_split(c, tiles);
+  if (c->fmt == HWKV_KV_I8) {
+    const bool short_items = *std::max_element(tiles.begin(), tiles.end()) <= 6;
+    most = tiles.size() > hwkv::kMaxItems || short_items ? 1.0 : 0.0;
+  }
   double us = 0.0;
   for (int32_t b0 = 0; b0 < c->batch && us < most; b0 += hwkv::kItemSeqs, ++launches) {
     plan_item_launch(c, layer, order, b0, std::min(hwkv::kItemSeqs, c->batch - b0), fused, parts,
@@ -896,6 +911,8 @@ int launch_items(hwkv_cache *c, int32_t layer, const int32_t *order,
       const int64_t at = (int64_t)L.b0 * c->cap_pad[u] * D;
       a.head[h].k_off = c->k_off[u] + at;
       a.head[h].v_off = c->v_off[u] + at;
+      if (c->fmt == HWKV_KV_I8)
+        a.head[h].s_off128 = (uint32_t)((c->s_off[u] + at / D * hwkv::kRowScaleBytes) / 128);
       a.head[h].page0 = page_tab_off(c, u, L.b0);
     }
     const size_t kv = (size_t)L.b0 * H * D, qo = kv * G;
@@ -912,7 +929,8 @@ int launch_items(hwkv_cache *c, int32_t layer, const int32_t *order,
     int rc = check_device(
         hwkv::launch_decode_item(c->fmt, (int)D, (int)G, a, s, ev[0], ev[1]), "decode item launch");
     if (rc == HWKV_OK && L.parts > 0)
-      rc = check_device(hwkv::launch_item_merge((int)D, (int)G, a, s, ev[2], ev[3]),
+      rc = check_device((c->fmt == HWKV_KV_I8 ? hwkv::launch_i8_merge : hwkv::launch_item_merge)(
+                            (int)D, (int)G, a, s, ev[2], ev[3]),
                         "decode item merge launch");
     if (rc != HWKV_OK) return rc;
   }
@@ -991,8 +1009,7 @@ int decode_impl(hwkv_cache *c, int32_t layer, const void *k_new,
   ItemLaunch one;                   // (a batch of one launch: nothing from the heap)
   std::vector<ItemLaunch> several(B > hwkv::kItemSeqs ? (B - 1) / hwkv::kItemSeqs + 1 : 0);
   ItemLaunch *const launches = several.empty() ? &one : several.data();
-  if (c->fmt != HWKV_KV_I8 &&
-      decode_by_item(c, layer, tiles, order, fused, total_splits, launches)) {
+  if (decode_by_item(c, layer, tiles, order, fused, total_splits, launches)) {
     const int rc = launch_items(c, layer, order, launches, k_new, v_new, q, scale, out,
                                 static_cast<float *>(ws), fused, s);
     if (rc != HWKV_OK) return rc;
@@ -2305,12 +2322,11 @@ int hwkv_append_rope(hwkv_cache *c, int32_t layer, const hwkv_rope *rope, const 
         hd.cap_pad = (int32_t)c->cap_pad[u];
         hd.window = (int32_t)c->window[u];
         hd.page0 = page_tab_off(c, u, b0);
-        if (c->fmt == HWKV_KV_I8) {
-          hd.s_off = c->s_off[u] + rows * hwkv::kRowScaleBytes;
-        } else {
+        hd.v_scale = c->v_scale[u];
+        if (c->fmt == HWKV_KV_I8)
+          hd.s_off128 = (uint32_t)((c->s_off[u] + rows * hwkv::kRowScaleBytes) / 128);
+        else
           hd.k_scale = c->k_scale[u];
-          hd.v_scale = c->v_scale[u];
-        }
       }
       for (int32_t i = 0; i < a.n_seqs; ++i) a.len[i] = (int32_t)seq_len(c, layer, b0 + i);
       a.pos = pos + b0;

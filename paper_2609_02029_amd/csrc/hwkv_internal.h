@@ -97,11 +97,10 @@ struct ItemHead {
   int32_t window;                // 0 = full
   int32_t page0;                 // page-table offset of sequence 0, or -1
   union {
-    struct {
-      float k_scale, v_scale;    // fp8 scales of the unit (else 1)
-    };
-    int64_t s_off;               // int8: scale pairs of the unit, sequence 0
+    float k_scale;               // fp8 scales of the unit (else 1)
+    uint32_t s_off128;           // int8: scale pairs of the unit, sequence 0, in 128 bytes
   };
+  float v_scale;
 };
 struct ItemArgs {
   ItemHead head[kMaxItems];
@@ -321,8 +320,12 @@ hipError_t launch_decode_split_fmt(int D, int G, const DecodeArgs &a,
                                    hipEvent_t e1);
 hipError_t launch_decode_i8(int D, int G, const DecodeArgs &a, int n_splits, hipStream_t s,
                             hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_decode_i8_item(int D, int G, const ItemArgs &a, hipStream_t s, hipEvent_t e0,
+                                 hipEvent_t e1);
 hipError_t launch_decode_item(int fmt, int D, int G, const ItemArgs &a, hipStream_t s,
                               hipEvent_t e0 = nullptr, hipEvent_t e1 = nullptr);
+hipError_t launch_i8_merge(int D, int G, const ItemArgs &a, hipStream_t s, hipEvent_t e0,
+                           hipEvent_t e1);
 hipError_t launch_item_merge(int D, int G, const ItemArgs &a, hipStream_t s,
                              hipEvent_t e0 = nullptr, hipEvent_t e1 = nullptr);
 template <int F>

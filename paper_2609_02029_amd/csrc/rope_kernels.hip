@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void append_rope(AppendRopeArgs a) {
     r = slot % kPageTokens;
   } else {
     at = (isk ? hd.k_off : hd.v_off) + (int64_t)b * hd.cap_pad * D;
-    if constexpr (F == HWKV_KV_I8) soff = hd.s_off + (int64_t)b * hd.cap_pad * kRowScaleBytes;
+    if constexpr (F == HWKV_KV_I8) soff = (int64_t)hd.s_off128 * 128 + (int64_t)b * hd.cap_pad * kRowScaleBytes;
   }
   uint8_t *const to = cache + (at + (isk ? (int64_t)(r / kTile) * kTile * D : (int64_t)r * D)) * EB;
   uint32_t e = 0;
