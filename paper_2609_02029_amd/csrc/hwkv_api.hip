@@ -614,8 +614,9 @@ int prefill_attn_impl(hwkv_cache *c, int32_t layer, int32_t seq, int64_t pos0,
   uint16_t *img = static_cast<uint16_t *>(ws);
   if (staged) {
     // the occupied rows of every unit (the keys below pos0), widened
-    hwkv::StageArgs sa;
-    std::memset(&sa, 0, sizeof sa);
+    hwkv::StageRowsArgs ra;
+    std::memset(&ra, 0, sizeof ra);
+    hwkv::StageArgs &sa = ra.units;
     int64_t max_chunks = 0;
     for (int32_t h = 0; h < H; ++h) {
       const int32_t u = layer * H + h;
@@ -636,10 +637,19 @@ int prefill_attn_impl(hwkv_cache *c, int32_t layer, int32_t seq, int64_t pos0,
     sa.image = img;
     sa.n_units = H;
     sa.max_chunks = (int32_t)max_chunks;
-    int rc;
-    if (max_chunks > 0 &&
-        (rc = check_device(hwkv::launch_stage_units(c->fmt, (int)D, sa, st), "stage launch")) != HWKV_OK)
-      return rc;
+    hipError_t e = hipSuccess;
+    if (c->fmt == HWKV_KV_I8) {      // and the chunk's rows, below, in one launch
+      ra.k = static_cast<const uint16_t *>(k);
+      ra.v = static_cast<const uint16_t *>(v);
+      ra.k_out = img + SL.k_in;
+      ra.v_out = img + SL.v_in;
+      ra.n_chunks = n_tokens * H * (D / 8);
+      e = hwkv::launch_stage_rows((int)D, ra, st);
+    } else if (max_chunks > 0) {
+      e = hwkv::launch_stage_units((int)D, sa, st);
+    }
+    const int rc = check_device(e, "stage launch");
+    if (rc != HWKV_OK) return rc;
     a.cache = img;
   } else {
     a.cache = reinterpret_cast<const uint16_t *>(c->base);
@@ -648,21 +658,23 @@ int prefill_attn_impl(hwkv_cache *c, int32_t layer, int32_t seq, int64_t pos0,
   }
   if (chunk_staged) {
     // the chunk's own keys and values as the cache will store them
-    hwkv::StageChunkArgs ca;
-    std::memset(&ca, 0, sizeof ca);
-    ca.fmt = c->fmt;
-    ca.k = static_cast<const uint16_t *>(k);
-    ca.v = static_cast<const uint16_t *>(v);
-    ca.k_out = img + SL.k_in;
-    ca.v_out = img + SL.v_in;
-    for (int32_t h = 0; h < H; ++h) {
-      ca.k_scale[h] = c->k_scale[layer * H + h];
-      ca.v_scale[h] = c->v_scale[layer * H + h];
+    if (c->fmt != HWKV_KV_I8) {
+      hwkv::StageChunkArgs ca;
+      std::memset(&ca, 0, sizeof ca);
+      ca.fmt = c->fmt;
+      ca.k = static_cast<const uint16_t *>(k);
+      ca.v = static_cast<const uint16_t *>(v);
+      ca.k_out = img + SL.k_in;
+      ca.v_out = img + SL.v_in;
+      for (int32_t h = 0; h < H; ++h) {
+        ca.k_scale[h] = c->k_scale[layer * H + h];
+        ca.v_scale[h] = c->v_scale[layer * H + h];
+      }
+      ca.n_chunks = n_tokens * H * (D / 8);
+      ca.n_kv_heads = H;
+      const int rc = check_device(hwkv::launch_stage_chunk((int)D, ca, st), "stage launch");
+      if (rc != HWKV_OK) return rc;
     }
-    ca.n_chunks = n_tokens * H * (D / 8);
-    ca.n_kv_heads = H;
-    const int rc = check_device(hwkv::launch_stage_chunk((int)D, ca, st), "stage launch");
-    if (rc != HWKV_OK) return rc;
     a.k = img + SL.k_in;
     a.v = img + SL.v_in;
   } else {
@@ -1749,20 +1761,33 @@ int hwkv_calib_replay_format(int32_t n_kv_heads, int32_t n_q_heads, int32_t head
     base = (base + 255) / 256 * 256;
     uint16_t *kst = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(ws) + base);
     uint16_t *vst = kst + (size_t)n_hist * n_kv_heads * head_dim;
-    hwkv::StageChunkArgs ca;
-    std::memset(&ca, 0, sizeof ca);
-    ca.fmt = kv_format;
-    ca.k = static_cast<const uint16_t *>(k);
-    ca.v = static_cast<const uint16_t *>(v);
-    ca.k_out = kst;
-    ca.v_out = vst;
-    for (int32_t h = 0; h < n_kv_heads; ++h) {
-      ca.k_scale[h] = ks[h];
-      ca.v_scale[h] = vs[h];
+    hipError_t e;
+    if (kv_format == HWKV_KV_I8) {
+      hwkv::StageRowsArgs sr;
+      std::memset(&sr, 0, sizeof sr);
+      sr.k = static_cast<const uint16_t *>(k);
+      sr.v = static_cast<const uint16_t *>(v);
+      sr.k_out = kst;
+      sr.v_out = vst;
+      sr.n_chunks = n_hist * n_kv_heads * (head_dim / 8);
+      e = hwkv::launch_stage_rows(head_dim, sr, st);
+    } else {
+      hwkv::StageChunkArgs ca;
+      std::memset(&ca, 0, sizeof ca);
+      ca.fmt = kv_format;
+      ca.k = static_cast<const uint16_t *>(k);
+      ca.v = static_cast<const uint16_t *>(v);
+      ca.k_out = kst;
+      ca.v_out = vst;
+      for (int32_t h = 0; h < n_kv_heads; ++h) {
+        ca.k_scale[h] = ks[h];
+        ca.v_scale[h] = vs[h];
+      }
+      ca.n_chunks = n_hist * n_kv_heads * (head_dim / 8);
+      ca.n_kv_heads = n_kv_heads;
+      e = hwkv::launch_stage_chunk(head_dim, ca, st);
     }
-    ca.n_chunks = n_hist * n_kv_heads * (head_dim / 8);
-    ca.n_kv_heads = n_kv_heads;
-    rc = check_device(hwkv::launch_stage_chunk(head_dim, ca, st), "stage launch");
+    rc = check_device(e, "stage launch");
     if (rc != HWKV_OK) return rc;
     k_src = kst;
     v_src = vst;
@@ -2253,7 +2278,6 @@ int hwkv_rope_apply(const hwkv_rope *rope, int64_t n_tokens, int32_t n_q_heads,
   a.k_stride = k_stride;
   a.n_q = n_q_heads;
   a.n_k = n_kv_heads;
-  a.heads_per = 4;
   rc = check_device(hwkv::launch_rope((int)D, a, (hipStream_t)stream), "rope launch");
   return rc == HWKV_OK ? ok() : rc;
 }

@@ -195,15 +195,16 @@ struct RopeTable {
   float magnitude;
 };
 
-// Rotation of n tokens' q and k heads: grid x over (token, 16 channels of a
-// head), grid y over the heads in groups of heads_per.
+// Rotation of n tokens' q and k heads: grid x over the tokens in groups of
+// tokens_per, grid y over the heads in groups of heads_per (both set at launch).
+constexpr int kRopeTokens = 8;
 struct RopeArgs {
   RopeTable rope;
   const int32_t *pos;            // [n_axes][n]
   const uint16_t *q, *k;         // rows of n_q, n_k heads, q_stride / k_stride apart
   uint16_t *q_out, *k_out;       // [n][heads][D]
   int64_t n, q_stride, k_stride; // strides in elements
-  int32_t n_q, n_k, heads_per;
+  int32_t n_q, n_k, tokens_per, heads_per;
 };
 hipError_t launch_rope(int D, const RopeArgs &a, hipStream_t s);
 
@@ -342,10 +343,9 @@ hipError_t launch_prefill_write(int fmt, int D, const WriteArgs &a,
 hipError_t launch_append(int fmt, int D, const AppendArgs &a, hipStream_t s);
 hipError_t launch_page_update(const PageUpdateArgs &a, hipStream_t s);
 
-// Staging of an fp8 or int8 cache for prefill attention: rows [0, n_rows) of
-// one (unit, sequence) widened to bf16 -- fp8 code values, int8 values -- in
-// the bf16 cache layout, and a chunk's K or V quantised as the cache stores it
-// and widened.
+// Staging of an fp8 or int8 cache for prefill attention: rows [0, n_rows) of one
+// (unit, sequence) widened to bf16 -- fp8 code values, int8 values -- in the bf16
+// cache layout, and a chunk's K or V quantised as the cache stores it and widened.
 struct StageUnit {
   int64_t src_k_off, src_v_off;  // element offsets (unpaged units)
   int64_t src_s_off;             // int8: scale pairs (unpaged units)
@@ -362,18 +362,27 @@ struct StageArgs {
   int32_t n_units;
   int32_t max_chunks;            // max over units of n_rows * D / 8 (per K or V)
 };
-hipError_t launch_stage_units(int fmt, int D, const StageArgs &a, hipStream_t s);
+hipError_t launch_stage_units(int D, const StageArgs &a, hipStream_t s);
 struct StageChunkArgs {
-  int32_t fmt;                   // HWKV_KV_FP8_E4M3, HWKV_KV_I8 or HWKV_KV_F16
+  int32_t fmt;                   // HWKV_KV_FP8_E4M3 or HWKV_KV_F16
   const uint16_t *k, *v;         // [n_tokens][Hkv][D] bf16 inputs
   uint16_t *k_out, *v_out;       // the same layout: the stored values, as bf16
-                                 // code values (fp8), bf16 (i8) or binary16 (f16)
+                                 // code values (fp8) or binary16 (f16)
   float k_scale[kMaxItems];      // per kv head of the layer
   float v_scale[kMaxItems];
   int64_t n_chunks;              // n_tokens * Hkv * D / 8
   int32_t n_kv_heads;
 };
 hipError_t launch_stage_chunk(int D, const StageChunkArgs &a, hipStream_t s);
+// Both for int8 caches, in one launch: a chunk of prefill attention, or a trace
+// (no units).
+struct StageRowsArgs {
+  StageArgs units;
+  const uint16_t *k, *v;         // as in StageChunkArgs
+  uint16_t *k_out, *v_out;
+  int64_t n_chunks;
+};
+hipError_t launch_stage_rows(int D, const StageRowsArgs &a, hipStream_t s);
 int prefill_attn_columns_per_block();   // (token, q head) columns
 // f16: the cache, k and v hold binary16 values (else bf16); q is bf16.
 hipError_t launch_prefill_attn(int D, bool f16, const PrefillAttnArgs &a, hipStream_t s);
@@ -454,6 +463,7 @@ static_assert(sizeof(hwkv::AppendRopeArgs) <= 4096, "append rope kernarg too lar
 static_assert(sizeof(hwkv::PageUpdateArgs) <= 4096, "page update kernarg too large");
 static_assert(sizeof(hwkv::StageArgs) <= 4096, "stage kernarg too large");
 static_assert(sizeof(hwkv::StageChunkArgs) <= 4096, "stage chunk kernarg too large");
+static_assert(sizeof(hwkv::StageRowsArgs) <= 4096, "stage rows kernarg too large");
 static_assert(sizeof(hwkv::PrefillAttnArgs) <= 4096, "prefill kernarg too large");
 static_assert(sizeof(hwkv::ReplayAttnArgs) <= 4096, "replay kernarg too large");
 static_assert(sizeof(hwkv::ReplayMergeArgs) <= 4096, "replay merge kernarg too large");

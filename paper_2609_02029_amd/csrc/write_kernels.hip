@@ -188,13 +188,12 @@ __device__ __forceinline__ uint4 widen_fp8x8(uint2 c) {
   return make_uint4(w(c.x, false), w(c.x, true), w(c.y, false), w(c.y, true));
 }
 
-// Staging of an fp8 or int8 cache for prefill attention: the occupied rows of
-// each (unit, sequence) of a layer widened to bf16 (fp8 code values; int8
-// values, with their row's scale), in the layout of a bf16 cache (K tiles chunk
-// for chunk, V rows), into an image the bf16 kernel reads.  blockIdx.y: the
-// unit; blockIdx.z: 0 = K, 1 = V.  Whole K tiles are staged (rows past the
-// occupied ones are never read).
-template <int D, int F>
+// Staging of an fp8 cache for prefill attention: the occupied rows of each
+// (unit, sequence) of a layer widened to bf16 code values, in the layout of
+// a bf16 cache (K tiles chunk for chunk, V rows), into an image the bf16
+// kernel reads.  blockIdx.y: the unit; blockIdx.z: 0 = K, 1 = V.  Whole K
+// tiles are staged (rows past the occupied ones are never read).
+template <int D>
 __global__ __launch_bounds__(256) void stage_units(StageArgs a) {
   constexpr int NC = D / 8;
   constexpr int TPP = kPageTokens / kTile;
@@ -204,37 +203,27 @@ __global__ __launch_bounds__(256) void stage_units(StageArgs a) {
                         : (int64_t)((su.n_rows + kTile - 1) / kTile) * kTile * NC;
   for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n;
        c += (int64_t)gridDim.x * 256) {
-    // K chunk c: position r of tile t; V chunk c: chunk g of row j
-    const int64_t row = isv ? c / NC : c / (kTile * NC) * kTile + c % kTile;
-    int64_t src, sc = 0;        // the codes, and the row's scale byte (int8)
+    int64_t src;
     if (su.pto < 0) {
       src = (isv ? su.src_v_off : su.src_k_off) + c * 8;
-      sc = su.src_s_off + row * kRowScaleBytes + (isv ? 1 : 0);
-    } else if (!isv) {
+    } else if (!isv) {          // K chunk c: tile t, position r in the tile
       const int64_t t = c / (kTile * NC), r = c % (kTile * NC);
       const int64_t pg = a.page_table[su.pto + t / TPP];
-      src = a.pool_off + pg * page_elems<F>(D) + (t % TPP) * kTile * D + r * 8;
-      sc = a.pool_off + pg * page_elems<F>(D) + 2 * kPageTokens * D + row % kPageTokens * kRowScaleBytes;
-    } else {
+      src = a.pool_off + pg * 2 * kPageTokens * D + (t % TPP) * kTile * D + r * 8;
+    } else {                    // V chunk c: row j, chunk g
       const int64_t j = c / NC, g = c % NC;
       const int64_t pg = a.page_table[su.pto + j / kPageTokens];
-      src = a.pool_off + pg * page_elems<F>(D) + (int64_t)kPageTokens * D +
+      src = a.pool_off + pg * 2 * kPageTokens * D + (int64_t)kPageTokens * D +
             (j % kPageTokens) * D + g * 8;
-      sc = a.pool_off + pg * page_elems<F>(D) + 2 * kPageTokens * D + row % kPageTokens * kRowScaleBytes + 1;
     }
     const uint2 codes = *reinterpret_cast<const uint2 *>(a.cache + src);
-    uint4 *const to = reinterpret_cast<uint4 *>(a.image + (isv ? su.dst_v_off : su.dst_k_off) + c * 8);
-    if constexpr (F == HWKV_KV_I8)
-      *to = widen8_row(codes, a.cache[sc]);
-    else
-      *to = widen_fp8x8(codes);
+    *reinterpret_cast<uint4 *>(a.image + (isv ? su.dst_v_off : su.dst_k_off) + c * 8) =
+        widen_fp8x8(codes);
   }
 }
 
 // The chunk's own K and V as the cache will store them: fp8 codes (code(x /
-// s) of the unit's scale) widened to bf16 code values, int8 codes widened to
-// their values, or binary16 values.  (The NC chunks of a row are NC lanes of one
-// wavefront, and in or out of range together.)
+// s) of the unit's scale) widened to bf16 code values, or binary16 values.
 template <int D, int F>
 __global__ __launch_bounds__(256) void stage_chunk(StageChunkArgs a) {
   constexpr int NC = D / 8;
@@ -246,17 +235,58 @@ __global__ __launch_bounds__(256) void stage_chunk(StageChunkArgs a) {
     if constexpr (F == HWKV_KV_F16) {
       *reinterpret_cast<uint4 *>(a.k_out + c * 8) = encode8<HWKV_KV_F16>(k, 1.0f);
       *reinterpret_cast<uint4 *>(a.v_out + c * 8) = encode8<HWKV_KV_F16>(v, 1.0f);
-    } else if constexpr (F == HWKV_KV_I8) {
-      const uint32_t ke = row_scale(group_max<NC>(top8(k)));
-      const uint32_t ve = row_scale(group_max<NC>(top8(v)));
-      *reinterpret_cast<uint4 *>(a.k_out + c * 8) = widen8_row(encode8_row(k, ke), ke);
-      *reinterpret_cast<uint4 *>(a.v_out + c * 8) = widen8_row(encode8_row(v, ve), ve);
     } else {
       *reinterpret_cast<uint4 *>(a.k_out + c * 8) =
           widen_fp8x8(encode8<HWKV_KV_FP8_E4M3>(k, a.k_scale[h]));
       *reinterpret_cast<uint4 *>(a.v_out + c * 8) =
           widen_fp8x8(encode8<HWKV_KV_FP8_E4M3>(v, a.v_scale[h]));
     }
+  }
+}
+
+// The same for int8 caches, values instead of code values, and with the chunk's
+// own rows in the launch: blockIdx.z: 0 = the units' K, 1 = their V, 2 = the chunk
+// (blockIdx.y 0 only).  (The NC chunks of a chunk's row are NC lanes of one
+// wavefront, and in or out of range together.)
+template <int D>
+__global__ __launch_bounds__(256) void stage_rows(StageRowsArgs a) {
+  constexpr int NC = D / 8;
+  constexpr int TPP = kPageTokens / kTile;
+  constexpr int64_t PAGE = page_elems<HWKV_KV_I8>(D);
+  const int64_t c0 = (int64_t)blockIdx.x * 256 + threadIdx.x, cs = (int64_t)gridDim.x * 256;
+  if (blockIdx.z == 2) {
+    if (blockIdx.y > 0) return;
+    for (int64_t c = c0; c < a.n_chunks; c += cs) {
+      const uint4 k = *reinterpret_cast<const uint4 *>(a.k + c * 8);
+      const uint4 v = *reinterpret_cast<const uint4 *>(a.v + c * 8);
+      const uint32_t ke = row_scale(group_max<NC>(top8(k)));
+      const uint32_t ve = row_scale(group_max<NC>(top8(v)));
+      *reinterpret_cast<uint4 *>(a.k_out + c * 8) = widen8_row(encode8_row(k, ke), ke);
+      *reinterpret_cast<uint4 *>(a.v_out + c * 8) = widen8_row(encode8_row(v, ve), ve);
+    }
+    return;
+  }
+  const StageUnit &su = a.units.unit[blockIdx.y];
+  const bool isv = blockIdx.z != 0;
+  const uint8_t *const cache = a.units.cache;
+  const int64_t n = isv ? (int64_t)su.n_rows * NC
+                        : (int64_t)((su.n_rows + kTile - 1) / kTile) * kTile * NC;
+  for (int64_t c = c0; c < n; c += cs) {
+    // K chunk c: position r of tile t; V chunk c: chunk g of row j
+    const int64_t row = isv ? c / NC : c / (kTile * NC) * kTile + c % kTile;
+    const uint8_t *codes, *pairs;
+    if (su.pto < 0) {
+      codes = cache + (isv ? su.src_v_off : su.src_k_off) + c * 8;
+      pairs = cache + su.src_s_off + row * kRowScaleBytes;
+    } else {
+      const int64_t pg = a.units.page_table[su.pto + row / kPageTokens];
+      const uint8_t *const page = cache + a.units.pool_off + pg * PAGE;
+      codes = isv ? page + kPageTokens * D + (row % kPageTokens) * D + c % NC * 8
+                  : page + (c / (kTile * NC)) % TPP * kTile * D + c % (kTile * NC) * 8;
+      pairs = page + 2 * kPageTokens * D + row % kPageTokens * kRowScaleBytes;
+    }
+    *reinterpret_cast<uint4 *>(a.units.image + (isv ? su.dst_v_off : su.dst_k_off) + c * 8) =
+        widen8_row(*reinterpret_cast<const uint2 *>(codes), pairs[isv]);
   }
 }
 
@@ -308,42 +338,48 @@ hipError_t launch_append(int fmt, int D, const AppendArgs &a, hipStream_t s) {
   return dispatch_df<AppendLaunch>(fmt, D, a, s);
 }
 
-hipError_t launch_stage_units(int fmt, int D, const StageArgs &a, hipStream_t s) {
+hipError_t launch_stage_units(int D, const StageArgs &a, hipStream_t s) {
   const int64_t per = 256;
   const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((a.max_chunks + per - 1) / per, 2048)),
                   (unsigned)a.n_units, 2);
-#define HWKV_SU(DD)                                                                    \
-  if (fmt == HWKV_KV_I8)                                                               \
-    hipLaunchKernelGGL((stage_units<DD, HWKV_KV_I8>), grid, dim3(256), 0, s, a);       \
-  else if (fmt == HWKV_KV_FP8_E4M3)                                                    \
-    hipLaunchKernelGGL((stage_units<DD, HWKV_KV_FP8_E4M3>), grid, dim3(256), 0, s, a); \
-  else                                                                                 \
-    return hipErrorInvalidValue
   switch (D) {
-    case 64: HWKV_SU(64); break;
-    case 128: HWKV_SU(128); break;
-    case 256: HWKV_SU(256); break;
+    case 64: hipLaunchKernelGGL(stage_units<64>, grid, dim3(256), 0, s, a); break;
+    case 128: hipLaunchKernelGGL(stage_units<128>, grid, dim3(256), 0, s, a); break;
+    case 256: hipLaunchKernelGGL(stage_units<256>, grid, dim3(256), 0, s, a); break;
     default: return hipErrorInvalidValue;
   }
-#undef HWKV_SU
   return hipGetLastError();
 }
 
-template <int D, int F>
-struct StageChunkLaunch {
-  static hipError_t run(const StageChunkArgs &a, dim3 grid, hipStream_t s) {
-    if constexpr (F == HWKV_KV_BF16) {
-      return hipErrorInvalidValue;
-    } else {
-      hipLaunchKernelGGL((stage_chunk<D, F>), grid, dim3(256), 0, s, a);
-      return hipGetLastError();
-    }
-  }
-};
-
 hipError_t launch_stage_chunk(int D, const StageChunkArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((a.n_chunks + 255) / 256, 4096)));
-  return dispatch_df<StageChunkLaunch>(a.fmt, D, a, grid, s);
+  if (a.fmt != HWKV_KV_F16 && a.fmt != HWKV_KV_FP8_E4M3) return hipErrorInvalidValue;
+#define HWKV_SC(DD)                                                                   \
+  if (a.fmt == HWKV_KV_F16)                                                           \
+    hipLaunchKernelGGL((stage_chunk<DD, HWKV_KV_F16>), grid, dim3(256), 0, s, a);     \
+  else                                                                                \
+    hipLaunchKernelGGL((stage_chunk<DD, HWKV_KV_FP8_E4M3>), grid, dim3(256), 0, s, a)
+  switch (D) {
+    case 64: HWKV_SC(64); break;
+    case 128: HWKV_SC(128); break;
+    case 256: HWKV_SC(256); break;
+    default: return hipErrorInvalidValue;
+  }
+#undef HWKV_SC
+  return hipGetLastError();
+}
+
+hipError_t launch_stage_rows(int D, const StageRowsArgs &a, hipStream_t s) {
+  const int64_t most = std::max<int64_t>(a.units.max_chunks, a.n_chunks);
+  const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((most + 255) / 256, 2048)),
+                  (unsigned)std::max(1, a.units.n_units), 3);
+  switch (D) {
+    case 64: hipLaunchKernelGGL(stage_rows<64>, grid, dim3(256), 0, s, a); break;
+    case 128: hipLaunchKernelGGL(stage_rows<128>, grid, dim3(256), 0, s, a); break;
+    case 256: hipLaunchKernelGGL(stage_rows<256>, grid, dim3(256), 0, s, a); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_page_update(const PageUpdateArgs &a, hipStream_t s) {
