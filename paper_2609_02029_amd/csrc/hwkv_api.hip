@@ -1029,6 +1029,19 @@ int decode_impl(hwkv_cache *c, int32_t layer, const void *k_new,
       for (int32_t b = 0; b < B; ++b) seq_len(c, layer, b) += 1;
     return ok();
   }
+  // int8 from head_dim 128 on splits into one workgroup per CU: its rings keep as
+  // much in flight as HBM takes (66 KB at 256), and half the partials are written
+  // and merged.  us a call with one / two: 256 x 6 at 112K 23.7 / 25.6, 32K tokens of
+  // 4 heads 20.6 / 22.0; 128 x 4, 8 heads, 8,000 tokens 11.4 / 12.2, 120,000 46.4 /
+  // 46.9, 32,000 19.6 / 19.0; but 64 x 8 at 50,000 20.1 / 17.6.
+  if (c->fmt == HWKV_KV_I8 && p.head_dim >= 128) {
+    total_splits = 0;
+    for (int i0 = 0; i0 < n_items_total; i0 += hwkv::kMaxItems) {
+      const int cnt = std::min(hwkv::kMaxItems, n_items_total - i0);
+      plan_workgroups(&tiles[i0], cnt, std::max<int64_t>(1, target / 2), &nwg[i0]);
+      for (int j = 0; j < cnt; ++j) total_splits += nwg[i0 + j];
+    }
+  }
   // launches of at most kMaxItems items
   int ws_split = 0;
   for (int i0 = 0; i0 < n_items_total; i0 += hwkv::kMaxItems) {
