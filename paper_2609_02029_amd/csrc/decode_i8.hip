@@ -100,7 +100,8 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
   constexpr int VB = D / 16;           // 16-channel blocks of the output
   constexpr int KB = 16 * D;           // a wave's part of a tile: K slice, V rows,
   constexpr int SB = 2 * KB + 256;     //   scale pairs
-  constexpr int WB = 2 * SB > G * D * 4 ? 2 * SB : G * D * 4;   // of two; its acc in the epilogue
+  constexpr int WB = 2 * SB;           //   of two tiles; its acc in the epilogue
+  static_assert(WB >= 16 * D * 4, "16 acc rows");
   constexpr int HC = G <= 4 ? 4 : 8;   // columns, and rows of a term
   __shared__ __attribute__((aligned(1024))) uint8_t area[kWaves * WB];
   __shared__ __attribute__((aligned(16))) uint8_t digits[3 * G * D];
@@ -439,22 +440,14 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
     sml[wave][0][lane] = m;
     sml[wave][1][lane] = lt;
   }
+  // (all 16 rows, a head's terms among them: the merge adds them as it reads)
   float *const accw = reinterpret_cast<float *>(area + wave * WB);
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int h = 4 * g4 + r;
+  for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int n = 0; n < KM; ++n) {
-      f32x4_t x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = o[4 * n + e][r];
-        if constexpr (HC == 4) x[e] += __shfl_xor(x[e], 16);
-        x[e] += __shfl_xor(x[e], 32);
-      }
-      if (h < G) *reinterpret_cast<f32x4_t *>(accw + h * D + 64 * n + 4 * l16) = x;
-    }
-  }
+    for (int n = 0; n < KM; ++n)
+      *reinterpret_cast<f32x4_t *>(accw + (4 * g4 + r) * D + 64 * n + 4 * l16) =
+          f32x4_t{o[4 * n][r], o[4 * n + 1][r], o[4 * n + 2][r], o[4 * n + 3][r]};
   __syncthreads();
 
   for (int idx = threadIdx.x; idx < G * D / 4; idx += kWaves * 64) {
@@ -467,8 +460,11 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float f = exp2f(sml[w][0][h] - M);
-      const f32x4_t x = *reinterpret_cast<const f32x4_t *>(area + w * WB + ((size_t)h * D + c) * 4);
       L += sml[w][1][h] * f;
+      f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < (HC == 4 ? 3 : 2); ++t)
+        x += *reinterpret_cast<const f32x4_t *>(area + w * WB + ((t * HC + h) * D + c) * 4);
       A += x * f;
     }
     const float back = 0x1p18f;        // 2^24 of the weights, 2^-6 of the codes
