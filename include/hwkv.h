@@ -450,7 +450,8 @@ int hwkv_decode_workspace_bytes(const hwkv_cache *cache, size_t *bytes);
  * bits and a sign under a power-of-two scaling per query head (exact for every
  * component within a factor 2^14 of the head's largest |q|, the others to 2^-22 of
  * that; the products and their sums are exact), and the weights the value product as
- * three bf16 terms that carry each weight to 2^-27 of itself; for binary16, q enters q.k as binary16 after a power-of-two scaling
+ * three bf16 terms that carry each weight to 2^-27 of itself (with value rows of
+ * magnitude 2^-98 to 2^108); for binary16, q enters q.k as binary16 after a power-of-two scaling
  * per query head, exact for every component within a factor 2^31 of the
  * head's largest |q| (the products are exact, the sums fp32). */
 int hwkv_decode_attn(hwkv_cache *cache, int32_t layer, const void *q,

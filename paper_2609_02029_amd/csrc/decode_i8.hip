@@ -17,7 +17,7 @@
 //          mod 4 up to 4 heads), and half of them take the second tile's logits:
 //          lane (g, c) has slots 4g .. 4g + 3 of one head and one tile.
 //   p.c    v_mfma_f32_16x16x32_bf16 over both tiles' slots: A = the weights
-//          p_s 2^(eV_s - 151) as three bf16 terms, each the rounded rest of those
+//          p_s 2^(eV_s - 139) as three bf16 terms, each the rounded rest of those
 //          before it (2^-27 of a weight is left behind; two terms leave 2^-18 and
 //          cost 2.5e-6 of the output, ten times what fp32 does).  The terms of a head
 //          are rows of their own, whose other tile's half comes from the lane that
@@ -105,7 +105,7 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
   constexpr int HC = G <= 4 ? 4 : 8;   // columns, and rows of a term
   __shared__ __attribute__((aligned(1024))) uint8_t area[kWaves * WB];
   __shared__ __attribute__((aligned(16))) uint8_t digits[3 * G * D];
-  __shared__ float zs_s[G];
+  __shared__ f32x2_t zs_s[G];
   __shared__ float sml[kWaves][2][8];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -236,7 +236,6 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
     for (int n = 0; n < KB / 1024; ++n) stage_lds<false>(vr, to + KB + n * 1024, vl[n], 0);
     stage_lds<true>(sr, to + 2 * KB, sl, 0);
   };
-
   const bool writes_new =
       __builtin_amdgcn_readfirstlane((int)(new_slot >= 0 && (ITEM || first == 0))) != 0;
   if (writes_new && wave == 0) {
@@ -252,8 +251,7 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
     }
   }
   // q: 8 channels a thread, as digits in the order the products read them; a
-  // head is scaled by the power of two that puts its largest |q| in [2^21, 2^22),
-  // less where the logit scale that takes it back would leave fp32's range
+  // head is scaled by the power of two that puts its largest |q| in [2^21, 2^22)
   const bool has_q = threadIdx.x < G * NC;
   uint4 q8 = make_uint4(0u, 0u, 0u, 0u);
   if (has_q) q8 = *reinterpret_cast<const uint4 *>(a.q + q_row * D + threadIdx.x * 8);
@@ -263,9 +261,7 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
   }
   {
     const uint32_t top = group_max<NC>(top8(q8));
-    int ez;
-    (void)frexpf(a.scale_log2, &ez);
-    const int sh = top ? min(148 - (int)max(top >> 7, 1u), ez + 110) : 0;
+    const int sh = 148 - (int)max(top >> 7, 1u);
     const uint32_t w[4] = {q8.x, q8.y, q8.z, q8.w};
     uint32_t d[3][2] = {};
 #pragma unroll
@@ -284,9 +280,15 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
 #pragma unroll
       for (int t = 0; t < 3; ++t)
         *reinterpret_cast<uint2 *>(digits + t * G * D + at) = make_uint2(d[t][0], d[t][1]);
-      // (2^-6: codes count 2^(e - 133), the bits of 2^(e - 127) are e << 23; a
-      // head that is not finite has NaN for its logits)
-      if (c == 0) zs_s[h] = top >= 0x7f80u ? __builtin_nanf("") : ldexpf(a.scale_log2, -6 - sh);
+      // What takes this back, and 2^-6 (codes count 2^(e - 133), the bits of 2^(e -
+      // 127) are e << 23), in two factors around the row's own, so that no step
+      // leaves fp32's range where q.k does not.  A head that is not finite has NaN
+      // for its logits.
+      if (c == 0) {
+        const int back = -6 - sh, near = min(max(back, -60), 60);
+        zs_s[h] = f32x2_t{ldexpf(1.0f, near),
+                          top >= 0x7f80u ? __builtin_nanf("") : ldexpf(a.scale_log2, back - near)};
+      }
     }
   }
   // only this workgroup reads the new slot in this launch (see decode_split)
@@ -307,7 +309,7 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
       qd[t][m] = *reinterpret_cast<const i32x4_t *>(digits + t * G * D + (hc < G ? hc : 0) * D + m * 64 + g4 * 16);
       if (hc >= G) qd[t][m] = i32x4_t{0, 0, 0, 0};
     }
-  const float zs = hc < G ? zs_s[hc] : 0.f;
+  const f32x2_t zs = hc < G ? zs_s[hc] : f32x2_t{0.f, 0.f};
 
   // the lane's head: running shift m (base 2, lazily raised: the weights stay
   // below 2^8) and the sum of its slots' weights
@@ -370,7 +372,7 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
     for (int i = 0; i < 4; ++i) {
       const uint32_t pr = (i < 2 ? pairs.x : pairs.y) >> (16 * (i & 1));
       const bool valid = slot0 + i < nv;
-      z[i] = valid ? sum[i] * __uint_as_float((pr & 255u) << 23) * zs : -INFINITY;
+      z[i] = valid ? sum[i] * zs.x * __uint_as_float((pr & 255u) << 23) * zs.y : -INFINITY;
       vs[i] = valid ? __uint_as_float((pr << 15) & 0x7f800000u) : 0.f;
     }
     float mx = max_of_rows(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])));
@@ -388,13 +390,14 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
         for (int vb = 0; vb < VB; ++vb) o[vb][r] *= al;
       }
     }
-    // 2^-24 keeps the weights of the largest rows in range
+    // 2^-12 centres the range: value rows from 2^-98 (below, the third term and then
+    // the second are lost) to 2^108 (above, long sums overflow)
     float w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float p = exp2f(z[i] - m);
       lsum += p;
-      w[i] = p * 0x1p-24f * vs[i];
+      w[i] = p * 0x1p-12f * vs[i];
     }
     u32x2_t t[4];
     t[0] = u32x2_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])};
@@ -467,7 +470,7 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
         x += *reinterpret_cast<const f32x4_t *>(area + w * WB + ((t * HC + h) * D + c) * 4);
       A += x * f;
     }
-    const float back = 0x1p18f;        // 2^24 of the weights, 2^-6 of the codes
+    const float back = 0x1p6f;         // 2^12 of the weights, 2^-6 of the codes
     if (whole) {
       __builtin_nontemporal_store(A * (back / L),
                                   reinterpret_cast<f32x4_t *>(&a.out[(q_row + h) * D + c]));

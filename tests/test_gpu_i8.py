@@ -265,6 +265,94 @@ def test_decode_large_and_small_queries():
     cache.free()
 
 
+def test_decode_keys_of_any_magnitude():
+    """Keys near the ends of the range, under a scale that makes the logits
+    ordinary; values of 2^-100 and 2^100."""
+    D, n = 64, 300
+    r = np.random.default_rng(8)
+    bits = lambda x: (np.ascontiguousarray(x, dtype=np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    for km, vm, qm in ((2.0 ** 110, 2.0 ** 100, 2.0 ** -50), (2.0 ** -110, 2.0 ** -100, 2.0 ** 50), (1.0, 2.0 ** 115, 1.0)):
+        k, v, q = bits(r.normal(size=(n, D)) * km), bits(r.normal(size=(n, D)) * vm), bits(r.normal(size=(2, D)) * qm)
+        cache, ws = _one_unit(k, v, D)
+        scale = float(np.float32(0.125 / (km * qm)))
+        got, ref = _decode(cache, ws, q, scale) / vm, _reference(q, k, v, scale) / vm
+        # as test_decode_large_and_small_queries: logits to 1e-5, weights to 2^-16
+        assert np.abs(got - ref).max() <= (2e-5 + 2.0 ** -16 + 2e-5) * 4.0 and np.abs(ref).max() > 1e-2
+        cache.free()
+
+
+def test_decode_one_long_sequence_among_many_short():
+    """More items than a split launch takes, one of them of hundreds of tiles:
+    its splits meet in the merge, the others stay whole."""
+    c = mini(batch=24, head_dim=128, n_q_heads=16, n_kv_heads=4, levels=[[0, 1, 1, 0]], level_windows=[3000, 0],
+             prompt=[37 + 11 * i for i in range(23)] + [20001], max_ctx=20100)
+    r = Run8(c)
+    for b in range(24):
+        r.prefill(0, b)
+    for st in range(2):
+        qa, out = r.step(0, fused=st == 1)
+        r.check_out(0, qa, out, f"step {st}")
+    for b in (0, 22, 23):
+        for h in range(4):
+            r.check_unit(0, h, b)
+    r.free()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_decode_past_four_gigabytes(paged):
+    """Rows, scale pairs and pages whose offsets pass 2^32: keys of zero give
+    every row the same weight, a loud key at the very end takes all of it."""
+    D, H, n, step = 64, 4, 17_000_000, 1_000_000
+    pol = hwkv.policy_set(1, H, H, D, 0, [0], [[0] * H])
+    cache = hwkv.cache_alloc(pol, 1, n, kv_format="i8", n_pages=H * -(-n // 256) if paged else None)
+    assert hwkv.cache_bytes(pol, 1, n, "i8") > 2 * 2 ** 32
+    total = torch.zeros((H, D), dtype=torch.float64, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for p0 in range(0, n, step):
+        log(f"rows {p0}")
+        k = torch.zeros((step, H, D), dtype=torch.bfloat16, device=DEV)
+        # rows whose codes are exact: multiples of 1/64 below 2, the first 1
+        v = (torch.randint(-100, 101, (step, H, D), generator=g, device=DEV).float() / 64).to(torch.bfloat16)
+        v[:, :, 0] = 1.0
+        v = v.clamp(-1.5, 1.5)
+        if p0 + step == n:
+            k[-1] = 8.0
+            last = v[-1].double()
+        total += v.double().sum(dim=0)
+        hwkv.prefill_write(cache, 0, 0, p0, k, v)
+    ws = torch.empty(hwkv.decode_workspace_bytes(cache), dtype=torch.uint8, device=DEV)
+    out = torch.empty((1, H, D), device=DEV)
+    hwkv.decode_attn(cache, 0, torch.zeros((1, H, D), dtype=torch.bfloat16, device=DEV), 1.0, out, ws)
+    # fp32 sums of 17M terms in thousands of parts: far below 1e-4 of a row's largest
+    assert (out[0].double() - total / n).abs().max() < 1e-4
+    hwkv.decode_attn(cache, 0, torch.full((1, H, D), 2.0, device=DEV).to(torch.bfloat16), 1.0, out, ws)
+    assert (out[0].double() - last).abs().max() < 1e-5        # e^-1024 is zero
+    cache.free()
+
+
+def test_two_streams_at_once():
+    """Calls on two caches and two streams, each with its own workspace, give
+    what they give alone."""
+    runs = [Run8(mini(seed=50 + i, batch=3, head_dim=128, n_q_heads=16, n_kv_heads=4, levels=[[0, 1, 1, 0]],
+                      prompt=[3000, 500, 77], max_ctx=3200)) for i in range(2)]
+    qs, alone = [], []
+    for i, r in enumerate(runs):
+        for b in range(3):
+            r.prefill(0, b)
+        qs.append(up(W.normal_bf16((3, 16, 128), 60 + i, 0, W.Q, 0), DEV))
+        alone.append(torch.empty((3, 16, 128), device=DEV))
+        hwkv.decode_attn(r.cache, 0, qs[i], r.scale, alone[i], r.ws)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in runs], [torch.zeros_like(a) for a in alone]
+    for _ in range(20):
+        for i, r in enumerate(runs):
+            hwkv.decode_attn(r.cache, 0, qs[i], r.scale, outs[i], r.ws, stream=streams[i])
+    torch.cuda.synchronize()
+    for i, r in enumerate(runs):
+        assert torch.equal(outs[i], alone[i])
+        r.free()
+
+
 @pytest.mark.parametrize("where", ["k", "v"])
 def test_decode_a_row_that_is_not_finite_poisons_only_what_sees_it(where):
     D, n = 64, 300
