@@ -218,3 +218,23 @@ def test_binding_checks(hw):
         hw.rope_apply(rope, pos, None, None, None, None)
     with pytest.raises(ValueError):
         hw.rope_apply(rope, pos, x, None, None, None)
+
+
+# ---------------------------------------------------------------------------
+# the kernels' registers
+# ---------------------------------------------------------------------------
+def test_kernels_are_present_within_their_registers(tmp_path):
+    """Two wavefronts per SIMD for int8 decode (256 registers); none of them, nor
+    the rotation's, uses scratch."""
+    import os
+
+    from paper_2609_02029_amd import build
+    from test_kernel_resources import _compile, _kernels
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("hipcc not found")
+    found = {}
+    for src in ("decode_i8.hip", "rope_kernels.hip"):
+        for name, vgprs, scratch in _kernels(_compile(src, str(tmp_path))):
+            assert vgprs <= 256 and scratch == 0, (name, vgprs, scratch)
+            found[name.split("<")[0]] = found.get(name.split("<")[0], 0) + 1
+    assert found == {"decode_i8": 30, "i8_merge": 15, "rope": 3, "append_rope": 12}, found
