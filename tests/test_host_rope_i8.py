@@ -232,9 +232,9 @@ def test_kernels_are_present_within_their_registers(tmp_path):
     from test_kernel_resources import _compile, _kernels
     if not os.path.exists(build.HIPCC):
         pytest.skip("hipcc not found")
-    found = {}
-    for src in ("decode_i8.hip", "rope_kernels.hip"):
-        for name, vgprs, scratch in _kernels(_compile(src, str(tmp_path))):
-            assert vgprs <= 256 and scratch == 0, (name, vgprs, scratch)
-            found[name.split("<")[0]] = found.get(name.split("<")[0], 0) + 1
-    assert found == {"decode_i8": 30, "i8_merge": 15, "rope": 3, "append_rope": 12}, found
+    # head_dims x groups x (split, by item), and the merge; head_dims x (1 + formats)
+    for src, count in (("decode_i8.hip", 3 * 5 * 3), ("rope_kernels.hip", 3 * (1 + 4))):
+        kernels = _kernels(_compile(src, str(tmp_path)))
+        assert len(kernels) == count, (src, [name for name, _, _ in kernels])
+        for name, vgprs, scratch in kernels:
+            assert vgprs <= 256 and scratch == 0, (src, name, vgprs, scratch)
