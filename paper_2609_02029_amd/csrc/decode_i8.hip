@@ -36,7 +36,7 @@
 // computed, so two tiles of every wave are always in flight: 66 KB a workgroup at
 // head_dim 256, two workgroups per CU (more at 64 and 128: rings of four and eight
 // tiles, which left room for two, were slower by 1 to 20 %).  No barrier falls
-// inside the walk.  16 sequences of 16K to 64K tokens, 256 x 6: 530 MB in 92 us, 5.8
+// inside the walk.  16 sequences of 16K to 64K tokens, 256 x 6: 530 MB in 90 us, 5.9
 // TB/s; a launch costs about 6 us beyond its bytes.
 #include <algorithm>
 
@@ -134,10 +134,13 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
     const ItemHead &hd = a.head[h];
     nv = min(n, hd.cap);
     const int all_tiles = (nv + 63) / 64;
-    first = split * a.tiles_per_wg;
-    if (first >= all_tiles) return;              // uniform: a shorter item
+    // an item of more than tiles_per_wg tiles in equal shares (none of them empty)
+    const int splits = (all_tiles + a.tiles_per_wg - 1) / a.tiles_per_wg;
+    if (split >= splits) return;                 // uniform: a shorter item
+    const int share = (all_tiles + splits - 1) / splits;
+    first = split * share;
     step = 1;
-    last = min(all_tiles, first + a.tiles_per_wg);
+    last = min(all_tiles, first + share);
     whole = last - first == all_tiles;
     pto = hd.page0 >= 0 ? hd.page0 + b * a.max_pages : -1;
     koff = hd.k_off + (int64_t)b * hd.cap_pad * D;

@@ -747,16 +747,49 @@ int64_t item_splits(const hwkv_cache *c, int32_t u, int32_t len, int64_t T) {
   return (tiles_for(std::min<int64_t>(len, c->cap[u])) + T - 1) / T;
 }
 
+// Tiles per workgroup of an int8 launch by item (len: longest first): the fewest,
+// from 8 up, at which all workgroups run at once (where the items alone are not more;
+// a sixteenth to spare, since shorter items leave empty ones among them), and at
+// which the partials fit.
+// decode_i8's registers hold four workgroups per CU at head_dim 64 (five: 61 us
+// against 38 for 32 sequences of 100-9,000 tokens, 8 KV heads), three at 128, two at
+// 256.  Against an even share of two per CU, us a layer: 256 x 6, 40 sequences of
+// 200-6,000 tokens, 4 KV heads 33 / 39, 24 of 2,000-30,000 53 / 58, 256 x 8, 12 of
+// 4,000 44 / 50; 128 x 4, 48 of 200-6,000 39 / 36.
+int64_t i8_tiles_per_wg(const hwkv_cache *c, int32_t layer, const int32_t *len, int32_t n, int64_t total,
+                        int64_t longest, int64_t most_parts) {
+  const int32_t H = c->pol.n_kv_heads, D = c->pol.head_dim;
+  const int64_t cus = hwkv::device_cu_count();
+  const int64_t slots = cus * (D == 64 ? 4 : D == 128 ? 3 : 2) * 15 / 16;
+  const bool at_once = (int64_t)n * H < slots;
+  int64_t T = std::max<int64_t>(8, (at_once ? total / slots : total / (2 * cus)) + 1);
+  for (; T < longest; T += 1 + T / 16) {
+    int64_t wgs = 0, parts = 0;
+    for (int32_t h = 0; h < H; ++h) {
+      const int32_t u = layer * H + h;
+      const int64_t top = item_splits(c, u, len[0], T);
+      for (int32_t i = 0; i < n; ++i) {
+        const int64_t s = item_splits(c, u, len[i], T);
+        if (s <= 1) {                 // and no longer one follows
+          wgs += n - i;
+          break;
+        }
+        wgs += s;
+        parts += top;
+      }
+    }
+    if (parts <= most_parts && (!at_once || wgs <= slots)) break;
+  }
+  return T;
+}
+
 // Plans the launch of sequences [b0, b0 + n), heads in `order` (by capacity),
 // with room for the partials of `parts` workgroups, and estimates its time.
 //
-// int8 (decode_i8, two to four workgroups per CU): T is an even share of two
-// workgroups per CU, and at least 8 tiles (the 48 sequences below 41 us; 0.5 / 0.75
-// / 1.5 shares 42.5 / 40.5 / 44.5; 16 sequences of 1,000 tokens, 8 KV heads, with at
-// least 2 / 4 / 8 tiles 19.8 / 15.6 / 15.1).
-// The others: T is a quarter above an even share of the CUs (48 ragged sequences of
-// 200-6,000 tokens, 8 KV heads: 84 us a layer with whole items, 78 / 77 at 1.0 /
-// 1.5 shares, 81 / 85 at 0.5 / 0.3), and at least one tile for each of 16 waves.
+// int8: i8_tiles_per_wg.  The others: T is a quarter above an even share of the CUs
+// (48 ragged sequences of 200-6,000 tokens, 8 KV heads: 84 us a layer with whole
+// items, 78 / 77 at 1.0 / 1.5 shares, 81 / 85 at 0.5 / 0.3), and at least one tile for
+// each of 16 waves.
 //
 // The estimate, in us: a start; on a CU, one workgroup at a time (two where the
 // registers let them: fp8, one q head), each with a part for its q heads, one for
@@ -783,7 +816,8 @@ void plan_item_launch(const hwkv_cache *c, int32_t layer, const int32_t *order, 
   const int64_t longest =
       std::max<int64_t>(1, tiles_for(std::min<int64_t>(L->len[0], c->cap[layer * H + order[0]])));
   int64_t T = std::max<int64_t>(16, total * 5 / (4 * cus) + 1);
-  if (c->fmt == HWKV_KV_I8) T = std::max<int64_t>(8, total / (2 * cus) + 1);
+  if (c->fmt == HWKV_KV_I8)
+    T = i8_tiles_per_wg(c, layer, L->len, n, total, longest, std::min<int64_t>(parts, UINT16_MAX));
   if (longest <= T + T / 4) T = longest;
   int64_t runs = 0;
   for (int32_t h = 0; h < H; ++h) runs += item_splits(c, layer * H + h, L->len[0], T);
