@@ -747,22 +747,22 @@ int64_t item_splits(const hwkv_cache *c, int32_t u, int32_t len, int64_t T) {
   return (tiles_for(std::min<int64_t>(len, c->cap[u])) + T - 1) / T;
 }
 
-// Tiles per workgroup of an int8 launch by item (len: longest first): the fewest,
-// from 8 up, at which all workgroups run at once (where the items alone are not more;
-// a sixteenth to spare, since shorter items leave empty ones among them), and at
-// which the partials fit.
-// decode_i8's registers hold four workgroups per CU at head_dim 64 (five: 61 us
-// against 38 for 32 sequences of 100-9,000 tokens, 8 KV heads), three at 128, two at
-// 256.  Against an even share of two per CU, us a layer: 256 x 6, 40 sequences of
-// 200-6,000 tokens, 4 KV heads 33 / 39, 24 of 2,000-30,000 53 / 58, 256 x 8, 12 of
-// 4,000 44 / 50; 128 x 4, 48 of 200-6,000 39 / 36.
+// Tiles per workgroup of an int8 launch by item (len: longest first): an even share of
+// two workgroups per CU, at least 8, and more until all workgroups run at once (where
+// the items alone are not more than can) and the partials fit.  decode_i8's registers
+// hold four workgroups per CU at head_dim 64, three at 128 and two at 256; a
+// sixteenth to spare, since shorter items leave empty ones among them.  us a layer
+// against the even share alone: 256 x 6, 40 sequences of 200-6,000 tokens, 4 KV heads
+// 33 / 39, 24 of 2,000-30,000 53 / 58, 256 x 8, 12 of 4,000 43 / 50.  Starting from as
+// many as can run instead: 128 x 4, 16 of 1,000-20,000, 8 KV heads 91 against 84, 128 x
+// 8, 24 of 100-12,000 80 against 72; 64 x 4, 32 of 12,000 73 against 76.
 int64_t i8_tiles_per_wg(const hwkv_cache *c, int32_t layer, const int32_t *len, int32_t n, int64_t total,
                         int64_t longest, int64_t most_parts) {
   const int32_t H = c->pol.n_kv_heads, D = c->pol.head_dim;
   const int64_t cus = hwkv::device_cu_count();
   const int64_t slots = cus * (D == 64 ? 4 : D == 128 ? 3 : 2) * 15 / 16;
   const bool at_once = (int64_t)n * H < slots;
-  int64_t T = std::max<int64_t>(8, (at_once ? total / slots : total / (2 * cus)) + 1);
+  int64_t T = std::max<int64_t>(8, total / (2 * cus) + 1);
   for (; T < longest; T += 1 + T / 16) {
     int64_t wgs = 0, parts = 0;
     for (int32_t h = 0; h < H; ++h) {
