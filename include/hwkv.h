@@ -376,8 +376,8 @@ int hwkv_append(hwkv_cache *cache, int32_t layer, const void *k_new,
  *   pairs      HWKV_ROPE_HALF or HWKV_ROPE_PAIRS
  *   n_axes     positions per token (1 for text; time, height and width for
  *              video), 1 <= n_axes <= 8
- *   freq       host double [rot_dim / 2], finite: theta^(-2i / rot_dim), scaled
- *              as the model scales it
+ *   freq       host double [rot_dim / 2], of magnitude at most 1e6:
+ *              theta^(-2i / rot_dim), scaled as the model scales it
  *   axis       host int32 [rot_dim / 2], in [0, n_axes): the position that turns
  *              each pair, blocks or interleaved; NULL = axis 0 for all
  *   magnitude  finite factor of the turned channels (1 in most models)
@@ -389,7 +389,8 @@ int hwkv_rope_set(hwkv_rope **out, int32_t head_dim, int32_t rot_dim,
 
 int hwkv_rope_free(hwkv_rope *rope);
 
-/* Rotate the query and key heads of n_tokens tokens, in one launch.
+/* Rotate the query and key heads of n_tokens tokens, in one launch (one for
+ * every 2^22 tokens).
  *   pos             device int32 [n_axes][n_tokens], any values
  *   q, k            device bf16, n_q_heads (n_kv_heads) rows of head_dim
  *                   contiguous channels per token, the tokens q_stride
@@ -401,8 +402,9 @@ int hwkv_rope_free(hwkv_rope *rope);
  * Either side may be absent: 0 heads, null pointers.  Angles are exact to fp32's
  * last place, or 2^-22 of a turn for the farthest positions; fp32 products, one
  * rounding to bf16 (to nearest even).  Pointers 16-byte aligned (pos 4-byte).
- * n_tokens == 0 is a no-op.  EINVAL on bad shapes, strides, alignment or
- * overlap, or n_tokens * head_dim >= 2^35. */
+ * n_tokens == 0 is a no-op.  EINVAL on bad shapes, strides (above 2^31 among
+ * them), alignment or overlap, more than 65536 heads, or n_tokens * head_dim >=
+ * 2^35. */
 int hwkv_rope_apply(const hwkv_rope *rope, int64_t n_tokens, int32_t n_q_heads,
                     int32_t n_kv_heads, const int32_t *pos, const void *q,
                     int64_t q_stride, const void *k, int64_t k_stride,

@@ -333,7 +333,8 @@ int check_rows(const char *name, const void *in, int64_t stride, const void *out
   if (!in || !out) return fail(HWKV_EINVAL, std::string(name) + " and its output must be non-null");
   if ((uintptr_t)in % 16 != 0 || (uintptr_t)out % 16 != 0)
     return fail(HWKV_EINVAL, std::string(name) + " must be 16-byte aligned");
-  if (stride % 8 != 0 || stride < elems || stride > ((int64_t)1 << 31) || (n - 1) > ((int64_t)1 << 58) / stride)
+  if (stride % 8 != 0 || stride < elems || stride > ((int64_t)1 << 31) ||
+      n - 1 > ((int64_t)1 << 58) / stride)
     return fail(HWKV_EINVAL, std::string(name) + " stride must be a multiple of 8 elements, at "
                                                  "least a row's, and at most 2^31");
   *span = {in, ((n - 1) * stride + elems) * 2};
@@ -2307,26 +2308,36 @@ int hwkv_rope_apply(const hwkv_rope *rope, int64_t n_tokens, int32_t n_q_heads,
   RowSpan span[3] = {{pos, rope->n_axes * n_tokens * 4}};
   int rc = check_rows("q", q, q_stride, q_out, n_tokens, n_q_heads * D, &span[1]);
   if (rc == HWKV_OK) rc = check_rows("k", k, k_stride, k_out, n_tokens, n_kv_heads * D, &span[2]);
-  if (rc == HWKV_OK && n_q_heads > 0) rc = check_apart("q_out", q_out, q, n_tokens * n_q_heads * D, q_stride == n_q_heads * D, span, 3);
-  if (rc == HWKV_OK && n_kv_heads > 0) rc = check_apart("k_out", k_out, k, n_tokens * n_kv_heads * D, k_stride == n_kv_heads * D, span, 3);
-  if (rc == HWKV_OK && n_q_heads > 0 && n_kv_heads > 0 &&
-      overlap({q_out, n_tokens * n_q_heads * D * 2}, {k_out, n_tokens * n_kv_heads * D * 2}))
+  const int64_t q_row = n_q_heads * D, k_row = n_kv_heads * D;
+  if (rc == HWKV_OK && q_row > 0)
+    rc = check_apart("q_out", q_out, q, n_tokens * q_row, q_stride == q_row, span, 3);
+  if (rc == HWKV_OK && k_row > 0)
+    rc = check_apart("k_out", k_out, k, n_tokens * k_row, k_stride == k_row, span, 3);
+  if (rc == HWKV_OK && q_row > 0 && k_row > 0 &&
+      overlap({q_out, n_tokens * q_row * 2}, {k_out, n_tokens * k_row * 2}))
     rc = fail(HWKV_EINVAL, "q_out and k_out overlap");
   if (rc != HWKV_OK) return rc;
   hwkv::RopeArgs a;
   a.rope = rope->table;
-  a.pos = pos;
-  a.q = static_cast<const uint16_t *>(q);
-  a.k = static_cast<const uint16_t *>(k);
-  a.q_out = static_cast<uint16_t *>(q_out);
-  a.k_out = static_cast<uint16_t *>(k_out);
-  a.n = n_tokens;
+  a.pos_stride = n_tokens;
   a.q_stride = q_stride;
   a.k_stride = k_stride;
   a.n_q = n_q_heads;
   a.n_k = n_kv_heads;
-  rc = check_device(hwkv::launch_rope((int)D, a, (hipStream_t)stream), "rope launch");
-  return rc == HWKV_OK ? ok() : rc;
+  // (an absent side is never addressed)
+  const uint16_t *const qi = static_cast<const uint16_t *>(q), *const ki = static_cast<const uint16_t *>(k);
+  uint16_t *const qo = static_cast<uint16_t *>(q_out), *const ko = static_cast<uint16_t *>(k_out);
+  for (int64_t t = 0; t < n_tokens; t += hwkv::kRopeLaunch) {
+    a.n = std::min(hwkv::kRopeLaunch, n_tokens - t);
+    a.pos = pos + t;
+    a.q = q_row > 0 ? qi + t * q_stride : nullptr;
+    a.k = k_row > 0 ? ki + t * k_stride : nullptr;
+    a.q_out = q_row > 0 ? qo + t * q_row : nullptr;
+    a.k_out = k_row > 0 ? ko + t * k_row : nullptr;
+    rc = check_device(hwkv::launch_rope((int)D, a, (hipStream_t)stream), "rope launch");
+    if (rc != HWKV_OK) return rc;
+  }
+  return ok();
 }
 
 int hwkv_append_rope(hwkv_cache *c, int32_t layer, const hwkv_rope *rope, const int32_t *pos,
@@ -2346,7 +2357,8 @@ int hwkv_append_rope(hwkv_cache *c, int32_t layer, const hwkv_rope *rope, const 
   int rc = check_rows("k_new", k_new, k_stride, k_new, B, H * D, &span[2]);
   if (rc == HWKV_OK) rc = check_rows("v_new", v_new, v_stride, v_new, B, H * D, &span[3]);
   if (rc == HWKV_OK) rc = check_rows("q", q, q_stride, q_out, B, n_q * D, &span[4]);
-  if (rc == HWKV_OK && q) rc = check_apart("q_out", q_out, q, B * n_q * D, q_stride == n_q * D, span, 5);
+  if (rc == HWKV_OK && q)
+    rc = check_apart("q_out", q_out, q, B * n_q * D, q_stride == n_q * D, span, 5);
   if (rc != HWKV_OK) return rc;
   for (int32_t b = 0; b < B; ++b)
     for (int32_t h = 0; h < H; ++h) {

@@ -197,13 +197,16 @@ struct RopeTable {
 
 // Rotation of n tokens' q and k heads: grid x over the tokens in groups of
 // tokens_per, grid y over the heads in groups of heads_per (both set at launch).
+// A launch has up to kRopeLaunch tokens: 2^32 work items are more than a grid
+// dimension holds.
 constexpr int kRopeTokens = 8;
+constexpr int64_t kRopeLaunch = (int64_t)1 << 22;
 struct RopeArgs {
   RopeTable rope;
-  const int32_t *pos;            // [n_axes][n]
+  const int32_t *pos;            // of the launch's first token, axes pos_stride apart
   const uint16_t *q, *k;         // rows of n_q, n_k heads, q_stride / k_stride apart
   uint16_t *q_out, *k_out;       // [n][heads][D]
-  int64_t n, q_stride, k_stride; // strides in elements
+  int64_t n, pos_stride, q_stride, k_stride;   // strides in elements
   int32_t n_q, n_k, tokens_per, heads_per;
 };
 hipError_t launch_rope(int D, const RopeArgs &a, hipStream_t s);

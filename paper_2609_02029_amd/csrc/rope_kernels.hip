@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256) void rope(RopeArgs a) {
     if (r0 < RW) {                               // once, behind the first rows' loads
       for (int i = threadIdx.x; i < toks * pairs; i += 256) {
         const int t = i / pairs, p = i - t * pairs;
-        cos_sin(a.rope, a.pos + tok0 + t, a.n, p, &cs[0][i], &cs[1][i]);
+        cos_sin(a.rope, a.pos + tok0 + t, a.pos_stride, p, &cs[0][i], &cs[1][i]);
       }
       __syncthreads();
     }

@@ -132,6 +132,24 @@ def test_many_heads_no_tokens_and_another_stream():
     hwkv.rope_apply(rope, pos[:0], none, None, none, None)
 
 
+def test_more_tokens_than_one_launch():
+    """The tokens past the first launch's, which start at neither side's first row,
+    of strided q and k in place, with two axes of positions."""
+    rope, freq, axis = rotation(64, 16, 2, 4)
+    n, cut = 2 ** 22 + 300, 2 ** 22 - 5
+    pos = torch.randint(0, 10 ** 6, (2, n), device=DEV, dtype=torch.int32)
+    both = torch.randn((n, 2, 64), dtype=torch.bfloat16, device=DEV)
+    q, k = both[:, :1], both[:, 1:].contiguous()
+    qo, ko = torch.empty((n, 1, 64), dtype=torch.bfloat16, device=DEV), k.clone()
+    hwkv.rope_apply(rope, pos, q, ko, qo, ko)
+    few = pos[:, cut:].contiguous()
+    q2, k2 = (torch.empty((n - cut, 1, 64), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    hwkv.rope_apply(rope, few, q[cut:], k[cut:], q2, k2)
+    assert torch.equal(qo[cut:], q2) and torch.equal(ko[cut:], k2)
+    close(q2, turned(q[cut:], few, freq, axis, "half"), q[cut:], 16, 1e6)
+    close(ko[:50], turned(k[:50], pos[:, :50], freq, axis, "half"), k[:50], 16, 1e6)
+
+
 FORMATS = ["bf16", "f16", "fp8", "i8"]
 
 
