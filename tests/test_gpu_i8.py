@@ -478,6 +478,85 @@ def test_prefill_attention(D, G, P, chunks, paged):
     r.free()
 
 
+@pytest.mark.parametrize("split", [False, True])
+def test_prefill_ignores_what_lies_behind_the_last_row(split):
+    """The buffer, the workspace and the partials may hold anything; the keys split
+    or not."""
+    D, G, n0, n = 128, 4, 650, 40
+    x = {kind: up(W.normal_bf16((n0 + n, 2, D), 3, 0, kind, 0), DEV) for kind in (W.K, W.V)}
+    k, v = x[W.K], x[W.V]
+    q = up(W.normal_bf16((n, 2 * G, D), 3, 0, W.Q, 0), DEV)
+    pol = hwkv.policy_set(1, 2, 2 * G, D, 3, [70, 0], [[0, 1]])
+    outs = []
+    for fill in (0x00, 0xff, 0x80):
+        buf = torch.full((hwkv.cache_bytes(pol, 1, 800, "i8"),), fill, dtype=torch.uint8, device=DEV)
+        cache = hwkv.cache_alloc(pol, 1, 800, dev_buf=buf, kv_format="i8")
+        hwkv.prefill_write(cache, 0, 0, 0, k[:n0], v[:n0])
+        ws = torch.full((hwkv.prefill_attn_workspace_bytes(cache, n),), fill, dtype=torch.uint8, device=DEV)
+        size = hwkv.prefill_attn_split_bytes(cache, 0, n0, n) if split else 0
+        parts = torch.full((max(size, 16),), fill, dtype=torch.uint8, device=DEV)
+        out = torch.empty((n, 2 * G, D), device=DEV)
+        hwkv.prefill_attn(cache, 0, 0, n0, q, k[n0:], v[n0:], 0.1, out, ws=ws, parts=parts)
+        outs.append(out.cpu())
+        cache.free()
+    assert torch.isfinite(outs[0]).all() and torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+def test_a_released_sequence_leaves_nothing_behind():
+    """Pages of a released sequence, whose rows were not finite, taken by others."""
+    c = mini(batch=3, head_dim=64, prompt=[700, 300, 520], max_ctx=800)
+    r = Run8(c, n_pages=3 + 2 + 3 + 1)
+    for b in range(3):
+        r.prefill(0, b)
+    bad = torch.full((700, 2, 64), float("inf"), dtype=torch.bfloat16, device=DEV)
+    hwkv.cache_reset_seq(r.cache, 0)
+    hwkv.prefill_write(r.cache, 0, 0, 0, bad, bad)
+    r.reset(0)
+    r.prefill(0, 0, P=130)           # into the first of its pages
+    r.reset(2)
+    r.prefill(0, 2, P=777)           # its own, and one of those
+    for st in range(2):
+        qa, out = r.step(0, fused=st == 1)
+        r.check_out(0, qa, out, f"step {st}")
+    r.check_layer(0)
+    r.free()
+
+
+@pytest.mark.parametrize("batch", [2, 24])
+def test_timed_steps_and_two_graphs(batch):
+    """Timing events around both ways of launching, and two captured calls, of
+    different layers, that share a workspace on one stream."""
+    c = mini(batch=batch, n_layers=2, head_dim=64, n_q_heads=8, n_kv_heads=4, levels=[[0, 1, 1, 0], [1, 1, 0, 0]],
+             prompt=[400 + 31 * i for i in range(batch)], max_ctx=1300)
+    r = Run8(c)
+    for layer in range(2):
+        for b in range(batch):
+            r.prefill(layer, b)
+    q = up(W.normal_bf16((batch, 8, 64), 1, 0, W.Q, 0), DEV)
+    want = [torch.empty((batch, 8, 64), device=DEV) for _ in range(2)]
+    got = [torch.zeros_like(want[0]) for _ in range(2)]
+    hwkv.decode_timing(r.cache, True)
+    for layer in range(2):
+        hwkv.decode_attn(r.cache, layer, q, r.scale, want[layer], r.ws)
+    split_ms, merge_ms, launches = hwkv.decode_timing_read(r.cache)
+    hwkv.decode_timing(r.cache, False)
+    assert split_ms > 0 and merge_ms >= 0 and launches >= 2
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for layer, g in enumerate(graphs):
+        with torch.cuda.graph(g):
+            hwkv.decode_attn(r.cache, layer, q, r.scale, got[layer], r.ws)
+    for i in range(3):
+        q.copy_(up(W.normal_bf16((batch, 8, 64), 1, 0, W.Q, i), DEV))
+        for layer in range(2):
+            got[layer].zero_()
+            hwkv.decode_attn(r.cache, layer, q, r.scale, want[layer], r.ws)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+    r.free()
+
+
 def test_prefill_refuses_a_cache_without_workspace():
     r = Run8(mini())
     x = torch.zeros((4, 8, 64), dtype=torch.bfloat16, device=DEV)
