@@ -34,7 +34,8 @@ import statistics
 import sys
 
 KERNELS = (r"(decode_split<[^>]*>|decode_mfma<[^>]*>|decode_combine<[^>]*>|prefill_write<[^>]*>"
-           r"|append_token<[^>]*>|prefill_attn<[^>]*>)")
+           r"|append_token<[^>]*>|prefill_attn<[^>]*>|decode_i8<[^>]*>|i8_merge<[^>]*>"
+           r"|append_rope<[^>]*>|rope<[^>]*>|stage_rows<[^>]*>)")
 N_SIMD = 1024   # 256 CUs x 4 SIMDs
 N_CU = 256
 # GRBM_GUI_ACTIVE comes back as one value per dispatch that sums the active
