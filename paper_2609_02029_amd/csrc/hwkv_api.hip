@@ -341,12 +341,13 @@ int check_rows(const char *name, const void *in, int64_t stride, const void *out
   return HWKV_OK;
 }
 
-// Whether an output of `elems` elements is its own input, in place, or apart
-// from every range the call reads.
-int check_apart(const char *name, const void *out, const void *in, int64_t elems, bool contiguous,
+// Whether an output of `elems` elements is its own input reads[own], in place, or
+// apart from it, and apart from every other range the call reads (one that starts
+// where its own input does among them: its rows would be read as they are turned).
+int check_apart(const char *name, const void *out, int own, int64_t elems, bool contiguous,
                 const RowSpan *reads, int n) {
   for (int i = 0; i < n; ++i) {
-    if (out == in && contiguous && reads[i].at == in) continue;
+    if (i == own && contiguous && out == reads[i].at) continue;
     if (overlap({out, elems * 2}, reads[i]))
       return fail(HWKV_EINVAL, std::string(name) + " overlaps an input");
   }
@@ -2310,9 +2311,9 @@ int hwkv_rope_apply(const hwkv_rope *rope, int64_t n_tokens, int32_t n_q_heads,
   if (rc == HWKV_OK) rc = check_rows("k", k, k_stride, k_out, n_tokens, n_kv_heads * D, &span[2]);
   const int64_t q_row = n_q_heads * D, k_row = n_kv_heads * D;
   if (rc == HWKV_OK && q_row > 0)
-    rc = check_apart("q_out", q_out, q, n_tokens * q_row, q_stride == q_row, span, 3);
+    rc = check_apart("q_out", q_out, 1, n_tokens * q_row, q_stride == q_row, span, 3);
   if (rc == HWKV_OK && k_row > 0)
-    rc = check_apart("k_out", k_out, k, n_tokens * k_row, k_stride == k_row, span, 3);
+    rc = check_apart("k_out", k_out, 2, n_tokens * k_row, k_stride == k_row, span, 3);
   if (rc == HWKV_OK && q_row > 0 && k_row > 0 &&
       overlap({q_out, n_tokens * q_row * 2}, {k_out, n_tokens * k_row * 2}))
     rc = fail(HWKV_EINVAL, "q_out and k_out overlap");
@@ -2358,7 +2359,7 @@ int hwkv_append_rope(hwkv_cache *c, int32_t layer, const hwkv_rope *rope, const 
   if (rc == HWKV_OK) rc = check_rows("v_new", v_new, v_stride, v_new, B, H * D, &span[3]);
   if (rc == HWKV_OK) rc = check_rows("q", q, q_stride, q_out, B, n_q * D, &span[4]);
   if (rc == HWKV_OK && q)
-    rc = check_apart("q_out", q_out, q, B * n_q * D, q_stride == n_q * D, span, 5);
+    rc = check_apart("q_out", q_out, 4, B * n_q * D, q_stride == n_q * D, span, 5);
   if (rc != HWKV_OK) return rc;
   for (int32_t b = 0; b < B; ++b)
     for (int32_t h = 0; h < H; ++h) {
