@@ -400,8 +400,8 @@ int hwkv_rope_free(hwkv_rope *rope);
  *                   itself where that is contiguous, and must not overlap any
  *                   input otherwise
  * Either side may be absent: 0 heads, null pointers.  Angles are exact to fp32's
- * last place, or 2^-22 of a turn for the farthest positions; fp32 products, one
- * rounding to bf16 (to nearest even).  Pointers 16-byte aligned (pos 4-byte).
+ * last place at every position and frequency; fp32 products, one rounding to bf16
+ * (to nearest even).  Pointers 16-byte aligned (pos 4-byte).
  * n_tokens == 0 is a no-op.  EINVAL on bad shapes, strides (above 2^31 among
  * them), alignment or overlap, more than 65536 heads, or n_tokens * head_dim >=
  * 2^35. */

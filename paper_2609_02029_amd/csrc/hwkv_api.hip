@@ -2269,7 +2269,8 @@ int hwkv_rope_set(hwkv_rope **out, int32_t head_dim, int32_t rot_dim, int32_t pa
   if (!freq) return fail(HWKV_EINVAL, "freq is null");
   if (!std::isfinite(magnitude)) return fail(HWKV_EINVAL, "magnitude must be finite");
   for (int32_t i = 0; i < rot_dim / 2; ++i) {
-    // (a position has 31 bits, and the product keeps its fraction up to 2^52 turns)
+    // (2^31 x 1e6 radians are 2^49 turns: an fp64 product still has their fraction's
+    // first bits, and its rest the others)
     if (!(std::fabs(freq[i]) <= 1e6)) return fail(HWKV_EINVAL, "freq must be finite, at most 1e6");
     if (axis && (axis[i] < 0 || axis[i] >= n_axes))
       return fail(HWKV_EINVAL, "axis must be in [0, n_axes)");
@@ -2283,7 +2284,10 @@ int hwkv_rope_set(hwkv_rope **out, int32_t head_dim, int32_t rot_dim, int32_t pa
   r->table.pairs = pairs;
   r->table.magnitude = magnitude;
   for (int32_t i = 0; i < rot_dim / 2; ++i) {
-    r->table.turns[i] = (double)((long double)freq[i] / 6.283185307179586476925286766559L);
+    // freq / 2 pi to 2^-106: 1 / 2 pi in two doubles, the product's rest by an fma
+    const double a = 0x1.45f306dc9c883p-3, b = -0x1.6b01ec5417056p-57, t = freq[i] * a;
+    r->table.turns[i] = t;
+    r->table.turns_low[i] = (float)(std::fma(freq[i], a, -t) + freq[i] * b);
     r->table.axis[i] = (uint8_t)(axis ? axis[i] : 0);
   }
   *out = r;

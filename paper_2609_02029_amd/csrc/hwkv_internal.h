@@ -185,10 +185,11 @@ struct AppendArgs {
 };
 
 // A rotation of the first rot_dim channels of a head (rope_kernels.hip): pair
-// i turns by pos[axis[i]] * turns[i] whole turns.
+// i turns by pos[axis[i]] * (turns[i] + turns_low[i]) whole turns.
 constexpr int kMaxPairs = 128;   // rot_dim / 2 at head_dim 256
 struct RopeTable {
-  double turns[kMaxPairs];       // turns per position, of each pair
+  double turns[kMaxPairs];       // turns per position, of each pair,
+  float turns_low[kMaxPairs];    // and what that leaves of them
   uint8_t axis[kMaxPairs];
   int32_t rot_dim;
   int32_t pairs;                 // HWKV_ROPE_*: which channels make a pair

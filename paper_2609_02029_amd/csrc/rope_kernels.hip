@@ -5,11 +5,14 @@
 // t = pos[axis[i]] freq[i]:
 //     a' = a cos t - b sin t,   b' = b cos t + a sin t,
 // both times the rotation's magnitude; the channels past rot_dim stay.  The
-// angle is taken in turns, pos x (freq / 2 pi), as one fp64 product whose nearest
-// whole number is dropped, so that a position of 2^31 still has its angle to
-// 2^-22 of a turn and near ones to fp32's last place; sine and cosine, and the
-// products, are fp32; one rounding to bf16 at the end.  The compiler contracts
-// nothing here by itself, so that both kernels turn a pair to the same bits.
+// angle is taken in turns, pos x (freq / 2 pi), with freq / 2 pi as a double and
+// the float that it leaves (2^-77 of it), and the product as an fp64 one, whose
+// nearest whole number is dropped, and its own rest: up to 2^49 turns (a position
+// of 2^31 at a frequency of 10^6) the fraction has fp32's last place.  (The fp64
+// product alone is off by 2^-23 turns at 2^31 x 3 radians, 2^-4 at 2^31 x 10^6.)
+// Sine and cosine, and the products, are fp32; one rounding to bf16 at the end.
+// The compiler contracts nothing here by itself, so that both kernels turn a pair
+// to the same bits.
 //
 // A lane holds 16 channels of a head: 8 pairs, which are chunks c and
 // c + rot_dim / 16 (halves) or 2c and 2c + 1 (adjacent pairs) of 8 channels.
@@ -30,8 +33,9 @@ __device__ __forceinline__ uint4 chunk(u4 x) { return make_uint4(x.x, x.y, x.z, 
 __device__ __forceinline__ void cos_sin(const RopeTable &t, const int32_t *pos, int64_t stride, int p,
                                         float *c, float *s) {
 #pragma clang fp contract(off)
-  const double x = (double)pos[t.axis[p] * stride] * t.turns[p];
-  const float f = 2.0f * (float)(x - __builtin_rint(x));
+  const double at = pos[t.axis[p] * stride], x = at * t.turns[p];
+  const double rest = __builtin_fma(at, t.turns[p], -x) + at * (double)t.turns_low[p];
+  const float f = 2.0f * (float)((x - __builtin_rint(x)) + rest);
   float sn, cn;
   sincospif(f, &sn, &cn);
   *s = sn * t.magnitude;
