@@ -39,6 +39,7 @@
 // inside the walk.  16 sequences of 16K to 64K tokens, 256 x 6: 530 MB in 90 us, 5.9
 // TB/s; a launch costs about 6 us beyond its bytes.
 #include <algorithm>
+#include <cfloat>
 
 #include "decode_split.h"
 #include "kv_rows8.h"
@@ -315,8 +316,8 @@ void decode_i8(std::conditional_t<ITEM, ItemArgs, DecodeArgs> a) {
   const f32x2_t zs = hc < G ? zs_s[hc] : f32x2_t{0.f, 0.f};
 
   // the lane's head: running shift m (base 2, lazily raised: the weights stay
-  // below 2^8) and the sum of its slots' weights
-  float m = -1e30f, lsum = 0.0f;
+  // below 2^8; it begins below every finite logit) and the sum of its slots' weights
+  float m = -FLT_MAX, lsum = 0.0f;
   f32x4_t o[VB];
 #pragma unroll
   for (int vb = 0; vb < VB; ++vb) o[vb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -504,7 +505,7 @@ __global__ __launch_bounds__(256) void i8_merge(ItemArgs a) {
   const int row = threadIdx.x / LPR, c = threadIdx.x % LPR * 4;
   const size_t p0 = (size_t)(a.part_begin[rank] + si) * G + g;
   const size_t step = (size_t)a.part_seqs[rank] * G;   // the next split's partial
-  float M = -1e30f, L = 0.f;
+  float M = -FLT_MAX, L = 0.f;
   f32x4_t A = {0.f, 0.f, 0.f, 0.f};
   for (int j0 = row; j0 < ns; j0 += U * R) {
     f32x2_t ml[U];
