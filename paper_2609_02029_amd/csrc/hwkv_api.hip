@@ -1033,7 +1033,39 @@ int decode_impl(hwkv_cache *c, int32_t layer, const void *k_new,
     plan_workgroups(&tiles[i0], cnt, target, &nwg[i0]);
     for (int j = 0; j < cnt; ++j) total_splits += nwg[i0 + j];
   }
-  const size_t need = (size_t)total_splits * partial_bytes(p);
+  int32_t order[hwkv::kMaxItems];   // heads by capacity
+  for (int32_t h = 0; h < H; ++h) order[h] = h;
+  std::sort(order, order + H, [&](int32_t x, int32_t y) {
+    const int64_t cx = c->cap[layer * H + x], cy = c->cap[layer * H + y];
+    return cx != cy ? cx > cy : x < y;
+  });
+  ItemLaunch one;                   // (a batch of one launch: nothing from the heap)
+  std::vector<ItemLaunch> several(B > hwkv::kItemSeqs ? (B - 1) / hwkv::kItemSeqs + 1 : 0);
+  ItemLaunch *const launches = several.empty() ? &one : several.data();
+  const bool i8 = c->fmt == HWKV_KV_I8;
+  const bool by_item = decode_by_item(c, layer, tiles, order, fused, total_splits, launches);
+  // int8 from head_dim 128 on splits into one workgroup per CU: its rings keep as
+  // much in flight as HBM takes (66 KB at 256), and half the partials are written
+  // and merged.  us a call with one / two: 256 x 6 at 112K 23.7 / 25.6, 32K tokens of
+  // 4 heads 20.6 / 22.0; 128 x 4, 8 heads, 8,000 tokens 11.4 / 12.2, 120,000 46.4 /
+  // 46.9, 32,000 19.6 / 19.0; but 64 x 8 at 50,000 20.1 / 17.6.
+  if (i8 && !by_item && p.head_dim >= 128) {
+    total_splits = 0;
+    for (int i0 = 0; i0 < n_items_total; i0 += hwkv::kMaxItems) {
+      const int cnt = std::min(hwkv::kMaxItems, n_items_total - i0);
+      plan_workgroups(&tiles[i0], cnt, std::max<int64_t>(1, target / 2), &nwg[i0]);
+      for (int j = 0; j < cnt; ++j) total_splits += nwg[i0 + j];
+    }
+  }
+  // What the call asks for: the partials that it writes (int8; launches by item use
+  // the same memory in turn), or those of split workgroups (the other formats)
+  int64_t partials = total_splits;
+  if (i8 && by_item) {
+    partials = 0;
+    const int n_launches = (B - 1) / hwkv::kItemSeqs + 1;
+    for (int i = 0; i < n_launches; ++i) partials = std::max(partials, launches[i].parts);
+  }
+  const size_t need = (size_t)partials * partial_bytes(p);
   if (static_ws && need > ws_bytes)
     return fail(HWKV_EINVAL, "the call needs " + std::to_string(need) +
                                  " bytes of split partials, more than the " +
@@ -1048,35 +1080,13 @@ int decode_impl(hwkv_cache *c, int32_t layer, const void *k_new,
     const int rc = take_pages(c, layer, want, s);
     if (rc != HWKV_OK) return rc;
   }
-  int32_t order[hwkv::kMaxItems];   // heads by capacity
-  for (int32_t h = 0; h < H; ++h) order[h] = h;
-  std::sort(order, order + H, [&](int32_t x, int32_t y) {
-    const int64_t cx = c->cap[layer * H + x], cy = c->cap[layer * H + y];
-    return cx != cy ? cx > cy : x < y;
-  });
-  ItemLaunch one;                   // (a batch of one launch: nothing from the heap)
-  std::vector<ItemLaunch> several(B > hwkv::kItemSeqs ? (B - 1) / hwkv::kItemSeqs + 1 : 0);
-  ItemLaunch *const launches = several.empty() ? &one : several.data();
-  if (decode_by_item(c, layer, tiles, order, fused, total_splits, launches)) {
+  if (by_item) {
     const int rc = launch_items(c, layer, order, launches, k_new, v_new, q, scale, out,
                                 static_cast<float *>(ws), fused, s);
     if (rc != HWKV_OK) return rc;
     if (fused)
       for (int32_t b = 0; b < B; ++b) seq_len(c, layer, b) += 1;
     return ok();
-  }
-  // int8 from head_dim 128 on splits into one workgroup per CU: its rings keep as
-  // much in flight as HBM takes (66 KB at 256), and half the partials are written
-  // and merged.  us a call with one / two: 256 x 6 at 112K 23.7 / 25.6, 32K tokens of
-  // 4 heads 20.6 / 22.0; 128 x 4, 8 heads, 8,000 tokens 11.4 / 12.2, 120,000 46.4 /
-  // 46.9, 32,000 19.6 / 19.0; but 64 x 8 at 50,000 20.1 / 17.6.
-  if (c->fmt == HWKV_KV_I8 && p.head_dim >= 128) {
-    total_splits = 0;
-    for (int i0 = 0; i0 < n_items_total; i0 += hwkv::kMaxItems) {
-      const int cnt = std::min(hwkv::kMaxItems, n_items_total - i0);
-      plan_workgroups(&tiles[i0], cnt, std::max<int64_t>(1, target / 2), &nwg[i0]);
-      for (int j = 0; j < cnt; ++j) total_splits += nwg[i0 + j];
-    }
   }
   // launches of at most kMaxItems items
   int ws_split = 0;
