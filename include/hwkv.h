@@ -79,6 +79,10 @@ extern "C" {
  *                     to +-127, and counts code * 2^(e-133); e = 1 for a row of
  *                     zeros and subnormals.  A row that holds an infinity or a
  *                     NaN has e = 255 and codes 0, and all its values are NaN.
+ *                     (Decode takes value rows of magnitude 2^-98 to 2^108:
+ *                     below, the weights lose bits; above, long sums may
+ *                     overflow.  Prefill attention and the replay take them as
+ *                     they take bf16 values.)
  * The value an element contributes to attention is its stored value (times s
  * for fp8, with the row's scale for int8).  Every other format code is refused. */
 #define HWKV_KV_BF16 0
@@ -273,7 +277,8 @@ int hwkv_prefill_write(hwkv_cache *cache, int32_t layer, int32_t seq,
  *   k, v  device bf16 [n_tokens][n_kv_heads][head_dim], post-RoPE keys
  *   out   device fp32 [n_tokens][n_q_heads][head_dim] (pre-gate)
  * bf16 MFMA products with fp32 accumulation; the softmax weights enter the
- * value product rounded to bf16.  ESTATE if pos0 != n(layer, seq);
+ * value product rounded to bf16.  A row whose every q.k lies below -1e30 has no
+ * weights and reads NaN.  ESTATE if pos0 != n(layer, seq);
  * ECAPACITY if pos0 + n_tokens > max_ctx; EINVAL on bad indices, null
  * pointers, a non-finite or non-positive scale, or a cache whose format is
  * not bf16 (hwkv_prefill_attn_ws takes every format); n_tokens == 0 is a
@@ -414,7 +419,8 @@ int hwkv_rope_apply(const hwkv_rope *rope, int64_t n_tokens, int32_t n_q_heads,
  * rounded to bf16 and stored in the cache's format, its value stored, and its
  * query rotated into q_out for the hwkv_decode_attn that follows.  The results
  * are those of hwkv_rope_apply and hwkv_append, bit for bit, in one launch (one
- * for every 192 sequences and 32 KV heads).
+ * for every 192 sequences and 32 KV heads, and one that updates the page table
+ * where sequences take new pages).
  *   pos                  device int32 [n_axes][batch]: a sequence's positions
  *                        (which need not be its length)
  *   k_new, v_new         device bf16, n_kv_heads rows of head_dim per sequence,
@@ -453,8 +459,8 @@ int hwkv_decode_workspace_bytes(const hwkv_cache *cache, size_t *bytes);
  * component within a factor 2^14 of the head's largest |q|, the others to 2^-22 of
  * that; the products and their sums are exact), and the weights the value product as
  * three bf16 terms that carry each weight to 2^-27 of itself (with value rows of
- * magnitude 2^-98 to 2^108); for binary16, q enters q.k as binary16 after a power-of-two scaling
- * per query head, exact for every component within a factor 2^31 of the
+ * the magnitudes named at HWKV_KV_I8); for binary16, q enters q.k as binary16
+ * after a power-of-two scaling per query head, exact for every component within a factor 2^31 of the
  * head's largest |q| (the products are exact, the sums fp32). */
 int hwkv_decode_attn(hwkv_cache *cache, int32_t layer, const void *q,
                      float scale, void *out, void *ws, size_t ws_bytes,

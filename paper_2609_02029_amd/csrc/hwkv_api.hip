@@ -757,7 +757,8 @@ int64_t item_splits(const hwkv_cache *c, int32_t u, int32_t len, int64_t T) {
 // against the even share alone: 256 x 6, 40 sequences of 200-6,000 tokens, 4 KV heads
 // 33 / 39, 24 of 2,000-30,000 53 / 58, 256 x 8, 12 of 4,000 43 / 50.  Starting from as
 // many as can run instead: 128 x 4, 16 of 1,000-20,000, 8 KV heads 91 against 84, 128 x
-// 8, 24 of 100-12,000 80 against 72; 64 x 4, 32 of 12,000 73 against 76.
+// 8, 24 of 100-12,000 80 against 72; 64 x 4, 32 of 12,000 73 against 76.  (128 x 1, 100
+// ragged sequences, loses: 57 against 55 with the even share alone.)
 int64_t i8_tiles_per_wg(const hwkv_cache *c, int32_t layer, const int32_t *len, int32_t n, int64_t total,
                         int64_t longest, int64_t most_parts) {
   const int32_t H = c->pol.n_kv_heads, D = c->pol.head_dim;
@@ -1046,9 +1047,13 @@ int decode_impl(hwkv_cache *c, int32_t layer, const void *k_new,
   const bool by_item = decode_by_item(c, layer, tiles, order, fused, total_splits, launches);
   // int8 from head_dim 128 on splits into one workgroup per CU: its rings keep as
   // much in flight as HBM takes (66 KB at 256), and half the partials are written
-  // and merged.  us a call with one / two: 256 x 6 at 112K 23.7 / 25.6, 32K tokens of
-  // 4 heads 20.6 / 22.0; 128 x 4, 8 heads, 8,000 tokens 11.4 / 12.2, 120,000 46.4 /
-  // 46.9, 32,000 19.6 / 19.0; but 64 x 8 at 50,000 20.1 / 17.6.
+  // and merged.  us a layer with one / two, in a captured step of 16 layers, one
+  // sequence: 256 x 6, 4 KV heads, 8,000 tokens 12.1 / 15.1, 32,000 19.6 / 21.1,
+  // 114,688 44.8 / 45.5 (with windows of 2K, 8K and 32K 22.6 / 25.0); 128 x 4, 8 heads,
+  // 4,000 9.3 / 11.0, 16,000 13.4 / 13.6, 32,000 18.8 / 18.8, 64,000 28.8 / 28.5, 120,000
+  // 46.0 / 46.0; 128 x 1 at 32,000 19.0 / 18.8; but 64 x 8 at 50,000 19.7 / 17.5 (at 8,000
+  // 9.1 / 9.7).  A single layer over and over, whose rows may come from the last-level
+  // cache, has two ahead at 128 x 4 (32,000 22.9 / 22.0, 120,000 55 / 48), not at 256 x 6.
   if (i8 && !by_item && p.head_dim >= 128) {
     total_splits = 0;
     for (int i0 = 0; i0 < n_items_total; i0 += hwkv::kMaxItems) {

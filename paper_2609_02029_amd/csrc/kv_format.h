@@ -3,7 +3,8 @@
 // The paper's storage accounting carries the cache format p_KV through the
 // effective bytes per element b^K, b^V (Method, Eq. nominal-storage), and a
 // format that changes numerical execution is used by every consumer of the
-// cache.  Three formats are stored:
+// cache.  Three formats are encoded element by element here (int8, whose scales
+// belong to rows, in kv_rows8.h):
 //   bf16      the input format, stored as is (b = 2);
 //   f16       IEEE binary16, round to nearest even, overflow to infinity
 //             (b = 2);
@@ -16,7 +17,7 @@
 // The value of a stored element is its decoded value (times s for fp8).
 //
 // Every format stores 8 elements per chunk (16 bytes for the 16-bit formats,
-// 8 bytes for fp8), so the tile layout of hwkv_internal.h holds for all three
+// 8 bytes for fp8), so the tile layout of hwkv_internal.h holds for every one
 // with the chunk as its unit.
 #pragma once
 

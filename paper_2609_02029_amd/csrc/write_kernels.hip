@@ -103,24 +103,24 @@ __global__ __launch_bounds__(256) void prefill_write(WriteArgs a) {
         store_chunk<F>(kt + ((size_t)g * kTile + sl) * LB, k_codes[g * kTile + (sl ^ g)]);
     }
   } else {
-  // K: thread -> (chunk g, slot), slot fastest: coalesced tile stores
-  for (int e = threadIdx.x; e < kTile * NC; e += 256) {
-    const int sl = e & (kTile - 1), g = e >> 6;
-    const int64_t r = src_row[sl];
-    if (r < 0) continue;
-    const uint4 val =
-        *reinterpret_cast<const uint4 *>(a.k + r * row_stride + h * D + g * 8);
-    store_chunk<F>(kt + ((size_t)g * kTile + sl) * LB, encode8<F>(val, wh.k_scale));
-  }
-  // V: thread -> (slot, chunk g), chunk fastest: row-contiguous both sides
-  for (int e = threadIdx.x; e < kTile * NC; e += 256) {
-    const int sl = e / NC, g = e % NC;
-    const int64_t r = src_row[sl];
-    if (r < 0) continue;
-    const uint4 val =
-        *reinterpret_cast<const uint4 *>(a.v + r * row_stride + h * D + g * 8);
-    store_chunk<F>(vt + (size_t)sl * D * EB + g * LB, encode8<F>(val, wh.v_scale));
-  }
+    // K: thread -> (chunk g, slot), slot fastest: coalesced tile stores
+    for (int e = threadIdx.x; e < kTile * NC; e += 256) {
+      const int sl = e & (kTile - 1), g = e >> 6;
+      const int64_t r = src_row[sl];
+      if (r < 0) continue;
+      const uint4 val =
+          *reinterpret_cast<const uint4 *>(a.k + r * row_stride + h * D + g * 8);
+      store_chunk<F>(kt + ((size_t)g * kTile + sl) * LB, encode8<F>(val, wh.k_scale));
+    }
+    // V: thread -> (slot, chunk g), chunk fastest: row-contiguous both sides
+    for (int e = threadIdx.x; e < kTile * NC; e += 256) {
+      const int sl = e / NC, g = e % NC;
+      const int64_t r = src_row[sl];
+      if (r < 0) continue;
+      const uint4 val =
+          *reinterpret_cast<const uint4 *>(a.v + r * row_stride + h * D + g * 8);
+      store_chunk<F>(vt + (size_t)sl * D * EB + g * LB, encode8<F>(val, wh.v_scale));
+    }
   }
 }
 

@@ -645,7 +645,8 @@ def calib_replay(k, v, rows, q, windows, n_sinks, scale, outs, scores, means, ws
     order; ``outs``: fp32 [K + 1, R, Hq, D]; ``scores``: fp32 [K, R, Hq];
     ``means``: fp32 [K, Hkv]; ``ws``: device workspace tensor.  ``kv_format``
     "fp8": attend over the trace as an fp8 cache stores it, with per-KV-head
-    ``k_scale``, ``v_scale`` (host arrays or scalars; None = 1.0)."""
+    ``k_scale``, ``v_scale`` (host arrays or scalars; None = 1.0); "i8": as an
+    int8 cache does."""
     n_hist, hkv, d = k.shape
     R, hq, _ = q.shape
     w = _i64_array(windows)
