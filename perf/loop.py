@@ -19,6 +19,7 @@ and again CALLS calls against the clock.
 """
 import math
 import os
+import os
 import sys
 import time
 
