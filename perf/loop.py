@@ -19,7 +19,6 @@ and again CALLS calls against the clock.
 """
 import math
 import os
-import os
 import sys
 import time
 
