@@ -233,6 +233,40 @@ int hwkv_cache_pages(const hwkv_cache *cache, int64_t *total,
  * any cache; a released sequence is filled again from position 0. */
 int hwkv_cache_reset_seq(hwkv_cache *cache, int32_t seq);
 
+/* Reorder the sequences of a cache, in every layer: sequence b becomes what
+ * sequence parents[b] was before the call (beam search keeps some beams several
+ * times and drops others; parallel samples fork one prompt), or empty where
+ * parents[b] is -1.
+ *   parents   host int32 [batch], each in [-1, batch); read before the call
+ *             returns
+ * Finite units, and full units of a cache that is not paged, are copied to the
+ * sequence's own rows.  In a paged cache the sequences that come from one parent
+ * share its whole pages from then on (a page returns to the pool with the last
+ * sequence that holds it); the partly filled last page stays with one of them (the
+ * parent itself, if it is its own parent, else its first child), and the others get
+ * copies, in the page that a sequence without children leaves, or from the pool.
+ * Every other call takes a sequence that shares pages like any other: shared
+ * pages are full, and full pages are never written again.
+ * EINVAL on a bad parent, more than 65534 sequences, or a cycle (0 <- 1, 1 <- 2, ..,
+ * n <- 0) of more than 191 sequences; ENOMEM if the pool has too few pages. */
+int hwkv_cache_reorder(hwkv_cache *cache, const int32_t *parents, void *stream);
+
+/* Move a cache into another buffer, with a pool of another size (a pool that has
+ * run out, or one that may shrink): the rows that its sequences hold are copied,
+ * pages that several hold once, and the pages in use become the new pool's first
+ * ones, in the order (layer, KV head, sequence, position).
+ *   n_pages             the new pool; 0 for a cache that is not paged
+ *   dev_buf, buf_bytes  as in hwkv_cache_alloc_paged, and apart from the present
+ *                       buffer; NULL: the library allocates
+ * The cache uses the new buffer from then on.  A buffer of the caller's that it
+ * leaves must stay until the work on `stream` is done; one that the library owns
+ * is freed, for which the call waits for `stream` (not under stream capture).  A
+ * kernel of an earlier call must be done, or on `stream`.  ENOMEM if the sequences
+ * hold more than n_pages pages, or the buffer is too small; EINVAL if it is not
+ * 16-byte aligned or overlaps the present one. */
+int hwkv_cache_move(hwkv_cache *cache, int64_t n_pages, void *dev_buf,
+                    size_t buf_bytes, void *stream);
+
 /* Release the cache; frees device memory only if the library allocated it.
  * The caller must make sure no enqueued work still uses the cache. */
 int hwkv_cache_free(hwkv_cache *cache);
@@ -490,6 +524,47 @@ int hwkv_append_decode_attn_noalloc(hwkv_cache *cache, int32_t layer,
                                     const void *k_new, const void *v_new,
                                     const void *q, float scale, void *out,
                                     void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Beam selection: what hwkv_cache_reorder and the next append follow         */
+/* ------------------------------------------------------------------------ */
+
+/* Types of logits. */
+#define HWKV_LOGITS_BF16 0
+#define HWKV_LOGITS_F16 1
+#define HWKV_LOGITS_F32 2
+
+/* Device workspace bytes of hwkv_beam_select (EINVAL as there). */
+int hwkv_beam_workspace_bytes(int64_t n_groups, int32_t n_beams, int32_t vocab,
+                              int32_t type, int32_t n_out, size_t *bytes);
+
+/* The n_out best continuations of each group of n_beams beams.  With the logits x
+ * of row r = group * n_beams + beam and its running score s,
+ *   lse[r] = log sum_t e^x[r][t],  score(r, t) = s[r] + (x[r][t] - lse[r]):
+ * the n_out largest scores of the group's rows and tokens, falling; equal ones go
+ * to the lowest (r, t).  Sums and scores are formed in 64 bits (lse to 2e-12) and
+ * order by these; the outputs are rounded to fp32.
+ *   logits       device, n_groups * n_beams rows of vocab elements of `type`,
+ *                `stride` elements apart, aligned to their elements
+ *   scores       device fp32 [n_groups][n_beams]; -infinity: the beam has no
+ *                continuations (the first step's copies of one beam)
+ *   out_scores   device fp32 [n_groups][n_out]
+ *   out_parents  device int32 [n_groups][n_out]: r
+ *   out_tokens   device int32 [n_groups][n_out]: t
+ *   ws           device workspace, 16-byte aligned
+ * A logit of -infinity (a token that is not allowed) is no continuation, nor is
+ * any of a row that holds a NaN or +infinity, or whose score is not finite; where a
+ * group has fewer than n_out, the rest are -infinity, -1 and -1.  The result is
+ * the same from run to run.  1 <= n_beams, n_out <= 64, 1 <= vocab <= 2^24,
+ * n_groups * n_beams <= 2^20, vocab <= stride <= 2^31; n_groups == 0 is a no-op.
+ * EINVAL otherwise, on null or misaligned pointers, a short workspace, and outputs
+ * or a workspace that overlap another argument.  Two launches; nothing is
+ * allocated, so the call may be captured. */
+int hwkv_beam_select(int64_t n_groups, int32_t n_beams, int32_t vocab,
+                     const void *logits, int32_t type, int64_t stride,
+                     const float *scores, int32_t n_out, float *out_scores,
+                     int32_t *out_parents, int32_t *out_tokens, void *ws,
+                     size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------ */
 /* Calibration (Method, "Sequential Prefix-Conditioned Calibration";         */

@@ -54,6 +54,8 @@ struct hwkv_cache {
   std::vector<int32_t> pt_host;  // host copy of the page table
   std::vector<int32_t> held;     // pages held per (full unit, sequence)
   std::vector<int32_t> free_list;  // free pages (taken from the back)
+  std::vector<int32_t> refs;     // sequences that hold each page: a page of 256 rows
+                                 //   may be shared, a partly filled one never is
   uint8_t *base = nullptr;
   size_t bytes = 0;
   bool owned = false;
@@ -223,6 +225,7 @@ int layout(const hwkv_policy &p, int32_t batch, int64_t max_ctx, int32_t fmt,
       c->full_index = fidx;
       c->pt_host.assign((size_t)n_full * batch * max_pages, -1);
       c->held.assign((size_t)n_full * batch, 0);
+      c->refs.assign((size_t)n_pages, 0);
       c->free_list.resize((size_t)n_pages);
       for (int64_t i = 0; i < n_pages; ++i)  // page 0 is taken first
         c->free_list[(size_t)i] = (int32_t)(n_pages - 1 - i);
@@ -400,6 +403,7 @@ int take_pages(hwkv_cache *c, int32_t layer,
         const int32_t pg = c->free_list.back();
         c->free_list.pop_back();
         c->pt_host[(size_t)pto + have] = pg;
+        c->refs[(size_t)pg] = 1;
         u.idx[u.n] = pto + have;
         u.page[u.n] = pg;
         if (++u.n == hwkv::kMaxPageUpdates) {
@@ -1442,7 +1446,8 @@ int hwkv_cache_reset_seq(hwkv_cache *c, int32_t seq) {
       if (pto < 0) continue;
       int32_t &have = c->held[(size_t)(pto / c->max_pages)];
       for (; have > 0; --have) {
-        c->free_list.push_back(c->pt_host[(size_t)pto + have - 1]);
+        const int32_t pg = c->pt_host[(size_t)pto + have - 1];
+        if (--c->refs[(size_t)pg] == 0) c->free_list.push_back(pg);
         c->pt_host[(size_t)pto + have - 1] = -1;
       }
     }
@@ -2617,6 +2622,539 @@ int hwkv_cache_read_scales(const hwkv_cache *c, int32_t layer, int32_t kv_head,
     host_v[j] = pairs[(size_t)(j * B + 1)];
   }
   return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// sequences reordered, caches moved
+// ---------------------------------------------------------------------------
+namespace {
+
+// Bytes of a K or V row, and of a row's scale pair.
+int32_t row_bytes(const hwkv_cache *c) { return c->pol.head_dim * c->elem; }
+
+int64_t pages_for(int64_t n) { return (n + hwkv::kPageTokens - 1) / hwkv::kPageTokens; }
+
+// The most rows of sequence b in any layer.
+int64_t most_rows(const hwkv_cache *c, int32_t b) {
+  int64_t n = 0;
+  for (int32_t l = 0; l < c->pol.n_layers; ++l) n = std::max(n, c->n[(size_t)l * c->batch + b]);
+  return n;
+}
+
+// Launches the moves over every unit that has a region.
+struct Move {
+  int32_t src, dst;
+  int64_t rows;
+};
+int launch_moves(const hwkv_cache *c, const Move *moves, size_t n, const uint8_t *from, uint8_t *to,
+                 hipStream_t s) {
+  if (n == 0) return HWKV_OK;
+  hwkv::MoveArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.from = from;
+  a.to = to;
+  a.row_bytes = row_bytes(c);
+  a.pair_bytes = (int32_t)row_scale_bytes(c->fmt);
+  a.n_moves = (int32_t)((n + hwkv::kMoveRound - 1) / hwkv::kMoveRound * hwkv::kMoveRound);
+  int64_t most = 0;
+  for (size_t i = 0; i < n; ++i) {
+    a.src[i] = (uint16_t)moves[i].src;
+    a.dst[i] = (uint16_t)moves[i].dst;
+    a.n[i] = (int32_t)moves[i].rows;
+    most = std::max(most, moves[i].rows);
+  }
+  a.most = (int32_t)most;
+  const int32_t U = (int32_t)c->cap.size();
+  for (int32_t u = 0; u < U;) {
+    int32_t k = 0;
+    int64_t begin = 0;
+    for (; u < U && k < hwkv::kMaxItems; ++u) {
+      if (c->k_off[u] < 0) continue;             // a paged unit
+      const int64_t wgs =
+          hwkv::move_workgroups(std::min(most, c->cap[u]), a.row_bytes, a.pair_bytes);
+      if (begin + wgs > INT32_MAX / 256) break;
+      a.unit[k].k_off = c->k_off[u] * c->elem;
+      a.unit[k].v_off = c->v_off[u] * c->elem;
+      a.unit[k].s_off = c->s_off[u];
+      a.unit[k].cap = (int32_t)c->cap[u];
+      a.unit[k].cap_pad = (int32_t)c->cap_pad[u];
+      a.wg_begin[k++] = (int32_t)begin;
+      begin += wgs;
+    }
+    a.wg_begin[k] = (int32_t)begin;
+    for (int32_t i = k + 1; i <= hwkv::kMaxItems; ++i) a.wg_begin[i] = INT32_MAX;
+    if (k == 0) continue;
+    const int rc = check_device(hwkv::launch_move_rows(a, s), "move launch");
+    if (rc != HWKV_OK) return rc;
+  }
+  return HWKV_OK;
+}
+
+// The moves parent[b] -> b of the sequences that change (and whose parent has
+// rows), in an order in which no source is overwritten before it has been read:
+// sequences without a child that is still to be written first, then the cycles
+// that are left.  Within a round all is read before anything is written, so a cycle
+// lies in one round, or starts one and goes through the carry.  EINVAL where a cycle
+// is longer than a launch.
+int plan_moves(const hwkv_cache *c, const int32_t *parent, std::vector<Move> *out) {
+  const int32_t B = c->batch;
+  std::vector<int32_t> waits(B, 0), ready;       // children of b still to be written
+  std::vector<char> todo(B, 0);
+  ready.reserve(B);
+  out->reserve(2 * (size_t)B + 4 * hwkv::kMoveRound);
+  for (int32_t b = 0; b < B; ++b)
+    if (parent[b] != b && parent[b] >= 0) {
+      todo[b] = 1;
+      ++waits[parent[b]];
+    }
+  for (int32_t b = 0; b < B; ++b)
+    if (todo[b] && waits[b] == 0) ready.push_back(b);
+  for (size_t i = 0; i < ready.size(); ++i) {
+    const int32_t b = ready[i], p = parent[b];
+    out->push_back({p, b, most_rows(c, p)});
+    todo[b] = 0;
+    if (--waits[p] == 0 && todo[p]) ready.push_back(p);
+  }
+  const auto end_round = [&]() {
+    while (out->size() % hwkv::kMoveRound != 0) out->push_back({0, 0, 0});
+  };
+  for (int32_t b = 0; b < B; ++b) {
+    if (!todo[b]) continue;
+    size_t len = 0;
+    for (int32_t x = b; len == 0 || x != b; x = parent[x]) ++len;
+    const size_t R = hwkv::kMoveRound;
+    const bool carried = len > R;
+    if (len + 1 > (size_t)hwkv::kMaxMoves)
+      return fail(HWKV_EINVAL, "a cycle of " + std::to_string(len) + " sequences (at most " +
+                                   std::to_string(hwkv::kMaxMoves - 1) + ")");
+    if (carried || out->size() % R + len > R) end_round();
+    // (a launch takes whole rounds, and a carry does not outlive it)
+    if (carried && out->size() % hwkv::kMaxMoves + len + 1 > (size_t)hwkv::kMaxMoves)
+      while (out->size() % hwkv::kMaxMoves != 0) out->push_back({0, 0, 0});
+    const int64_t first_rows = most_rows(c, b);
+    if (carried) out->push_back({b, hwkv::kMoveCarry, first_rows});
+    int32_t x = b;
+    do {
+      const int32_t p = parent[x];
+      out->push_back({carried && p == b ? (int32_t)hwkv::kMoveCarry : p, x, p == b ? first_rows : most_rows(c, p)});
+      todo[x] = 0;
+      x = p;
+    } while (x != b);
+    if (carried) end_round();
+  }
+  return HWKV_OK;
+}
+
+// The page table's part of a reorder.  A unit's chains share prefixes only, so two
+// chains that hold the same page at j are alike up to there, and the work is in
+// their ends.
+struct PageCopy {
+  int32_t src, dst, rows;        // dst -1: its page comes from the free list,
+  int32_t pto, j;                //   for entry j of the row at pto
+};
+struct PagePlan {
+  std::vector<int32_t> changed;  // sequences whose parent is another
+  std::vector<int32_t> heir;     // who keeps b's partly filled page: b itself, else its
+                                 //   first child; -1: b has none
+  std::vector<int32_t> common;   // [full unit][changed]: pages that child and parent share
+  std::vector<int32_t> old;      // a unit's new entries, by changed sequence
+  std::vector<int32_t> freed, orphans;
+  std::vector<PageCopy> copies;
+  std::vector<std::pair<int32_t, int32_t>> entries;   // (table index, page)
+};
+
+// The full units in order: f(unit index, layer, table offset of sequence 0).
+template <typename F>
+void each_full_unit(const hwkv_cache *c, F f) {
+  if (!c->paged) return;
+  for (size_t u = 0; u < c->cap.size(); ++u)
+    if (c->full_index[u] >= 0) f(c->full_index[u], (int32_t)u / c->pol.n_kv_heads, page_tab_off(c, (int32_t)u, 0));
+}
+
+// Reorders the page table (host copy, reference counts, free list); the copies and
+// the device's entries are left in *P.  A child shares its parent's whole pages; the
+// partly filled last one goes to the parent's heir, and every further child gets a
+// copy: in the page of a sequence without children, both in rising order, or in
+// one from the pool.  ENOMEM, with nothing changed, if that has too few.
+int reorder_pages(hwkv_cache *c, const int32_t *parent, PagePlan *P) {
+  const int32_t B = c->batch;
+  const int64_t PT = hwkv::kPageTokens;
+  const auto row = [&](int32_t pto0, int32_t b) { return &c->pt_host[(size_t)(pto0 + (int64_t)b * c->max_pages)]; };
+  const auto held = [&](int32_t fi, int32_t b) -> int32_t & { return c->held[(size_t)fi * B + b]; };
+  const auto len = [&](int32_t l, int32_t b) { return b < 0 ? 0 : c->n[(size_t)l * B + b]; };
+  P->heir.assign(B, -1);
+  for (int32_t b = B - 1; b >= 0; --b)
+    if (parent[b] >= 0) P->heir[parent[b]] = b;
+  for (int32_t b = 0; b < B; ++b) {
+    if (parent[b] == b) P->heir[b] = b;
+    else P->changed.push_back(b);
+  }
+  // what child and parent share already, and room for all that follows
+  size_t entries = 0, dropped = 0, most_old = 0, n_full = 0;
+  each_full_unit(c, [&](int32_t fi, int32_t l, int32_t pto0) {
+    size_t old = 0;
+    ++n_full;
+    for (int32_t b : P->changed) {
+      const int32_t p = parent[b], need = (int32_t)pages_for(len(l, p));
+      int32_t j = p < 0 ? 0 : std::min({held(fi, b), need, held(fi, p)});
+      while (j > 0 && row(pto0, b)[j - 1] != row(pto0, p)[j - 1]) --j;
+      P->common.push_back(j);
+      old += need - j;
+      dropped += held(fi, b) - j;
+    }
+    entries += old;
+    most_old = std::max(most_old, old);
+  });
+  P->old.reserve(most_old);
+  P->entries.reserve(entries);
+  P->freed.reserve(dropped);
+  P->orphans.reserve(P->changed.size());
+  P->copies.reserve(P->changed.size() * n_full);
+
+  // whole pages of b's new chain, and whether b gets a copy of its last page
+  const auto shared = [&](int32_t l, int32_t b) {
+    const int32_t p = parent[b];
+    return p >= 0 && P->heir[p] == b ? pages_for(len(l, p)) : len(l, p) / PT;
+  };
+  const auto copied = [&](int32_t l, int32_t b) { return shared(l, b) < pages_for(len(l, parent[b])); };
+  // b's own last page, where no one inherits it
+  const auto orphan = [&](int32_t fi, int32_t l, int32_t b) {
+    return P->heir[b] < 0 && len(l, b) % PT != 0 && held(fi, b) == pages_for(len(l, b));
+  };
+  int64_t wanted = 0, spare = 0;
+  size_t k0 = 0;
+  each_full_unit(c, [&](int32_t fi, int32_t l, int32_t pto0) {
+    const size_t n = P->changed.size();
+    for (size_t k = 0; k < n; ++k)
+      for (int64_t j = P->common[k0 + k]; j < shared(l, P->changed[k]); ++j)
+        ++c->refs[(size_t)row(pto0, parent[P->changed[k]])[j]];
+    int64_t copies = 0, orphans = 0;
+    for (size_t k = 0; k < n; ++k) {
+      const int32_t b = P->changed[k];
+      copies += copied(l, b) ? 1 : 0;
+      orphans += orphan(fi, l, b) ? 1 : 0;
+      for (int32_t j = P->common[k0 + k]; j < held(fi, b); ++j) {
+        const int32_t pg = row(pto0, b)[j];
+        if (--c->refs[(size_t)pg] == 0 && !(orphan(fi, l, b) && j == held(fi, b) - 1)) P->freed.push_back(pg);
+      }
+    }
+    wanted += std::max<int64_t>(0, copies - orphans);
+    spare += std::max<int64_t>(0, orphans - copies);
+    k0 += n;
+  });
+  if (wanted > (int64_t)(c->free_list.size() + P->freed.size()) + spare) {
+    k0 = 0;
+    each_full_unit(c, [&](int32_t fi, int32_t l, int32_t pto0) {
+      for (size_t k = 0; k < P->changed.size(); ++k) {
+        const int32_t b = P->changed[k], j0 = P->common[k0 + k];
+        for (int64_t j = j0; j < shared(l, b); ++j) --c->refs[(size_t)row(pto0, parent[b])[j]];
+        for (int32_t j = j0; j < held(fi, b); ++j) ++c->refs[(size_t)row(pto0, b)[j]];
+      }
+      k0 += P->changed.size();
+    });
+    return fail(HWKV_ENOMEM, "page pool exhausted: " + std::to_string(wanted) + " pages needed, " +
+                                 std::to_string(c->free_list.size() + P->freed.size() + (size_t)spare) + " free");
+  }
+  // (nothing allocates from here on: the free list has room for the whole pool)
+  for (size_t i = P->freed.size(); i-- > 0;) c->free_list.push_back(P->freed[i]);
+  k0 = 0;
+  each_full_unit(c, [&](int32_t fi, int32_t l, int32_t pto0) {
+    const size_t n = P->changed.size();
+    P->old.clear();
+    P->orphans.clear();
+    for (size_t k = 0; k < n; ++k) {
+      const int32_t b = P->changed[k], p = parent[b];
+      for (int64_t j = P->common[k0 + k]; j < pages_for(len(l, p)); ++j) P->old.push_back(row(pto0, p)[j]);
+      if (orphan(fi, l, b)) P->orphans.push_back(row(pto0, b)[held(fi, b) - 1]);
+    }
+    size_t next_old = 0, next_orphan = 0;
+    for (size_t k = 0; k < n; ++k) {
+      const int32_t b = P->changed[k], p = parent[b], need = (int32_t)pages_for(len(l, p));
+      const int32_t pto = pto0 + (int32_t)(b * c->max_pages);
+      for (int32_t j = P->common[k0 + k]; j < need; ++j) {
+        int32_t pg = P->old[next_old++];
+        if (j >= shared(l, b)) {
+          PageCopy copy = {pg, -1, (int32_t)(len(l, p) % PT), pto, j};
+          if (next_orphan < P->orphans.size()) {
+            copy.dst = P->orphans[next_orphan++];
+            c->refs[(size_t)copy.dst] = 1;
+          }
+          P->copies.push_back(copy);
+          pg = copy.dst;
+        }
+        row(pto0, b)[j] = pg;
+        if (pg >= 0) P->entries.push_back({pto + j, pg});
+      }
+      for (int32_t j = need; j < held(fi, b); ++j) row(pto0, b)[j] = -1;
+    }
+    for (int32_t b : P->changed) held(fi, b) = (int32_t)pages_for(len(l, parent[b]));
+    for (; next_orphan < P->orphans.size(); ++next_orphan) c->free_list.push_back(P->orphans[next_orphan]);
+    k0 += n;
+  });
+  for (PageCopy &copy : P->copies) {
+    if (copy.dst >= 0) continue;
+    copy.dst = c->free_list.back();
+    c->free_list.pop_back();
+    c->refs[(size_t)copy.dst] = 1;
+    c->pt_host[(size_t)copy.pto + copy.j] = copy.dst;
+    P->entries.push_back({copy.pto + copy.j, copy.dst});
+  }
+  return HWKV_OK;
+}
+
+// Copies the pages and installs the entries of a reorder.
+int launch_page_copies(const hwkv_cache *c, const PagePlan &P, hipStream_t s) {
+  hwkv::PageCopyArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.pool = c->base + c->pool_off * c->elem;
+  a.table = device_page_table(c);
+  a.row_bytes = row_bytes(c);
+  a.pair_bytes = (int32_t)row_scale_bytes(c->fmt);
+  size_t i = 0, e = 0;
+  while (i < P.copies.size() || e < P.entries.size()) {
+    for (a.n_copies = 0; a.n_copies < hwkv::kMaxPageCopies && i < P.copies.size(); ++i, ++a.n_copies) {
+      a.src[a.n_copies] = P.copies[i].src;
+      a.dst[a.n_copies] = P.copies[i].dst;
+      a.rows[a.n_copies] = P.copies[i].rows;
+    }
+    for (a.n_entries = 0; a.n_entries < hwkv::kMaxEntries && e < P.entries.size(); ++e, ++a.n_entries) {
+      a.idx[a.n_entries] = P.entries[e].first;
+      a.page[a.n_entries] = P.entries[e].second;
+    }
+    const int rc = check_device(hwkv::launch_page_copy(a, s), "page copy launch");
+    if (rc != HWKV_OK) return rc;
+  }
+  return HWKV_OK;
+}
+
+int reorder_impl(hwkv_cache *c, const int32_t *parent, hipStream_t s) {
+  std::vector<Move> moves;
+  int rc = plan_moves(c, parent, &moves);
+  if (rc != HWKV_OK) return rc;
+  PagePlan P;
+  std::vector<int64_t> n(c->n);
+  rc = reorder_pages(c, parent, &P);
+  if (rc != HWKV_OK) return rc;
+  for (int32_t l = 0; l < c->pol.n_layers; ++l)
+    for (int32_t b = 0; b < c->batch; ++b)
+      c->n[(size_t)l * c->batch + b] = parent[b] < 0 ? 0 : n[(size_t)l * c->batch + parent[b]];
+  rc = launch_page_copies(c, P, s);
+  for (size_t i = 0; rc == HWKV_OK && i < moves.size(); i += hwkv::kMaxMoves)
+    rc = launch_moves(c, &moves[i], std::min<size_t>(hwkv::kMaxMoves, moves.size() - i), c->base, c->base, s);
+  return rc;
+}
+
+// The cache in another buffer, with a pool of n_pages pages.
+int move_impl(hwkv_cache *c, int64_t n_pages, void *dev_buf, size_t buf_bytes, hipStream_t s) {
+  const int32_t B = c->batch;
+  hwkv_cache to;                     // the layout there
+  size_t bytes = 0;
+  int rc = layout(c->pol, B, c->max_ctx, c->fmt, c->paged, n_pages, &bytes, &to);
+  if (rc != HWKV_OK) return rc;
+  // the pages in the order (unit, sequence, place), as runs of new ones and of
+  // ones that an earlier sequence has
+  std::vector<hwkv::PageRun> runs;
+  std::vector<int32_t> moved((size_t)c->n_pages, -1);
+  int32_t used = 0;
+  to.free_list.clear();
+  each_full_unit(c, [&](int32_t fi, int32_t l, int32_t pto0) {
+    for (int32_t b = 0; b < B; ++b) {
+      const int32_t pto = pto0 + (int32_t)(b * c->max_pages);
+      const int64_t n = c->n[(size_t)l * B + b];
+      const int32_t need = (int32_t)pages_for(n);
+      for (int32_t j = 0; j < need; ++j) {
+        int32_t &page = moved[(size_t)c->pt_host[(size_t)pto + j]];
+        const int32_t copy = page < 0 ? 1 : 0;
+        if (copy) page = used++;
+        if (j > 0 && runs.back().copy == copy && runs.back().dst0 + j - runs.back().j0 == page) {
+        } else {
+          runs.push_back({pto, j, page, 0, (int32_t)(n - (int64_t)j * hwkv::kPageTokens), copy});
+        }
+        runs.back().begin = j + 1 - runs.back().j0;    // (its length, until it is launched)
+        to.pt_host[(size_t)pto + j] = page;
+        if (page < n_pages) ++to.refs[(size_t)page];
+      }
+      to.held[(size_t)fi * B + b] = need;
+    }
+  });
+  if (used > n_pages)
+    return fail(HWKV_ENOMEM, "a pool of " + std::to_string(n_pages) + " pages for " + std::to_string(used) +
+                                 " pages in use");
+  for (int64_t i = n_pages - 1; c->paged && i >= used; --i) to.free_list.push_back((int32_t)i);
+  std::vector<Move> moves;
+  for (int32_t b = 0; b < B; ++b)
+    if (most_rows(c, b) > 0) moves.push_back({b, b, most_rows(c, b)});
+
+  const bool owned = dev_buf == nullptr;
+  if (!owned) {
+    if (buf_bytes < bytes)
+      return fail(HWKV_ENOMEM, "device buffer smaller than cache bytes (" + std::to_string(bytes) + ")");
+    if ((uintptr_t)dev_buf % 16 != 0) return fail(HWKV_EINVAL, "the buffer must be 16-byte aligned");
+    if (overlap({c->base, (int64_t)c->bytes}, {dev_buf, (int64_t)bytes}))
+      return fail(HWKV_EINVAL, "the buffer overlaps the cache's");
+  } else {
+    const hipError_t e = hipMalloc(&dev_buf, bytes ? bytes : 256);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      return fail(e == hipErrorOutOfMemory ? HWKV_ENOMEM : HWKV_EDEVICE,
+                  std::string("hipMalloc: ") + hipGetErrorString(e));
+    }
+  }
+  uint8_t *const base = static_cast<uint8_t *>(dev_buf);
+  hwkv::PageMoveArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.from_pool = c->base + c->pool_off * c->elem;
+  a.to_pool = base + to.pool_off * c->elem;
+  a.from_table = device_page_table(c);
+  a.to_table = reinterpret_cast<int32_t *>(base + to.table_off);
+  a.row_bytes = row_bytes(c);
+  a.pair_bytes = (int32_t)row_scale_bytes(c->fmt);
+  for (size_t i = 0; rc == HWKV_OK && i < runs.size();) {
+    int k = 0;
+    for (a.n_pages = 0; k < hwkv::kMaxRuns && i < runs.size() && a.n_pages < (1 << 19); ++i, ++k) {
+      const int32_t len = runs[i].begin;
+      a.run[k] = runs[i];
+      a.run[k].begin = a.n_pages;
+      a.n_pages += len;
+    }
+    for (; k < hwkv::kMaxRuns; ++k) a.run[k].begin = INT32_MAX;
+    rc = check_device(hwkv::launch_page_move(a, s), "page move launch");
+  }
+  for (size_t i = 0; rc == HWKV_OK && i < moves.size(); i += hwkv::kMaxMoves)
+    rc = launch_moves(c, &moves[i], std::min<size_t>(hwkv::kMaxMoves, moves.size() - i), c->base, base, s);
+  if (rc == HWKV_OK && c->owned) {
+    rc = check_device(hipStreamSynchronize(s), "hipStreamSynchronize");
+    if (rc == HWKV_OK) rc = check_device(hipFree(c->base), "hipFree");
+  }
+  if (rc != HWKV_OK) {
+    if (owned) {                     // (work that writes there may be under way)
+      (void)hipStreamSynchronize(s);
+      (void)hipFree(base);
+    }
+    return rc;
+  }
+  c->base = base;
+  c->bytes = bytes;
+  c->owned = owned;
+  if (c->paged) {
+    c->n_pages = n_pages;
+    c->table_off = to.table_off;
+    c->pt_host.swap(to.pt_host);
+    c->held.swap(to.held);
+    c->refs.swap(to.refs);
+    c->free_list.swap(to.free_list);
+  }
+  return HWKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hwkv_cache_reorder(hwkv_cache *c, const int32_t *parents, void *stream) {
+  if (!c || !parents) return fail(HWKV_EINVAL, "cache and parents must be non-null");
+  if (c->batch >= (int32_t)hwkv::kMoveCarry) return fail(HWKV_EINVAL, "more than 65534 sequences");
+  bool same = true;
+  for (int32_t b = 0; b < c->batch; ++b) {
+    if (parents[b] < -1 || parents[b] >= c->batch)
+      return fail(HWKV_EINVAL, "parents must be sequences, or -1");
+    same = same && parents[b] == b;
+  }
+  if (same) return ok();
+  try {
+    const int rc = reorder_impl(c, parents, (hipStream_t)stream);
+    return rc == HWKV_OK ? ok() : rc;
+  } catch (const std::bad_alloc &) {
+    return fail(HWKV_ENOMEM, "host allocation failed");
+  }
+}
+
+int hwkv_cache_move(hwkv_cache *c, int64_t n_pages, void *dev_buf, size_t buf_bytes, void *stream) {
+  if (!c) return fail(HWKV_EINVAL, "cache is null");
+  if (!c->paged && n_pages != 0) return fail(HWKV_EINVAL, "n_pages must be 0 for a cache that is not paged");
+  try {
+    const int rc = move_impl(c, n_pages, dev_buf, buf_bytes, (hipStream_t)stream);
+    return rc == HWKV_OK ? ok() : rc;
+  } catch (const std::bad_alloc &) {
+    return fail(HWKV_ENOMEM, "host allocation failed");
+  }
+}
+
+// ---------------------------------------------------------------------------
+// beam selection
+// ---------------------------------------------------------------------------
+namespace {
+
+// Checks a selection's sizes; its workspace: the sums' parts, then the blocks' maxima.
+int beam_layout(int64_t n_groups, int32_t n_beams, int32_t vocab, int32_t type, int32_t n_out, hwkv::BeamArgs *a,
+                size_t *part_bytes, size_t *bytes) {
+  if (type != HWKV_LOGITS_BF16 && type != HWKV_LOGITS_F16 && type != HWKV_LOGITS_F32)
+    return fail(HWKV_EINVAL, "unknown type of logits");
+  if (n_beams < 1 || n_beams > hwkv::kMaxBeams) return fail(HWKV_EINVAL, "n_beams must be in [1, 64]");
+  if (n_out < 1 || n_out > hwkv::kMaxSelected) return fail(HWKV_EINVAL, "n_out must be in [1, 64]");
+  if (vocab < 1 || vocab > (1 << 24)) return fail(HWKV_EINVAL, "vocab must be in [1, 2^24]");
+  if (n_groups < 0 || n_groups > (1 << 20) / n_beams)
+    return fail(HWKV_EINVAL, "n_groups must be >= 0, and n_groups * n_beams at most 2^20");
+  const int64_t rows = n_groups * n_beams;
+  a->n_beams = n_beams;
+  a->n_out = n_out;
+  a->vocab = vocab;
+  a->n_blocks = hwkv::beam_blocks(type, vocab);
+  a->n_splits = hwkv::beam_splits(std::max<int64_t>(1, rows), a->n_blocks);
+  *part_bytes = (size_t)rows * a->n_splits * 16;
+  *bytes = *part_bytes + (size_t)rows * a->n_blocks * 4;
+  return HWKV_OK;
+}
+
+}  // namespace
+
+int hwkv_beam_workspace_bytes(int64_t n_groups, int32_t n_beams, int32_t vocab, int32_t type, int32_t n_out,
+                              size_t *bytes) {
+  if (!bytes) return fail(HWKV_EINVAL, "bytes is null");
+  hwkv::BeamArgs a;
+  size_t part = 0;
+  const int rc = beam_layout(n_groups, n_beams, vocab, type, n_out, &a, &part, bytes);
+  return rc == HWKV_OK ? ok() : rc;
+}
+
+int hwkv_beam_select(int64_t n_groups, int32_t n_beams, int32_t vocab, const void *logits, int32_t type,
+                     int64_t stride, const float *scores, int32_t n_out, float *out_scores, int32_t *out_parents,
+                     int32_t *out_tokens, void *ws, size_t ws_bytes, void *stream) {
+  hwkv::BeamArgs a;
+  std::memset(&a, 0, sizeof a);
+  size_t part = 0, need = 0;
+  const int rc = beam_layout(n_groups, n_beams, vocab, type, n_out, &a, &part, &need);
+  if (rc != HWKV_OK) return rc;
+  if (n_groups == 0) return ok();
+  if (!logits || !scores || !out_scores || !out_parents || !out_tokens)
+    return fail(HWKV_EINVAL, "logits, scores and the outputs must be non-null");
+  const int64_t elem = type == HWKV_LOGITS_F32 ? 4 : 2, rows = n_groups * n_beams, outs = n_groups * n_out;
+  if ((uintptr_t)logits % elem != 0 || (uintptr_t)scores % 4 != 0 || (uintptr_t)out_scores % 4 != 0 ||
+      (uintptr_t)out_parents % 4 != 0 || (uintptr_t)out_tokens % 4 != 0)
+    return fail(HWKV_EINVAL, "logits, scores and the outputs must be aligned to their elements");
+  if (stride < vocab || stride > ((int64_t)1 << 31))
+    return fail(HWKV_EINVAL, "stride must be at least vocab, and at most 2^31");
+  if (!ws || ws_bytes < need || (uintptr_t)ws % 16 != 0)
+    return fail(HWKV_EINVAL, "workspace missing, not 16-byte aligned or too small (need " + std::to_string(need) +
+                                 " bytes)");
+  const RowSpan spans[] = {{out_scores, outs * 4}, {out_parents, outs * 4}, {out_tokens, outs * 4},
+                           {ws, (int64_t)need}, {logits, ((rows - 1) * stride + vocab) * elem}, {scores, rows * 4}};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 6; ++j)
+      if (overlap(spans[i], spans[j]))
+        return fail(HWKV_EINVAL, "an output or the workspace overlaps another argument");
+  a.logits = logits;
+  a.stride = stride;
+  a.scores = scores;
+  a.part = static_cast<double *>(ws);
+  a.block_max = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + part);
+  a.out_scores = out_scores;
+  a.out_parents = out_parents;
+  a.out_tokens = out_tokens;
+  const int e = check_device(hwkv::launch_beam_select(type, a, n_groups, (hipStream_t)stream), "beam launch");
+  return e == HWKV_OK ? ok() : e;
 }
 
 }  // extern "C"

@@ -241,6 +241,84 @@ struct PageUpdateArgs {
   int32_t page[kMaxPageUpdates];
 };
 
+// Rows of whole sequences copied within a cache, or from one buffer into another of
+// the same layout (reorder_kernels.hip): moves src -> dst in rounds of kMoveRound,
+// each reading all its sources before it writes.  A cycle longer than a round keeps
+// its first sequence's rows in registers (dst kMoveCarry) until its last move (src
+// kMoveCarry).  Every unit with a region: workgroups [wg_begin, that of the next
+// unit) take kMoveChunks x 256 chunks of 16 bytes each, of K, then V, then scale
+// pairs.
+constexpr int kMaxMoves = 192, kMoveRound = 8, kMoveChunks = 2;
+constexpr uint16_t kMoveCarry = 0xffff;
+struct MoveUnit {
+  int64_t k_off, v_off, s_off;   // byte offsets of sequence 0
+  int32_t cap, cap_pad;          // rows holding data; rows allocated
+};
+struct MoveArgs {
+  MoveUnit unit[kMaxItems];
+  int32_t wg_begin[kMaxItems + 1];   // INT32_MAX past the last
+  int32_t n[kMaxMoves];          // rows of src below its capacity (0: no move)
+  uint16_t src[kMaxMoves], dst[kMaxMoves];
+  const uint8_t *from;           // cache bases
+  uint8_t *to;
+  int32_t n_moves, most;         // moves, whole rounds; the most rows of any
+  int32_t row_bytes, pair_bytes; // of a K or V row, and of a row's scale pair (0: none)
+};
+hipError_t launch_move_rows(const MoveArgs &a, hipStream_t s);
+// Workgroups of a unit for `rows` rows.
+int64_t move_workgroups(int64_t rows, int32_t row_bytes, int32_t pair_bytes);
+
+// Pages copied within a pool, and page-table entries installed.
+constexpr int kMaxPageCopies = 120, kMaxEntries = 240;
+struct PageCopyArgs {
+  int32_t src[kMaxPageCopies], dst[kMaxPageCopies];
+  int32_t rows[kMaxPageCopies];  // that src holds
+  int32_t idx[kMaxEntries], page[kMaxEntries];
+  int32_t n_copies, n_entries;
+  uint8_t *pool;
+  int32_t *table;
+  int32_t row_bytes, pair_bytes;
+};
+hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t s);
+
+// Pages that go from one pool into another: runs of consecutive pages of a
+// (unit, sequence), whose j-th goes to page dst0 + j - j0 of the new pool; where
+// `copy` is 0 it is there already, and only the table gets its entry.
+constexpr int kMaxRuns = 128;
+struct PageRun {
+  int32_t pto;                   // page-table offset of the row, in both tables
+  int32_t j0, dst0;
+  int32_t begin;                 // pages of the launch's runs before it
+  int32_t rows;                  // of the row from page j0 on
+  int32_t copy;
+};
+struct PageMoveArgs {
+  PageRun run[kMaxRuns];         // begin INT32_MAX past the last
+  const uint8_t *from_pool;
+  uint8_t *to_pool;
+  const int32_t *from_table;
+  int32_t *to_table;
+  int32_t n_pages, row_bytes, pair_bytes;
+};
+hipError_t launch_page_move(const PageMoveArgs &a, hipStream_t s);
+
+// Beam search's selection (beam_kernels.hip).
+constexpr int kMaxBeams = 64, kMaxSelected = 64;
+constexpr int kScanTarget = 2048;  // workgroups that the scan of all rows aims at
+struct BeamArgs {
+  const void *logits;            // rows stride elements apart
+  int64_t stride;
+  const float *scores;           // [rows]
+  double *part;                  // [rows][n_splits][2]: sums, and their powers of two
+  float *block_max;              // [rows][n_blocks]
+  float *out_scores;             // [groups][n_out]
+  int32_t *out_parents, *out_tokens;
+  int32_t vocab, n_beams, n_out, n_blocks, n_splits;
+};
+int32_t beam_blocks(int32_t type, int32_t vocab);
+int32_t beam_splits(int64_t n_rows, int32_t n_blocks);
+hipError_t launch_beam_select(int32_t type, const BeamArgs &a, int64_t n_groups, hipStream_t s);
+
 // Prefill attention of one chunk [p0, p0 + n_tokens) of one sequence: per
 // kv head the (unit, sequence) region offsets and canonical window; the
 // kernel's workgroups visit heads in order (most keys first) and each
@@ -465,6 +543,9 @@ static_assert(sizeof(hwkv::AppendArgs) <= 4096, "append kernarg too large");
 static_assert(sizeof(hwkv::RopeArgs) <= 4096, "rope kernarg too large");
 static_assert(sizeof(hwkv::AppendRopeArgs) <= 4096, "append rope kernarg too large");
 static_assert(sizeof(hwkv::PageUpdateArgs) <= 4096, "page update kernarg too large");
+static_assert(sizeof(hwkv::MoveArgs) <= 4096, "move kernarg too large");
+static_assert(sizeof(hwkv::PageCopyArgs) <= 4096, "page copy kernarg too large");
+static_assert(sizeof(hwkv::PageMoveArgs) <= 4096, "page move kernarg too large");
 static_assert(sizeof(hwkv::StageArgs) <= 4096, "stage kernarg too large");
 static_assert(sizeof(hwkv::StageChunkArgs) <= 4096, "stage chunk kernarg too large");
 static_assert(sizeof(hwkv::StageRowsArgs) <= 4096, "stage rows kernarg too large");

@@ -1,0 +1,168 @@
+// reorder_kernels.hip -- rows and pages of whole sequences copied (gfx950): a
+// cache's sequences reordered in place, or a cache taken into another buffer.
+//
+// Nothing is computed: 16-byte chunks are read and written as they lie, so one
+// kernel serves every format and head_dim.  What bounds it: HBM where there is much
+// to copy, the launch where there is little.
+#include <algorithm>
+
+#include "hwkv_internal.h"
+
+namespace hwkv {
+namespace {
+
+typedef uint32_t chunk_t __attribute__((ext_vector_type(4)));
+
+constexpr int64_t kWgChunks = (int64_t)kMoveChunks * 256;
+constexpr int kPageParts = 8;        // workgroups that copy a page
+
+__host__ __device__ constexpr int64_t whole_tiles(int64_t rows) {
+  return (rows + kTile - 1) / kTile * kTile;
+}
+// Chunks of 16 bytes of `rows` rows of K (whole tiles), V and the scale pairs.
+__host__ __device__ constexpr int64_t part_chunks(int part, int64_t rows, int row_bytes, int pair_bytes) {
+  return part == 0 ? whole_tiles(rows) * row_bytes / 16
+                   : part == 1 ? rows * row_bytes / 16 : (rows * pair_bytes + 15) / 16;
+}
+
+// Every thread holds its chunks of all sequences, so that a permutation in place
+// needs no order between threads: a chunk's sources are read before any of its
+// destinations is written, within a round by the registers, from round to round by
+// the order of the moves (host).
+__global__ __launch_bounds__(256) void move_rows(MoveArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int u = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.wg_begin[lane] <= (int)blockIdx.x)) - 1);
+  const MoveUnit &unit = a.unit[u];
+  // the part (K, V, pairs) of this workgroup, by the most rows any move has
+  int64_t wg = (int)blockIdx.x - a.wg_begin[u];
+  int part = 0;
+  for (; part < 2; ++part) {
+    const int64_t wgs =
+        (part_chunks(part, min(a.most, unit.cap), a.row_bytes, a.pair_bytes) + kWgChunks - 1) / kWgChunks;
+    if (wg < wgs) break;
+    wg -= wgs;
+  }
+  const int64_t at = part == 0 ? unit.k_off : part == 1 ? unit.v_off : unit.s_off;
+  const int64_t stride = (int64_t)unit.cap_pad * (part == 2 ? a.pair_bytes : a.row_bytes);
+  const int64_t c0 = wg * kWgChunks + threadIdx.x;
+  chunk_t carry[kMoveChunks] = {};
+  for (int r = 0; r < a.n_moves; r += kMoveRound) {
+    chunk_t x[kMoveRound][kMoveChunks];
+    bool has[kMoveRound][kMoveChunks];
+#pragma unroll
+    for (int i = 0; i < kMoveRound; ++i) {
+      const int src = a.src[r + i];
+      const int64_t n = part_chunks(part, min(a.n[r + i], unit.cap), a.row_bytes, a.pair_bytes);
+      const chunk_t *const from = reinterpret_cast<const chunk_t *>(a.from + at + src * stride);
+#pragma unroll
+      for (int j = 0; j < kMoveChunks; ++j) {
+        has[i][j] = c0 + j * 256 < n;
+        if (src == kMoveCarry)
+          x[i][j] = carry[j];
+        else if (has[i][j])
+          x[i][j] = from[c0 + j * 256];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kMoveRound; ++i) {
+      const int dst = a.dst[r + i];
+      chunk_t *const to = reinterpret_cast<chunk_t *>(a.to + at + dst * stride);
+#pragma unroll
+      for (int j = 0; j < kMoveChunks; ++j) {
+        if (!has[i][j]) continue;
+        if (dst == kMoveCarry)
+          carry[j] = x[i][j];
+        else
+          to[c0 + j * 256] = x[i][j];
+      }
+    }
+  }
+}
+
+// Part `part` of kPageParts of a page's first `rows` rows.
+__device__ __forceinline__ void copy_page(const uint8_t *from, uint8_t *to, int part, int rows, int row_bytes,
+                                          int pair_bytes) {
+  const int k = (int)part_chunks(0, rows, row_bytes, pair_bytes);
+  const int v = (int)part_chunks(1, rows, row_bytes, pair_bytes);
+  const int all = k + v + (int)part_chunks(2, rows, row_bytes, pair_bytes);
+  const int v_at = kPageTokens * row_bytes / 16, s_at = 2 * v_at;
+  const chunk_t *const src = reinterpret_cast<const chunk_t *>(from);
+  chunk_t *const dst = reinterpret_cast<chunk_t *>(to);
+  constexpr int step = kPageParts * 256;
+  for (int c = part * 256 + (int)threadIdx.x; c < all; c += 4 * step) {
+    chunk_t x[4];
+    int at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int ci = c + i * step;
+      at[i] = ci < k ? ci : ci < k + v ? v_at + ci - k : s_at + ci - k - v;
+      if (ci < all) x[i] = src[at[i]];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i * step < all) dst[at[i]] = x[i];
+  }
+}
+
+__host__ __device__ constexpr int64_t page_bytes(int row_bytes, int pair_bytes) {
+  return (int64_t)kPageTokens * (2 * row_bytes + pair_bytes);
+}
+
+// Grid: kPageParts workgroups a copy, and one that installs the entries.
+__global__ __launch_bounds__(256) void page_copy(PageCopyArgs a) {
+  const int i = blockIdx.x / kPageParts;
+  if (i == a.n_copies) {
+    for (int e = threadIdx.x; e < a.n_entries; e += 256) a.table[a.idx[e]] = a.page[e];
+    return;
+  }
+  const int64_t page = page_bytes(a.row_bytes, a.pair_bytes);
+  copy_page(a.pool + a.src[i] * page, a.pool + a.dst[i] * page, blockIdx.x % kPageParts, a.rows[i], a.row_bytes,
+            a.pair_bytes);
+}
+
+// Grid: kPageParts workgroups a page.
+__global__ __launch_bounds__(256) void page_move(PageMoveArgs a) {
+  const int lane = threadIdx.x & 63, p = blockIdx.x / kPageParts, part = blockIdx.x % kPageParts;
+  int run = -1;
+  for (int i = 0; i < kMaxRuns; i += 64) run += __popcll(__ballot(a.run[i + lane].begin <= p));
+  const PageRun r = a.run[__builtin_amdgcn_readfirstlane(run)];
+  const int j = p - r.begin, dst = r.dst0 + j;
+  const int src = a.from_table[r.pto + r.j0 + j];
+  if (part == 0 && threadIdx.x == 0) a.to_table[r.pto + r.j0 + j] = dst;
+  if (!r.copy) return;
+  const int64_t page = page_bytes(a.row_bytes, a.pair_bytes);
+  copy_page(a.from_pool + src * page, a.to_pool + dst * page, part, min(kPageTokens, r.rows - j * kPageTokens),
+            a.row_bytes, a.pair_bytes);
+}
+
+}  // namespace
+
+int64_t move_workgroups(int64_t rows, int32_t row_bytes, int32_t pair_bytes) {
+  int64_t n = 0;
+  for (int part = 0; part < 3; ++part)
+    n += (part_chunks(part, rows, row_bytes, pair_bytes) + kWgChunks - 1) / kWgChunks;
+  return n;
+}
+
+hipError_t launch_move_rows(const MoveArgs &a, hipStream_t s) {
+  int n = 0;
+  while (n < kMaxItems && a.wg_begin[n + 1] != INT32_MAX) ++n;
+  if (a.wg_begin[n] == 0) return hipSuccess;
+  hipLaunchKernelGGL(move_rows, dim3((unsigned)a.wg_begin[n]), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t s) {
+  const int wgs = a.n_copies * kPageParts + (a.n_entries > 0 ? 1 : 0);
+  if (wgs == 0) return hipSuccess;
+  hipLaunchKernelGGL(page_copy, dim3((unsigned)wgs), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_move(const PageMoveArgs &a, hipStream_t s) {
+  if (a.n_pages == 0) return hipSuccess;
+  hipLaunchKernelGGL(page_move, dim3((unsigned)(a.n_pages * kPageParts)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace hwkv

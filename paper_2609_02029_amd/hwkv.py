@@ -53,6 +53,11 @@ SYMBOLS = {
                                ctypes.c_int),
     "hwkv_cache_pages": ([_vp, _P(_i64), _P(_i64)], ctypes.c_int),
     "hwkv_cache_reset_seq": ([_vp, _i32], ctypes.c_int),
+    "hwkv_cache_reorder": ([_vp, _P(_i32), _vp], ctypes.c_int),
+    "hwkv_cache_move": ([_vp, _i64, _vp, _sz, _vp], ctypes.c_int),
+    "hwkv_beam_workspace_bytes": ([_i64, _i32, _i32, _i32, _i32, _P(_sz)], ctypes.c_int),
+    "hwkv_beam_select": ([_i64, _i32, _i32, _vp, _i32, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp],
+                         ctypes.c_int),
     "hwkv_cache_bytes": ([_vp, _i32, _i64, _P(_sz)], ctypes.c_int),
     "hwkv_cache_alloc": ([_P(_vp), _vp, _i32, _i64, _vp, _sz], ctypes.c_int),
     "hwkv_cache_free": ([_vp], ctypes.c_int),
@@ -281,6 +286,26 @@ def cache_pages(cache):
 
 def cache_reset_seq(cache, seq):
     _check(_lib.hwkv_cache_reset_seq(cache.handle, seq))
+
+
+def cache_reorder(cache, parents, stream=None):
+    """Sequence b becomes what sequence ``parents[b]`` was (-1: empty), in every
+    layer.  ``parents``: ``batch`` ints in host memory (a list, a CPU tensor)."""
+    p = [int(x) for x in (parents.tolist() if hasattr(parents, "tolist") else parents)]
+    if len(p) != cache.batch:
+        raise ValueError("parents must hold one entry per sequence")
+    _check(_lib.hwkv_cache_reorder(cache.handle, (_i32 * len(p))(*p), _stream(stream)))
+
+
+def cache_move(cache, n_pages=None, dev_buf=None, stream=None):
+    """Moves the cache into ``dev_buf`` (uint8 device tensor, kept alive; None: the
+    library allocates), with a pool of ``n_pages`` pages (None: not a paged
+    cache).  The buffer that it leaves must live until the stream's work is done."""
+    _on_current_device(dev_buf)
+    ptr = _dev(dev_buf, "uint8", "dev_buf")
+    _check(_lib.hwkv_cache_move(cache.handle, 0 if n_pages is None else n_pages, ptr,
+                                0 if dev_buf is None else dev_buf.numel(), _stream(stream)))
+    cache.dev_buf = dev_buf
 
 
 def cache_format(cache):
@@ -613,6 +638,51 @@ def decode_timing_read(cache):
     _check(_lib.hwkv_decode_timing_read(cache.handle, ctypes.byref(sp), ctypes.byref(mg),
                                         ctypes.byref(n)))
     return sp.value, mg.value, n.value
+
+
+# ---------------------------------------------------------------------------
+# beam selection
+# ---------------------------------------------------------------------------
+LOGITS_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _logits(t):
+    """(groups, beams, vocab, address, type, elements between rows) of logits
+    [groups, beams, vocab] whose rows are contiguous and evenly apart."""
+    if not t.is_cuda or t.dtype not in LOGITS_TYPES:
+        raise ValueError("logits must be a bfloat16, float16 or float32 device tensor")
+    if t.dim() != 3:
+        raise ValueError("logits must be [groups, beams, vocab]")
+    (g, b, v), (sg, sb, sv) = t.shape, t.stride()
+    stride = sb if b > 1 else sg if g > 1 else v
+    if (v > 1 and sv != 1) or (b > 1 and g > 1 and sg != b * sb):
+        raise ValueError("logits: rows must be contiguous and evenly apart")
+    return g, b, v, t.data_ptr(), LOGITS_TYPES[t.dtype], stride
+
+
+def beam_workspace_bytes(logits, n_out):
+    g, b, v, _, code, _ = _logits(logits)
+    r = _sz()
+    _check(_lib.hwkv_beam_workspace_bytes(g, b, v, code, n_out, ctypes.byref(r)))
+    return r.value
+
+
+def beam_select(logits, scores, out_scores, parents, tokens, ws, stream=None):
+    """The best continuations of each group: ``logits`` [groups, beams, vocab]
+    (bf16, f16 or fp32; rows any distance apart), ``scores`` fp32 [groups, beams];
+    ``out_scores`` fp32, ``parents`` (rows: group * beams + beam) and ``tokens`` int32
+    [groups, n_out].  ``ws``: uint8, see beam_workspace_bytes."""
+    _on_current_device(logits, scores, out_scores, parents, tokens, ws)
+    g, b, v, ptr, code, stride = _logits(logits)
+    if tuple(scores.shape) != (g, b):
+        raise ValueError("scores must be [groups, beams]")
+    shape = tuple(out_scores.shape)
+    if len(shape) != 2 or shape[0] != g or tuple(parents.shape) != shape or tuple(tokens.shape) != shape:
+        raise ValueError("out_scores, parents and tokens must be [groups, n_out]")
+    _check(_lib.hwkv_beam_select(g, b, v, ptr, code, stride, _dev(scores, "float32", "scores"), shape[1],
+                                 _dev(out_scores, "float32", "out_scores"), _dev(parents, "int32", "parents"),
+                                 _dev(tokens, "int32", "tokens"), _dev(ws, "uint8", "ws"), ws.numel(),
+                                 _stream(stream)))
 
 
 def calib_workspace_bytes(n_q_heads, head_dim, n_sinks, n_hist, n_rows, n_kv_heads=None,

@@ -1,0 +1,366 @@
+"""GPU tests of sequences reordered and caches moved: what a cache holds after
+the call, row by row and in stored bits, against what it held before; the pages it
+takes against a count of its own; and a beam search that runs the calls together."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_02029_amd import hwkv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+PT = hwkv.PAGE_TOKENS
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+
+
+class Held:
+    """A cache and a count of the pages that its sequences should hold: every
+    chain a list of names, whole pages shared by a fork, a partly filled one not."""
+
+    def __init__(self, levels, lens, fmt="bf16", paged=True, D=64, G=1, S=4, book=(70, 0), max_ctx=1400, pages=None, seed=0,
+                 dev_buf=None):
+        self.L, self.H, self.D, self.B = len(levels), len(levels[0]), D, len(lens)
+        self.full = sum(book[k] == 0 for row in levels for k in row)
+        self.pol = hwkv.policy_set(self.L, self.H, self.H * G, D, S, list(book), levels)
+        self.pages = (pages if pages is not None else self.full * self.B * -(-max_ctx // PT)) if paged else None
+        kw = dict(k_scale=0.03, v_scale=0.02) if fmt == "fp8" else {}
+        self.fmt = fmt
+        self.cache = hwkv.cache_alloc(self.pol, self.B, max_ctx, kv_format=fmt, n_pages=self.pages, dev_buf=dev_buf, **kw)
+        self.gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.n, self.chains, self.names = list(lens), [], 0
+        for b, n in enumerate(lens):
+            self.chains.append([self.name() for _ in range(-(-n // PT))])
+            for layer in range(self.L):
+                if n:
+                    hwkv.prefill_write(self.cache, layer, b, 0, *self.rows(n))
+
+    def name(self):
+        self.names += 1
+        return self.names
+
+    def rows(self, n):
+        return [torch.randn((n, self.H, self.D), generator=self.gen, device=DEV).to(torch.bfloat16) for _ in range(2)]
+
+    def read(self):
+        """[layer][head][seq] -> (rows held, stored K and V rows, scale bytes)."""
+        got = {}
+        for layer in range(self.L):
+            for h in range(self.H):
+                for b in range(self.B):
+                    k, v, nv = hwkv.cache_read_unit(self.cache, layer, h, b)
+                    one = [k[:nv].copy(), v[:nv].copy()]
+                    if self.fmt == "i8":
+                        one += [x[:nv].copy() for x in hwkv.cache_read_scales(self.cache, layer, h, b)]
+                    got[layer, h, b] = one
+        return got
+
+    def reorder(self, parents, **kw):
+        hwkv.cache_reorder(self.cache, parents, **kw)
+        n, old = self.n, self.chains
+        self.n = [n[p] if p >= 0 else 0 for p in parents]
+        heir = {p: p if parents[p] == p else parents.index(p) for p in parents if p >= 0}
+        self.chains = []
+        for b, p in enumerate(parents):
+            chain = [] if p < 0 else list(old[p])
+            if p >= 0 and n[p] % PT and heir[p] != b:
+                chain[-1] = self.name()
+            self.chains.append(chain)
+
+    def append(self):
+        for layer in range(self.L):
+            k, v = self.rows(self.B)
+            hwkv.append(self.cache, layer, k, v)
+        for b in range(self.B):
+            if self.n[b] % PT == 0:
+                self.chains[b].append(self.name())
+            self.n[b] += 1
+
+    def check_pages(self):
+        if self.pages is not None:
+            used = self.full * len({p for chain in self.chains for p in chain})
+            assert hwkv.cache_pages(self.cache) == (self.pages, self.pages - used)
+        for b in range(self.B):
+            assert all(hwkv.cache_seq_len(self.cache, layer, b) == self.n[b] for layer in range(self.L))
+
+
+def same(was, now, parents=None):
+    for (layer, h, b), rows in now.items():
+        p = b if parents is None else parents[b]
+        if p < 0:
+            assert len(rows[0]) == 0
+            continue
+        for x, y in zip(was[layer, h, p], rows):
+            assert np.array_equal(x, y), (layer, h, b, p)
+
+
+LEVELS = [[0, 1, 1], [1, 0, 1]]
+LENS = [300, 5, 513, 256, 1, 74, 73, 0, 700, 255, 257, 129]
+ORDERS = {
+    "fork": [0] * 12,
+    "swap": [1, 0, 3, 2, 5, 4, 7, 6, 9, 8, 11, 10],
+    "beams": [1, 1, 3, 2, 4, 4, 6, 4, 8, 11, 8, 9],
+    "cycles": [1, 2, 0, 4, 5, 6, 3, 8, 7, 10, 11, 9],
+    "one cycle": [1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 0],
+    "cycle and trees": [4, 0, 1, 2, 3, 0, 5, 6, 6, 7, 4, 3],
+    "dropped": [-1, 0, 2, -1, -1, 8, 8, 8, -1, 2, 3, 11],
+}
+
+
+@pytest.mark.parametrize("order", list(ORDERS))
+@pytest.mark.parametrize("paged", [True, False])
+def test_every_row_follows_its_parent(order, paged):
+    parents = ORDERS[order]
+    r = Held(LEVELS, LENS, paged=paged)
+    was = r.read()
+    r.reorder(parents)
+    same(was, r.read(), parents)
+    r.check_pages()
+    # tokens of their own: nobody writes into another's rows
+    was = r.read()
+    for _ in range(3):
+        r.append()
+    now = r.read()
+    for (layer, h, b), rows in now.items():
+        n, w = r.n[b], hwkv.cache_unit_info(r.cache, layer, h)[1]
+        if w == 0 or n <= 74:
+            assert np.array_equal(rows[0][:n - 3], was[layer, h, b][0])
+    r.check_pages()
+    r.reorder([11 - b for b in range(12)])
+    same(now, r.read(), [11 - b for b in range(12)])
+    r.check_pages()
+    for b in range(12):
+        hwkv.cache_reset_seq(r.cache, b)
+    if paged:
+        assert hwkv.cache_pages(r.cache) == (r.pages, r.pages)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f16", "fp8", "i8"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_formats_and_head_dims(fmt, D):
+    r = Held([[0, 1]], [300, 90, 20, 513], fmt=fmt, D=D, max_ctx=600)
+    for parents in ([1, 1, 3, 0], [3, 0, 1, 2], [0, 0, 0, 0]):
+        was = r.read()
+        r.reorder(parents)
+        same(was, r.read(), parents)
+        r.check_pages()
+
+
+def test_large_batches_and_long_cycles():
+    """More sequences than a launch's moves, cycles of up to 191, and one beyond."""
+    B = 420
+    rng = np.random.default_rng(1)
+    r = Held([[0]], [int(n) for n in rng.integers(1, 40, B)], book=(24, 0), paged=False, max_ctx=64)
+    shuffled = [int(x) for x in rng.permutation(B)]
+    for trial in range(5):
+        if trial == 0:
+            parents = list(range(1, 191)) + [0] + list(range(192, 380)) + [191] + [int(x) for x in rng.integers(0, 420, 40)]
+        elif trial == 1:
+            parents = [int(x) for x in rng.integers(-1, B, B)]
+        elif trial == 2:      # cycles of 9 to 12, in shuffled places
+            parents, at = list(range(B)), 0
+            for length in [9, 10, 11, 12] * 10:
+                ring = shuffled[at:at + length]
+                for x, y in zip(ring, ring[1:] + ring[:1]):
+                    parents[x] = y
+                at += length
+        elif trial == 3:
+            parents = [b ^ 1 for b in range(B)]
+        else:
+            parents = [int(b) // 20 * 20 + int(x) for b, x in enumerate(rng.integers(0, 20, B))]
+        was = r.read()
+        r.reorder(parents)
+        same(was, r.read(), parents)
+    ring = list(range(1, 192)) + [0] + list(range(192, B))
+    with pytest.raises(hwkv.HwkvError, match="cycle"):
+        hwkv.cache_reorder(r.cache, ring)
+    same(r.read(), r.read())
+
+
+def test_shared_pages_are_counted():
+    """Forks of forks: pages go back to the pool with their last holder."""
+    r = Held([[1]], [700, 0, 0, 0], pages=20)
+    r.reorder([0, 0, 0, 0])
+    r.check_pages()
+    assert hwkv.cache_pages(r.cache) == (20, 20 - 2 - 4)
+    for _ in range(70):
+        r.append()                         # 770: every sequence takes a page of its own
+    r.check_pages()
+    r.reorder([1, 1, 2, 1])
+    r.check_pages()
+    for b in range(3):
+        hwkv.cache_reset_seq(r.cache, b)
+        r.chains[b], r.n[b] = [], 0
+        r.check_pages()
+    r.reorder([3, 3, -1, -1])
+    r.check_pages()
+
+
+def test_a_short_pool_changes_nothing():
+    """Three copies of a partly filled page; the pool has one, and nobody leaves one."""
+    r = Held([[1, 0]], [300, 300, 0, 0, 0], pages=5, seed=3)
+    was = r.read()
+    with pytest.raises(hwkv.HwkvError, match="3 pages needed, 1 free"):
+        hwkv.cache_reorder(r.cache, [0, 1, 0, 1, 0])
+    same(was, r.read())
+    r.check_pages()
+    r.reorder([0, 1, 0, -1, -1])
+    same(was, r.read(), [0, 1, 0, -1, -1])
+    r.check_pages()
+
+
+def test_a_pool_that_just_fits():
+    """Copies take the pages that sequences without children leave, then those that
+    the call itself frees."""
+    r = Held([[1]], [600, 300, 10, 0], pages=6)      # 3 + 2 + 1: none is free
+    was = r.read()
+    r.reorder([0, 0, 0, -1])                         # two copies, three pages left
+    same(was, r.read(), [0, 0, 0, -1])
+    r.check_pages()
+    assert hwkv.cache_pages(r.cache)[1] == 1
+    r.reorder([0, 1, 2, 2])
+    assert hwkv.cache_pages(r.cache)[1] == 0
+    r.check_pages()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f16", "fp8", "i8"])
+@pytest.mark.parametrize("paged", [True, False])
+def test_a_moved_cache_goes_on_as_before(fmt, paged):
+    """Moved into the caller's buffers and into the library's, grown and shrunk, with
+    shared pages and holes: rows, pages and decoding are those of a twin."""
+    mk = lambda: Held(LEVELS, LENS[:7] + [9], fmt=fmt, D=128, G=2, paged=paged, seed=7)   # noqa: E731
+    r, twin = mk(), mk()
+    scale = 1 / math.sqrt(128)
+    ws = torch.empty(hwkv.decode_workspace_bytes(r.cache), dtype=torch.uint8, device=DEV)
+    for turn, pages in enumerate((120, 60, 25, 90)):
+        for x in (r, twin):
+            if turn == 1:
+                x.reorder([2, 0, 2, 2, -1, 5, 5, 0])
+                hwkv.cache_reset_seq(x.cache, 3)
+                x.n[3], x.chains[3] = 0, []
+                x.reorder([0, 1, 2, 1, 1, 5, 6, 7])
+        if turn == 2 and paged:
+            used = r.full * len({p for chain in r.chains for p in chain})
+            pages = used
+            with pytest.raises(hwkv.HwkvError, match="pages in use"):
+                hwkv.cache_move(r.cache, used - 1)
+        buf = None
+        if turn % 2 == 0:
+            need = hwkv.cache_bytes(r.pol, r.B, 1400, fmt, pages if paged else None)
+            buf = torch.full((need + 256,), 0xff, dtype=torch.uint8, device=DEV)
+        hwkv.cache_move(r.cache, pages if paged else None, None if buf is None else buf[:need])
+        torch.cuda.synchronize()
+        if buf is not None:
+            assert (buf[need:] == 0xff).all()
+        if paged:
+            r.pages = pages
+            r.check_pages()
+            if turn == 2:
+                hwkv.cache_move(r.cache, 80)          # room to go on
+                r.pages = 80
+        same(twin.read(), r.read())
+        for _ in range(2):
+            outs = []
+            q = torch.randn((r.B, 2 * r.H, 128), device=DEV).to(torch.bfloat16)
+            for x in (r, twin):
+                x.append()
+                out = torch.empty(q.shape, device=DEV)
+                for layer in range(r.L):
+                    hwkv.decode_attn(x.cache, layer, q, scale, out, ws)
+                    outs.append(out.clone())
+            assert torch.equal(torch.stack(outs[:r.L]), torch.stack(outs[r.L:]))
+        same(twin.read(), r.read())
+
+
+def test_a_move_into_bad_buffers_changes_nothing():
+    r = Held([[0, 1]], [300, 20])
+    was = r.read()
+    need = hwkv.cache_bytes(r.pol, r.B, 1400, "bf16", r.pages)
+    buf = torch.zeros(need + 64, dtype=torch.uint8, device=DEV)
+    for bad in (buf[:need - 1], buf[8:]):
+        with pytest.raises(hwkv.HwkvError):
+            hwkv.cache_move(r.cache, r.pages, bad)
+    hwkv.cache_move(r.cache, r.pages, buf[:need])
+    with pytest.raises(hwkv.HwkvError, match="overlaps"):
+        hwkv.cache_move(r.cache, r.pages, buf[32:32 + need])
+    same(was, r.read())
+
+
+def test_an_empty_cache_moves():
+    r = Held([[0, 1]], [0, 0])
+    hwkv.cache_move(r.cache, 3)
+    r.pages = 3
+    r.check_pages()
+    hwkv.cache_move(r.cache, 0)
+    assert hwkv.cache_pages(r.cache) == (0, 0)
+
+
+def test_on_another_stream():
+    r = Held([[0, 1]], [600, 30, 300], seed=2)
+    was = r.read()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    r.reorder([0, 0, 0], stream=s)
+    need = hwkv.cache_bytes(r.pol, r.B, 1400, "bf16", 40)
+    buf = torch.zeros(need, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    hwkv.cache_move(r.cache, 40, buf, stream=s)
+    s.synchronize()
+    same(was, r.read(), [0, 0, 0])
+
+
+def test_beam_search():
+    """Selection, reordering, appends and decoding together: at every step the
+    choice is that of 64-bit scores over the step's logits, and the outputs are
+    attention over the tokens of each beam's own history."""
+    V, beams, groups, H, G, D, S, w, steps = 211, 4, 3, 2, 2, 64, 2, 40, 30
+    B = beams * groups
+    g = torch.Generator(device=DEV).manual_seed(11)
+    emb = {x: torch.randn((V, n, D), generator=g, device=DEV).to(torch.bfloat16) for x, n in (("q", H * G), ("k", H), ("v", H))}
+    head = torch.randn((H * G * D, V), generator=g, device=DEV) * 0.2
+    prompts = [torch.randint(0, V, (n,), generator=g, device=DEV) for n in (250, 300, 7)]
+    pol = hwkv.policy_set(1, H, H * G, D, S, [w, 0], [[0, 1]])
+    cache = hwkv.cache_alloc(pol, B, 512, n_pages=24)
+    ws = torch.empty(hwkv.decode_workspace_bytes(cache), dtype=torch.uint8, device=DEV)
+    for i, p in enumerate(prompts):
+        hwkv.prefill_write(cache, 0, i * beams, 0, emb["k"][p[:-1]].contiguous(), emb["v"][p[:-1]].contiguous())
+    hwkv.cache_reorder(cache, [b // beams * beams for b in range(B)])
+    tokens = torch.stack([p[-1] for p in prompts]).repeat_interleave(beams)
+    history = [prompts[b // beams].tolist() for b in range(B)]
+    scores = torch.tensor([[0.0] + [-math.inf] * (beams - 1)] * groups, device=DEV)
+    out = torch.empty((B, H * G, D), device=DEV)
+    new_s, par, tok = torch.empty((groups, beams), device=DEV), *(torch.empty((groups, beams), dtype=torch.int32, device=DEV) for _ in range(2))
+    k_all, v_all, q_all = (emb[x].double().cpu() for x in "kvq")
+    from test_gpu_beam import check
+    for step in range(steps):
+        hwkv.append(cache, 0, emb["k"][tokens].contiguous(), emb["v"][tokens].contiguous())
+        hwkv.decode_attn(cache, 0, emb["q"][tokens].contiguous(), 0.125, out, ws)
+        if step % 7 == 0 or step == steps - 1:
+            got = out.cpu().double()
+            for b in range(B):
+                h = torch.tensor(history[b])
+                for kv in range(H):
+                    keep = (torch.arange(len(h)) < S) | (torch.arange(len(h)) >= len(h) - w) if kv == 0 else torch.ones(len(h), dtype=torch.bool)
+                    kk, vv = k_all[h[keep], kv], v_all[h[keep], kv]
+                    qq = q_all[h[-1], kv * G:(kv + 1) * G]
+                    ref = torch.softmax(qq @ kk.T * 0.125, dim=1) @ vv
+                    # fp32 sums over bf16 inputs
+                    assert (got[b, kv * G:(kv + 1) * G] - ref).abs().max() <= 2e-5 * vv.abs().max()
+        logits = (out.flatten(1) @ head).view(groups, beams, V)
+        hwkv.beam_select(logits, scores, new_s, par, tok, torch.empty(hwkv.beam_workspace_bytes(logits, beams), dtype=torch.uint8, device=DEV))
+        check((new_s, par, tok), logits, scores, beams)
+        parents, tokens = par.flatten().tolist(), tok.flatten().long()
+        hwkv.cache_reorder(cache, parents)
+        history = [history[p] + [int(t)] for p, t in zip(parents, tokens)]
+        scores.copy_(new_s)
+    total, free = hwkv.cache_pages(cache)
+    for b in range(B):
+        hwkv.cache_reset_seq(cache, b)
+    assert hwkv.cache_pages(cache) == (total, total) and free < total
