@@ -253,8 +253,8 @@ int hwkv_cache_reorder(hwkv_cache *cache, const int32_t *parents, void *stream);
 
 /* Move a cache into another buffer, with a pool of another size (a pool that has
  * run out, or one that may shrink): the rows that its sequences hold are copied,
- * pages that several hold once, and the pages in use become the new pool's first
- * ones, in the order (layer, KV head, sequence, position).
+ * pages whole and those that several hold once, and the pages in use become the new
+ * pool's first ones, in the order (layer, KV head, sequence, position).
  *   n_pages             the new pool; 0 for a cache that is not paged
  *   dev_buf, buf_bytes  as in hwkv_cache_alloc_paged, and apart from the present
  *                       buffer; NULL: the library allocates
@@ -499,6 +499,28 @@ int hwkv_decode_workspace_bytes(const hwkv_cache *cache, size_t *bytes);
 int hwkv_decode_attn(hwkv_cache *cache, int32_t layer, const void *q,
                      float scale, void *out, void *ws, size_t ws_bytes,
                      void *stream);
+
+/* hwkv_decode_attn where sequences share pages (hwkv_cache_reorder): whole pages
+ * that several sequences hold are read once for all of them, with the query heads of
+ * up to 64 columns at a time.  Right for every cache and every batch, forked or not;
+ * where nothing is shared hwkv_decode_attn is as fast or faster.  Which pages are
+ * shared is known to the host: the call reads nothing back.
+ *   ws, ws_bytes  device workspace of >= hwkv_decode_shared_workspace_bytes, 16-byte
+ *                 aligned
+ * Other arguments and errors as hwkv_decode_attn, and EINVAL on more than 65535
+ * sequences and on misaligned pointers.  Queries and rows enter as there (int8: the
+ * query as bf16, scaled by a power of two per query head, products exact, sums fp32);
+ * the weights as three bf16 terms that carry each to 2^-27 of itself, or, over
+ * binary16 values, two binary16 terms (2^-22).  Outputs differ from those of
+ * hwkv_decode_attn by the order of fp32 sums; equal calls on equal caches give equal
+ * bits. */
+int hwkv_decode_attn_shared(hwkv_cache *cache, int32_t layer, const void *q,
+                            float scale, void *out, void *ws, size_t ws_bytes,
+                            void *stream);
+
+/* Workspace bytes hwkv_decode_attn_shared needs for any layer, lengths and
+ * sharing. */
+int hwkv_decode_shared_workspace_bytes(const hwkv_cache *cache, size_t *bytes);
 
 /* hwkv_append followed by hwkv_decode_attn, in one pass over the cache: the
  * new token is attended from k_new/v_new and written to its slot by the same

@@ -22,7 +22,8 @@ ARCH = "gfx950"
 SOURCES = ["hwkv_api.hip", "decode_kernels.hip", "decode_split_bf16.hip",
            "decode_split_f16.hip", "decode_split_fp8.hip", "decode_i8.hip",
            "write_kernels.hip", "rope_kernels.hip", "prefill_attn_kernels.hip", "calib_kernels.hip",
-           "beam_kernels.hip", "reorder_kernels.hip"]
+           "beam_kernels.hip", "reorder_kernels.hip", "decode_shared_bf16.hip",
+           "decode_shared_f16.hip", "decode_shared_fp8.hip", "decode_shared_i8.hip", "decode_shared_merge.hip"]
 PROBE_SOURCE = os.path.join("probe", "read_probe.hip")
 PROBE_LIB = os.path.join(LIBDIR, "libhwkv_probe.so")
 

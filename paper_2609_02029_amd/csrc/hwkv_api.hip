@@ -2962,16 +2962,13 @@ int move_impl(hwkv_cache *c, int64_t n_pages, void *dev_buf, size_t buf_bytes, h
   each_full_unit(c, [&](int32_t fi, int32_t l, int32_t pto0) {
     for (int32_t b = 0; b < B; ++b) {
       const int32_t pto = pto0 + (int32_t)(b * c->max_pages);
-      const int64_t n = c->n[(size_t)l * B + b];
-      const int32_t need = (int32_t)pages_for(n);
+      const int32_t need = (int32_t)pages_for(c->n[(size_t)l * B + b]);
       for (int32_t j = 0; j < need; ++j) {
         int32_t &page = moved[(size_t)c->pt_host[(size_t)pto + j]];
         const int32_t copy = page < 0 ? 1 : 0;
         if (copy) page = used++;
-        if (j > 0 && runs.back().copy == copy && runs.back().dst0 + j - runs.back().j0 == page) {
-        } else {
-          runs.push_back({pto, j, page, 0, (int32_t)(n - (int64_t)j * hwkv::kPageTokens), copy});
-        }
+        if (j == 0 || runs.back().copy != copy || runs.back().dst0 + j - runs.back().j0 != page)
+          runs.push_back({pto, j, page, 0, copy});
         runs.back().begin = j + 1 - runs.back().j0;    // (its length, until it is launched)
         to.pt_host[(size_t)pto + j] = page;
         if (page < n_pages) ++to.refs[(size_t)page];
@@ -3076,6 +3073,292 @@ int hwkv_cache_move(hwkv_cache *c, int64_t n_pages, void *dev_buf, size_t buf_by
   if (!c->paged && n_pages != 0) return fail(HWKV_EINVAL, "n_pages must be 0 for a cache that is not paged");
   try {
     const int rc = move_impl(c, n_pages, dev_buf, buf_bytes, (hipStream_t)stream);
+    return rc == HWKV_OK ? ok() : rc;
+  } catch (const std::bad_alloc &) {
+    return fail(HWKV_ENOMEM, "host allocation failed");
+  }
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// decode over shared pages
+// ---------------------------------------------------------------------------
+namespace {
+
+// Sequences that share whole pages of a layer's full units, and how many.
+struct Family {
+  std::vector<int32_t> members;
+  int32_t pages;
+};
+
+// Pages that b and o share, of their whole ones (chains share prefixes only).
+int32_t shared_pages(const hwkv_cache *c, int32_t layer, int32_t unit, int32_t b, int32_t o) {
+  const int32_t *x = &c->pt_host[(size_t)page_tab_off(c, unit, b)], *y = &c->pt_host[(size_t)page_tab_off(c, unit, o)];
+  int32_t lo = 0;
+  int32_t hi = (int32_t)(std::min(c->n[(size_t)layer * c->batch + b], c->n[(size_t)layer * c->batch + o]) /
+                         hwkv::kPageTokens);
+  while (lo < hi) {
+    const int32_t mid = (lo + hi + 1) / 2;
+    if (x[mid - 1] == y[mid - 1]) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Splits `set` into the families that save most reads: all of it over the pages that
+// it shares, or the families of the parts into which it falls behind them.  Returns
+// the pages saved.
+int64_t find_families(const hwkv_cache *c, int32_t layer, int32_t unit, const std::vector<int32_t> &set,
+                      std::vector<Family> *out) {
+  if (set.size() < 2) return 0;
+  int32_t pages = INT32_MAX;
+  for (size_t i = 1; i < set.size(); ++i) pages = std::min(pages, shared_pages(c, layer, unit, set[0], set[i]));
+  const int64_t whole = (int64_t)pages * (int64_t)(set.size() - 1);
+  std::map<int32_t, std::vector<int32_t>> parts;           // by the page behind the shared ones
+  for (int32_t b : set)
+    if (c->n[(size_t)layer * c->batch + b] / hwkv::kPageTokens > pages)
+      parts[c->pt_host[(size_t)page_tab_off(c, unit, b) + pages]].push_back(b);
+  std::vector<Family> apart;
+  int64_t saved = 0;
+  for (const auto &part : parts)
+    if (part.second.size() < set.size()) saved += find_families(c, layer, unit, part.second, &apart);
+  if (saved > whole) {
+    out->insert(out->end(), apart.begin(), apart.end());
+    return saved;
+  }
+  if (whole > 0) out->push_back({set, pages});
+  return whole;
+}
+
+// The column groups of 16 that the kernel is compiled for.
+int32_t column_groups(int64_t columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
+
+// Workgroups that a launch aims at: as many as run at once.
+int64_t shared_target(int32_t n_col_groups) { return (n_col_groups == 1 ? 2 : 1) * hwkv::device_cu_count(); }
+
+// Most workgroups, and workgroups of blocks, of a launch of n_heads heads (n_full of
+// them full and paged) and n_seqs sequences.
+void shared_bounds(int64_t n_heads, int64_t n_full, int64_t n_seqs, int64_t *wgs, int64_t *block_wgs) {
+  const int64_t blocks = n_full > 0 ? std::min<int64_t>(hwkv::kSharedBlocks, n_seqs / 2) : 0;
+  *wgs = std::max(shared_target(1), n_heads * n_seqs + n_full * blocks);
+  *block_wgs = blocks > 0 ? std::max(shared_target(1), n_full * blocks) : 0;
+}
+
+// Bytes of the parts of so many workgroups: acc and (m, l) of the blocks', then of all.
+size_t shared_part_bytes(const hwkv_policy &p, int64_t wgs, int64_t block_wgs, int32_t n_col_groups) {
+  const size_t rows = (size_t)block_wgs * 16 * n_col_groups + (size_t)wgs * (size_t)group_size(p);
+  return rows * (size_t)(p.head_dim + 2) * sizeof(float);
+}
+
+int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *out, void *ws, size_t ws_bytes,
+                hipStream_t s) {
+  const hwkv_policy &p = c->pol;
+  const int32_t H = p.n_kv_heads, B = c->batch;
+  const int64_t G = group_size(p), D = p.head_dim;
+  const auto len = [&](int32_t b) { return c->n[(size_t)layer * B + b]; };
+  // heads, full ones first, by capacity
+  std::vector<int32_t> heads(H);
+  for (int32_t h = 0; h < H; ++h) heads[h] = h;
+  const auto full = [&](int32_t h) { return c->paged && c->full_index[layer * H + h] >= 0; };
+  std::sort(heads.begin(), heads.end(), [&](int32_t x, int32_t y) {
+    if (full(x) != full(y)) return full(x);
+    const int64_t cx = c->cap[layer * H + x], cy = c->cap[layer * H + y];
+    return cx != cy ? cx > cy : x < y;
+  });
+  std::vector<Family> families;
+  if (full(heads[0])) {
+    std::vector<int32_t> all(B);
+    for (int32_t b = 0; b < B; ++b) all[b] = b;
+    find_families(c, layer, layer * H + heads[0], all, &families);
+  }
+  std::sort(families.begin(), families.end(),
+            [](const Family &x, const Family &y) { return x.members[0] < y.members[0]; });
+  // blocks of at most kSharedColumns columns, and the sequences of none as one each
+  std::vector<char> taken(B, 0);
+  std::vector<Family> blocks;
+  for (const Family &f : families) {
+    const int64_t n = (int64_t)f.members.size(), most = hwkv::kSharedColumns / G;
+    const int64_t parts = (n + most - 1) / most, per = (n + parts - 1) / parts;
+    for (int64_t i = 0; i < n; i += per) {
+      const auto at = f.members.begin() + i;
+      blocks.push_back({std::vector<int32_t>(at, at + std::min(per, n - i)), f.pages});
+    }
+    for (int32_t b : f.members) taken[b] = 1;
+  }
+  for (int32_t b = 0; b < B; ++b)
+    if (!taken[b]) blocks.push_back({{b}, 0});
+
+  struct Launch {
+    hwkv::SharedArgs a;
+    int64_t wgs, block_wgs;
+  };
+  std::vector<Launch> launches;
+  size_t need = 0;
+  for (size_t next = 0; next < blocks.size();) {
+    hwkv::SharedArgs a;
+    std::memset(&a, 0, sizeof a);
+    int64_t columns = 0;
+    std::vector<int64_t> own;                    // tiles of a sequence's own rows in a full unit
+    while (next < blocks.size() && a.n_seqs + blocks[next].members.size() <= (size_t)hwkv::kSharedSeqs) {
+      const Family &f = blocks[next];
+      if (f.pages > 0) {
+        if (a.n_blocks == hwkv::kSharedBlocks) break;
+        a.block_pages[a.n_blocks] = f.pages;
+        a.block_first[a.n_blocks] = (uint8_t)a.n_seqs;
+        a.block_count[a.n_blocks] = (uint8_t)f.members.size();
+        columns = std::max<int64_t>(columns, (int64_t)f.members.size() * G);
+      }
+      for (int32_t b : f.members) {
+        a.seq[a.n_seqs] = (uint16_t)b;
+        a.len[a.n_seqs] = (int32_t)len(b);
+        a.seq_block[a.n_seqs++] = f.pages > 0 ? (uint8_t)a.n_blocks : hwkv::kNoBlock;
+        own.push_back(tiles_for(len(b) - (int64_t)f.pages * hwkv::kPageTokens));
+      }
+      if (f.pages > 0) ++a.n_blocks;
+      ++next;
+    }
+    a.cache = c->base;
+    a.page_table = device_page_table(c);
+    a.pool_off = c->pool_off;
+    a.q = static_cast<const uint16_t *>(q);
+    a.out = static_cast<float *>(out);
+    a.n_q_heads = p.n_q_heads;
+    a.group = (int32_t)G;
+    a.max_pages = (int32_t)c->max_pages;
+    a.n_col_groups = column_groups(std::max(columns, G));
+    a.scale_log2 = scale * 1.4426950408889634f;
+    int64_t longest_len = 0;
+    for (int32_t i = 0; i < a.n_seqs; ++i) longest_len = std::max<int64_t>(longest_len, a.len[i]);
+    for (int32_t h0 = 0; h0 < H; h0 += hwkv::kSharedHeads) {
+      a.n_heads = std::min(hwkv::kSharedHeads, H - h0);
+      a.n_full = 0;
+      while (a.n_full < a.n_heads && full(heads[h0 + a.n_full])) ++a.n_full;
+      // tiles per workgroup: the least at which the launch has no more workgroups than
+      // it aims at, or one for every item
+      int64_t total = 0, longest = 1;
+      const auto window_tiles = [&](int32_t r) {
+        return tiles_for(std::min(longest_len, c->cap[layer * H + heads[h0 + r]]));
+      };
+      const auto count = [&](int64_t T) {
+        int64_t n = 0;
+        if (a.n_full > 0) {
+          for (int32_t i = 0; i < a.n_blocks; ++i) n += (a.block_pages[i] * 4 + T - 1) / T;
+          for (int64_t t : own) n += (t + T - 1) / T;
+          n *= a.n_full;
+        }
+        for (int32_t r = a.n_full; r < a.n_heads; ++r) n += (window_tiles(r) + T - 1) / T * a.n_seqs;
+        return n;
+      };
+      for (int32_t i = 0; i < a.n_blocks && a.n_full > 0; ++i) {
+        total += (int64_t)a.block_pages[i] * 4 * a.n_full;
+        longest = std::max<int64_t>(longest, a.block_pages[i] * 4);
+      }
+      for (int64_t t : own) {
+        total += a.n_full > 0 ? t * a.n_full : 0;
+        longest = std::max(longest, a.n_full > 0 ? t : 1);
+      }
+      for (int32_t r = a.n_full; r < a.n_heads; ++r) {
+        total += window_tiles(r) * a.n_seqs;
+        longest = std::max(longest, window_tiles(r));
+      }
+      const int64_t target = shared_target(a.n_col_groups);
+      int64_t T = std::max<int64_t>(1, (total + target - 1) / target);
+      while (T < longest && count(T) > target) T += 1 + T / 64;
+      T = std::min(T, longest);
+      a.tiles_per_wg = (int32_t)T;
+      if (a.n_full > 0) {
+        int64_t begin = 0;
+        int32_t k = 0;
+        for (int32_t i = 0; i < a.n_blocks; ++i) {
+          a.item_begin[k++] = (uint16_t)begin;
+          begin += (a.block_pages[i] * 4 + T - 1) / T;
+        }
+        a.block_wgs = (int32_t)begin;
+        for (int64_t t : own) {
+          a.item_begin[k++] = (uint16_t)begin;
+          begin += (t + T - 1) / T;
+        }
+        a.item_begin[k++] = (uint16_t)begin;
+        for (; k < hwkv::kSharedItems; ++k) a.item_begin[k] = UINT16_MAX;
+      } else {
+        a.block_wgs = 0;
+      }
+      int64_t begin = 0;
+      const int32_t items = a.n_blocks + a.n_seqs;
+      for (int32_t r = 0; r < a.n_heads; ++r) {
+        const int32_t h = heads[h0 + r], u = layer * H + h;
+        hwkv::ItemHead &hd = a.head[r];
+        hd.k_off = c->k_off[u];
+        hd.v_off = c->v_off[u];
+        hd.cap = (int32_t)c->cap[u];
+        hd.cap_pad = (int32_t)c->cap_pad[u];
+        hd.window = (int32_t)c->window[u];
+        hd.page0 = page_tab_off(c, u, 0);
+        hd.v_scale = c->v_scale[u];
+        if (c->fmt == HWKV_KV_I8) hd.s_off128 = (uint32_t)(std::max<int64_t>(0, c->s_off[u]) / 128);
+        else hd.k_scale = c->k_scale[u];
+        a.head_id[r] = (uint8_t)h;
+        a.wg_begin[r] = (int32_t)begin;
+        begin += r < a.n_full ? a.item_begin[items] : (window_tiles(r) + T - 1) / T * a.n_seqs;
+      }
+      for (int32_t r = a.n_heads; r < hwkv::kMaxItems; ++r) a.wg_begin[r] = r == a.n_heads ? (int32_t)begin : INT32_MAX;
+      launches.push_back({a, begin, (int64_t)a.n_full * a.block_wgs});
+      need = std::max(need, shared_part_bytes(p, begin, launches.back().block_wgs, a.n_col_groups));
+    }
+  }
+  if (!ws || ws_bytes < need)
+    return fail(HWKV_EINVAL, "workspace missing or too small (need " + std::to_string(need) + " bytes)");
+  for (Launch &L : launches) {                   // (they use the workspace in turn)
+    hwkv::SharedArgs &a = L.a;
+    const size_t cols = (size_t)L.block_wgs * 16 * a.n_col_groups, rows = (size_t)L.wgs * G;
+    a.block_acc = static_cast<float *>(ws);
+    a.own_acc = a.block_acc + cols * D;
+    a.block_ml = a.own_acc + rows * D;
+    a.own_ml = a.block_ml + cols * 2;
+    int rc = check_device(hwkv::launch_decode_shared(c->fmt, (int)D, a, s), "shared decode launch");
+    if (rc == HWKV_OK) rc = check_device(hwkv::launch_shared_merge((int)D, a, s), "shared decode merge launch");
+    if (rc != HWKV_OK) return rc;
+  }
+  return HWKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hwkv_decode_shared_workspace_bytes(const hwkv_cache *c, size_t *bytes) {
+  if (!c || !bytes) return fail(HWKV_EINVAL, "null argument");
+  const hwkv_policy &p = c->pol;
+  const int64_t seqs = std::min(hwkv::kSharedSeqs, c->batch), H = p.n_kv_heads;
+  const int64_t G = group_size(p);
+  size_t most = 0;
+  for (int32_t l = 0; l < p.n_layers; ++l) {
+    int64_t n_full = 0;
+    for (int32_t h = 0; h < H && c->paged; ++h) n_full += c->full_index[l * H + h] >= 0 ? 1 : 0;
+    int64_t wgs = 0, block_wgs = 0;
+    shared_bounds(std::min<int64_t>(hwkv::kSharedHeads, H), std::min<int64_t>(hwkv::kSharedHeads, n_full), seqs, &wgs,
+                  &block_wgs);
+    const int64_t columns = std::min<int64_t>(hwkv::kSharedColumns, seqs * G);
+    most = std::max(most, shared_part_bytes(p, wgs, block_wgs, column_groups(columns)));
+  }
+  *bytes = most;
+  return ok();
+}
+
+int hwkv_decode_attn_shared(hwkv_cache *c, int32_t layer, const void *q, float scale, void *out, void *ws,
+                            size_t ws_bytes, void *stream) {
+  if (!c) return fail(HWKV_EINVAL, "cache is null");
+  if (layer < 0 || layer >= c->pol.n_layers) return fail(HWKV_EINVAL, "layer out of range");
+  if (!q || !out) return fail(HWKV_EINVAL, "q and out must be non-null");
+  if ((uintptr_t)q % 16 != 0 || (uintptr_t)out % 16 != 0 || (uintptr_t)ws % 16 != 0)
+    return fail(HWKV_EINVAL, "q, out and the workspace must be 16-byte aligned");
+  if (!std::isfinite(scale)) return fail(HWKV_EINVAL, "scale must be finite");
+  if (c->batch > UINT16_MAX) return fail(HWKV_EINVAL, "more than 65535 sequences");
+  for (int32_t b = 0; b < c->batch; ++b)
+    if (seq_len(c, layer, b) == 0) return fail(HWKV_EINVAL, "decode on an empty sequence");
+  try {
+    const int rc = shared_impl(c, layer, q, scale, out, ws, ws_bytes, (hipStream_t)stream);
     return rc == HWKV_OK ? ok() : rc;
   } catch (const std::bad_alloc &) {
     return fail(HWKV_ENOMEM, "host allocation failed");

@@ -131,8 +131,7 @@ __global__ __launch_bounds__(256) void page_move(PageMoveArgs a) {
   if (part == 0 && threadIdx.x == 0) a.to_table[r.pto + r.j0 + j] = dst;
   if (!r.copy) return;
   const int64_t page = page_bytes(a.row_bytes, a.pair_bytes);
-  copy_page(a.from_pool + src * page, a.to_pool + dst * page, part, min(kPageTokens, r.rows - j * kPageTokens),
-            a.row_bytes, a.pair_bytes);
+  copy_page(a.from_pool + src * page, a.to_pool + dst * page, part, kPageTokens, a.row_bytes, a.pair_bytes);
 }
 
 }  // namespace

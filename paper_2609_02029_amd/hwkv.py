@@ -75,6 +75,8 @@ SYMBOLS = {
     "hwkv_append": ([_vp, _i32, _vp, _vp, _vp], ctypes.c_int),
     "hwkv_decode_workspace_bytes": ([_vp, _P(_sz)], ctypes.c_int),
     "hwkv_decode_attn": ([_vp, _i32, _vp, _flt, _vp, _vp, _sz, _vp], ctypes.c_int),
+    "hwkv_decode_attn_shared": ([_vp, _i32, _vp, _flt, _vp, _vp, _sz, _vp], ctypes.c_int),
+    "hwkv_decode_shared_workspace_bytes": ([_vp, _P(_sz)], ctypes.c_int),
     "hwkv_append_decode_attn": ([_vp, _i32, _vp, _vp, _vp, _flt, _vp, _vp, _sz, _vp], ctypes.c_int),
     "hwkv_append_decode_attn_noalloc": ([_vp, _i32, _vp, _vp, _vp, _flt, _vp, _vp], ctypes.c_int),
     "hwkv_cache_read_scales": ([_vp, _i32, _i32, _i32, _vp, _vp], ctypes.c_int),
@@ -593,6 +595,21 @@ def decode_attn(cache, layer, q, scale, out, ws, stream=None):
     wp, wn = _decode_shapes(cache, q, out, ws)
     _check(_lib.hwkv_decode_attn(cache.handle, layer, _dev(q, "bfloat16", "q"), float(scale),
                                  _dev(out, "float32", "out"), wp, wn, _stream(stream)))
+
+
+def decode_shared_workspace_bytes(cache):
+    r = _sz()
+    _check(_lib.hwkv_decode_shared_workspace_bytes(cache.handle, ctypes.byref(r)))
+    return r.value
+
+
+def decode_attn_shared(cache, layer, q, scale, out, ws, stream=None):
+    """``decode_attn`` that reads the pages which sequences share (cache_reorder)
+    once for all of them; ``ws``: see decode_shared_workspace_bytes."""
+    wp, wn = _decode_shapes(cache, q, out, ws)
+    _on_current_device(q, out, ws)
+    _check(_lib.hwkv_decode_attn_shared(cache.handle, layer, _dev(q, "bfloat16", "q"), float(scale),
+                                        _dev(out, "float32", "out"), wp, wn, _stream(stream)))
 
 
 def append_decode_attn(cache, layer, k_new, v_new, q, scale, out, ws, stream=None):
