@@ -24,7 +24,8 @@
 namespace hwkv {
 namespace {
 
-constexpr int kScanWaves = 4, kScanDeep = 4;   // waves; blocks a wave has in flight
+constexpr int kScanWaves = 4;
+constexpr int kBlock = 512;          // logits of a block: 8 a lane
 constexpr double kLog2e = 0x1.71547652b82fep+0;
 constexpr float kInf = __builtin_inff();
 
@@ -35,6 +36,8 @@ template <int T>
 constexpr int kBytes = T == HWKV_LOGITS_F32 ? 4 : 2;
 template <int T>
 constexpr int kPerChunk = 16 / kBytes<T>;
+template <int T>
+constexpr int kBlockChunks = kBlock / 64 / kPerChunk<T>;   // a lane's
 
 // Element e of a chunk.
 template <int T>
@@ -81,31 +84,48 @@ struct Row {
   }
 };
 
-// The larger, NaN if either is.
-__device__ __forceinline__ float most(float x, float y) { return __builtin_elementwise_maximum(x, y); }
-
+// op(x, y) over the wavefront, in every lane: lanes 1 and 2 apart, a half row's
+// mirror, a row's, and the rows, two and two (registers only, where a shuffle goes
+// through LDS).  Words: 32-bit parts of the value.
 template <int CTRL>
-__device__ __forceinline__ float most_dpp(float x) {
-  return most(x, __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xf, 0xf, true)));
+__device__ __forceinline__ uint32_t from_dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, true);
 }
-
-// The largest over the wavefront, in every lane (NaN if any is).
-__device__ __forceinline__ float wave_most(float x) {
-  x = most_dpp<0xb1>(x);                     // lanes 1 apart,
-  x = most_dpp<0x4e>(x);                     // 2,
-  x = most_dpp<0x141>(x);                    // a half row's mirror,
-  x = most_dpp<0x140>(x);                    // the row's
-  const uint32_t u = __float_as_uint(x);
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const uint32_t y = __float_as_uint(most(__uint_as_float(a[0]), __uint_as_float(a[1])));
-  const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-  return most(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
-__device__ __forceinline__ double wave_sum(double x) {
+template <typename V, typename F>
+__device__ __forceinline__ V over_wave(V x, F op) {
+  constexpr int W = sizeof(V) / 4;
+  struct Words {
+    uint32_t w[W];
+  };
+  auto step = [&](auto f) {
+    Words a = __builtin_bit_cast(Words, x), b;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    for (int i = 0; i < W; ++i) b.w[i] = f(a.w[i]);
+    x = op(x, __builtin_bit_cast(V, b));
+  };
+  step([](uint32_t u) { return from_dpp<0xb1>(u); });
+  step([](uint32_t u) { return from_dpp<0x4e>(u); });
+  step([](uint32_t u) { return from_dpp<0x141>(u); });
+  step([](uint32_t u) { return from_dpp<0x140>(u); });
+  auto rows = [&](auto swap) {
+    Words a = __builtin_bit_cast(Words, x), b;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const auto r = swap(a.w[i]);
+      a.w[i] = r[0];
+      b.w[i] = r[1];
+    }
+    x = op(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b));
+  };
+  rows([](uint32_t u) { return __builtin_amdgcn_permlane16_swap(u, u, false, false); });
+  rows([](uint32_t u) { return __builtin_amdgcn_permlane32_swap(u, u, false, false); });
   return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return over_wave(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ double wave_sum(double x) {
+  return over_wave(x, [](double a, double b) { return a + b; });
 }
 
 // 2^f on [-1/2, 1/2].
@@ -121,18 +141,19 @@ __device__ __forceinline__ double exp2_small(double f) {
   return __builtin_fma(p, f, 1.0);
 }
 
-// A sum of e^x as sum * e^base, base a logit (kNone where there is none).  Held so, and
-// a score as s + ((x - base) - log sum), rows far from zero lose nothing.
+// A sum of e^x as sum * e^base, base a logit (kNone where there is none): x - base is
+// exact, also far from zero.
 constexpr double kNone = -0x1p1000;
 struct Sum {
   double sum, base;
 };
 
 // Grid: n_splits workgroups a row.  Wave w of split i takes blocks 4 i + w, and so
-// on in steps of 4 n_splits.  What bounds it: HBM, and the 64-bit sums beside it.
-template <int T>
+// on in steps of 4 n_splits, DEEP at a time.  What bounds it: HBM, and the 64-bit sums
+// beside it.
+template <int T, int DEEP>
 __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
-  constexpr int N = kPerChunk<T>;
+  constexpr int N = kPerChunk<T>, C = kBlockChunks<T>;
   const int64_t row = blockIdx.x / a.n_splits;
   const int split = blockIdx.x % a.n_splits;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -143,24 +164,27 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
   // one, and of a block whose largest passes it by 600.  A logit more than 690 below
   // it counts as that (e^-690).
   double sum = 0.0, base = kNone;
-  for (int b0 = split * kScanWaves + wave; b0 < a.n_blocks; b0 += kScanDeep * step) {
-    u32x4_t c[kScanDeep];
+  for (int b0 = split * kScanWaves + wave; b0 < a.n_blocks; b0 += DEEP * step) {
+    u32x4_t v[DEEP][C];
 #pragma unroll
-    for (int i = 0; i < kScanDeep; ++i) c[i] = r.load((b0 + i * step) * 64 + lane, a.vocab);
+    for (int i = 0; i < DEEP; ++i)
 #pragma unroll
-    for (int i = 0; i < kScanDeep; ++i) {
+      for (int c = 0; c < C; ++c) v[i][c] = r.load(((b0 + i * step) * C + c) * 64 + lane, a.vocab);
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) {
       const int b = b0 + i * step;
       if (b >= a.n_blocks) break;
-      float x[N];
+      float x[C * N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = element<T>(c[i], e);
+      for (int e = 0; e < C * N; ++e) x[e] = element<T>(v[i][e / N], e % N);
       float top = x[0];
 #pragma unroll
-      for (int e = 1; e < N; ++e) top = most(top, x[e]);
-      top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wave_most(top))));
+      for (int e = 1; e < C * N; ++e) top = __builtin_elementwise_maximum(top, x[e]);   // (NaN if any is)
+      top = top == top ? top : kInf;
+      top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wave_max(top))));
       if (lane == 0) block_max[b] = top;
       if (top == -kInf) continue;
-      if (!(top < kInf)) {                   // an infinity or NaN: the row has no sum
+      if (top == kInf) {                     // an infinity or NaN: the row has no sum
         sum = __builtin_nan("");
         continue;
       }
@@ -169,7 +193,7 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
         base = (double)top;
       }
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
+      for (int e = 0; e < C * N; ++e) {
         // with 1.5 * 2^52 added, the low word is the whole part of d log2 e
         const double d = fmax((double)x[e] - base, -690.0);
         const double y = __builtin_fma(d, kLog2e, 0x1.8p52);
@@ -195,84 +219,117 @@ __device__ __forceinline__ uint64_t order_key(double score) {
   const uint64_t u = __double_as_longlong(score + 0.0);
   return score > -__builtin_inf() ? u ^ (u >> 63 ? ~0ull : 1ull << 63) : 0;
 }
-__device__ __forceinline__ float key_score(uint64_t key) {
-  return (float)__longlong_as_double(key >> 63 ? key ^ 1ull << 63 : ~key);
+__device__ __forceinline__ double key_score(uint64_t key) {
+  return __longlong_as_double(key >> 63 ? key ^ 1ull << 63 : ~key);
 }
 
-constexpr int kPickWaves = 4, kListed = 1024;
+constexpr int kPickThreads = 512, kListed = 1024;
+constexpr int kHeldMax = 8192;       // block maxima that a workgroup keeps in LDS,
+constexpr int kHeldBlocks = 16;      //   and blocks of logits
 
-struct Candidate {
-  uint64_t key;
-  uint32_t at;
-};
 struct PickShared {
-  double s[kMaxBeams], base[kMaxBeams];
-  double log_sum[kMaxBeams];                 // NaN: a beam without candidates
+  double s[kMaxBeams], lse[kMaxBeams];       // lse NaN: a beam without candidates
+  float bound[kMaxBeams];                    // below every logit of the beam that is asked for
   uint64_t key[kListed];
   uint32_t at[kListed];
-  uint64_t lane_key[kPickWaves][64];
+  uint32_t lane_key[kPickThreads / 64][64];
   uint64_t best_key[kMaxSelected];
   uint32_t best_at[kMaxSelected];
+  uint16_t block_beam[kMaxSelected];         // of the blocks whose logits are read
+  uint16_t block_in[kMaxSelected];
   uint64_t least;
-  int listed, count[kPickWaves];
+  int listed, hits[kPickThreads / 64];
+  union {
+    float max[kHeldMax];
+    u32x4_t logits[kHeldBlocks * kBlock / 4];
+  };
 };
 
-// Items of the workgroup for which f holds; `visit` calls its argument with every
-// (key, place) of the thread.
-template <typename V, typename F>
-__device__ __forceinline__ int count_items(PickShared &sh, V visit, F f) {
-  int n = 0;
-  visit([&](uint64_t key, uint32_t at) { n += f(key, at) ? 1 : 0; });
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.count[threadIdx.x >> 6] = n;
-  __syncthreads();
-  n = 0;
-  for (int w = 0; w < kPickWaves; ++w) n += sh.count[w];
-  return n;
-}
-
 // The n first items in the order (key falling, place rising) of those that `visit`
-// gives, into best_key / best_at; returns how many there are.  `least`: a key that at
-// least n items reach (or 1).  The items from there on are listed and counted
-// against each other.  Where the list does not hold them (long runs of equal or
-// rising logits), the n-th key and then the n-th item's place are found bit by bit
-// first.
+// gives (its argument is called with a beam, a logit and a place), into best_key /
+// best_at; returns how many there are.  `least`: a key that at least n items reach (or
+// 1).  The items from there on are listed and counted against each other; a bound for
+// the beam's logits keeps all others out with one comparison.  Where the list does not
+// hold them (long runs of equal or rising logits), the n-th key, how many lie above it
+// and then the n-th item's place are found bit by bit first.
+//
+// (One visit in a loop, whatever it is for: the kernel runs through its code once.
+// With a visit for each purpose, unrolled, it took 13 to 23 us; so 11 to 24, of which
+// half went into the keys of logits that the bound now keeps out.)
 template <typename V>
-__device__ __forceinline__ int pick(PickShared &sh, int n, uint64_t least, V visit) {
+__device__ __forceinline__ int pick(PickShared &sh, int n, int n_beams, uint64_t least, V visit) {
+  enum { kList, kKey, kAbove, kPlace, kLast };
+  int mode = kList, bit = 0, more = 0;
   uint32_t last = 0xffffffffu;               // the last place of items with key `least`
-  for (int round = 0;; ++round) {
-    if (threadIdx.x == 0) sh.listed = 0;
+  for (;;) {
+    // items above `over`, and those at `equal` up to place `upto`
+    uint64_t over = least, equal = least;
+    uint32_t upto = last;
+    if (mode == kKey) over = least | 1ull << bit, equal = over, upto = 0xffffffffu;
+    if (mode == kAbove) equal = ~0ull;
+    if (mode == kPlace) over = ~0ull, upto = (last | 1u << bit) - 1;
+    const bool listing = mode == kList || mode == kLast;
+    if (threadIdx.x < n_beams) {
+      // score >= that of `least`: x >= score - s + lse, less what fp64 and fp32 round
+      float bound = -kInf;
+      if (listing && least > 1) {
+        const int b = threadIdx.x;
+        const double t = key_score(least), at = t - sh.s[b] + sh.lse[b];
+        const double off = (__builtin_fabs(t) + __builtin_fabs(sh.s[b]) + __builtin_fabs(sh.lse[b])) * 0x1p-48 +
+                           __builtin_fabs(at) * 0x1p-22;
+        bound = (float)(at - off);
+      }
+      sh.bound[threadIdx.x] = bound;
+    }
+    if (listing && threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
-    visit([&](uint64_t key, uint32_t at) {
-      if (key > least || (key == least && at <= last)) {
-        const int i = atomicAdd(&sh.listed, 1);
-        if (i < kListed) {
-          sh.key[i] = key;
-          sh.at[i] = at;
-        }
+    int hits = 0;
+    visit([&](int b, float x, uint32_t at) {
+      if (x < sh.bound[b]) return;
+      const uint64_t key = order_key(sh.s[b] + ((double)x - sh.lse[b]));
+      if (!(key > over || (key == equal && at <= upto))) return;
+      ++hits;
+      if (!listing) return;
+      const int i = atomicAdd(&sh.listed, 1);
+      if (i < kListed) {
+        sh.key[i] = key;
+        sh.at[i] = at;
       }
     });
-    __syncthreads();
-    if (sh.listed <= kListed || round == 1) break;
-    least = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t k = least | 1ull << bit;
-      if (count_items(sh, visit, [&](uint64_t key, uint32_t) { return key >= k; }) >= n) least = k;
+    if (!listing) {
+      hits = over_wave(hits, [](int a, int b) { return a + b; });
+      if ((threadIdx.x & 63) == 0) sh.hits[threadIdx.x >> 6] = hits;
     }
-    const int more = n - count_items(sh, visit, [&](uint64_t key, uint32_t) { return key > least; });
-    last = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t p = last | 1u << bit;
-      if (count_items(sh, visit, [&](uint64_t key, uint32_t at) { return key == least && at < p; }) < more) last = p;
+    __syncthreads();
+    if (listing) {
+      if (sh.listed <= kListed || mode == kLast) break;
+      mode = kKey;
+      bit = 63;
+      least = 0;
+      __syncthreads();
+      continue;
+    }
+    hits = 0;
+    for (int w = 0; w < kPickThreads / 64; ++w) hits += sh.hits[w];
+    if (mode == kKey) {
+      if (hits >= n) least = over;
+      if (--bit < 0) mode = kAbove;
+    } else if (mode == kAbove) {
+      more = n - hits;                       // items at `least` that are taken
+      mode = kPlace;
+      bit = 31;
+      last = 0;
+    } else {
+      if (hits < more) last |= 1u << bit;
+      if (--bit < 0) mode = kLast;
     }
   }
   const int all = min(sh.listed, kListed);
-  for (int i = threadIdx.x; i < all; i += kPickWaves * 64) {
+  for (int i = threadIdx.x; i < all; i += kPickThreads) {
     const uint64_t key = sh.key[i];
     const uint32_t at = sh.at[i];
     int before = 0;
+#pragma unroll 4
     for (int j = 0; j < all; ++j) before += sh.key[j] > key || (sh.key[j] == key && sh.at[j] < at) ? 1 : 0;
     if (before < n) {
       sh.best_key[before] = key;
@@ -283,94 +340,97 @@ __device__ __forceinline__ int pick(PickShared &sh, int n, uint64_t least, V vis
   return min(all, n);
 }
 
-// Grid: one workgroup a group.  What bounds it: latency, a chain of two reads and
-// four short searches.
+// Grid: one workgroup a group.  What bounds it: latency, a chain of two reads (each
+// whole into LDS first, as far as it fits) and four short searches.
 template <int T>
-__global__ __launch_bounds__(kPickWaves * 64) void beam_pick(BeamArgs a) {
-  constexpr int N = kPerChunk<T>;
-  __shared__ PickShared sh;
+__global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
+  constexpr int N = kPerChunk<T>, CHUNKS = kBlock / N, WAVES = kPickThreads / 64;
+  __shared__ __attribute__((aligned(16))) PickShared sh;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int64_t row0 = (int64_t)blockIdx.x * a.n_beams;
   const int n = a.n_out;
 
-  for (int b = wave; b < a.n_beams; b += kPickWaves) {
+  const float *const maxima = a.block_max + row0 * a.n_blocks;
+  const int n_max = a.n_beams * a.n_blocks;
+  const bool max_held = n_max <= kHeldMax;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n_max && max_held; i += kPickThreads) sh.max[i] = maxima[i];
+  for (int b = wave; b < a.n_beams; b += WAVES) {
     const double *const part = a.part + ((row0 + b) * a.n_splits + lane) * 2;
     const double sum = lane < a.n_splits ? part[0] : 0.0, base = lane < a.n_splits ? part[1] : kNone;
-    double top = base;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmax(top, __shfl_xor(top, d));
-    const double all = wave_sum(sum * exp(base - top));
     const double s = (double)a.scores[row0 + b];
+    const double top = over_wave(base, [](double x, double y) { return fmax(x, y); });
+    const double all = wave_sum(sum * exp(base - top));
     const bool some = all > 0.0 && all < __builtin_inf() && __builtin_fabs(s) < __builtin_inf();
     if (lane == 0) {
       sh.s[b] = some ? s : 0.0;
-      sh.base[b] = top;
-      sh.log_sum[b] = some ? log(all) : __builtin_nan("");
+      sh.lse[b] = some ? top + log(all) : __builtin_nan("");
     }
   }
   __syncthreads();
-  // (the key of a logit, 0 in a beam without candidates: its score is NaN)
-  auto key_of = [&](int b, float x) { return order_key(sh.s[b] + (((double)x - sh.base[b]) - sh.log_sum[b])); };
 
-  // the n-th largest of 64 sets' largest block maxima: n blocks reach it
+  // The n-th largest of 64 sets' largest block maxima: n blocks reach it.  By the upper
+  // half of the keys, which is enough for a key that they reach.
   auto blocks = [&](auto f) {
-    for (int b = wave; b < a.n_beams; b += kPickWaves) {
-      if (sh.log_sum[b] != sh.log_sum[b]) continue;
-      const float *const m = a.block_max + (row0 + b) * a.n_blocks;
-      for (int j = lane; j < a.n_blocks; j += 64) f(key_of(b, m[j]), (uint32_t)(b * a.n_blocks + j));
+    int b = 0, j = threadIdx.x;
+    for (int i = threadIdx.x; i < n_max; i += kPickThreads, j += kPickThreads) {
+      for (; j >= a.n_blocks; j -= a.n_blocks) ++b;
+      f(b, max_held ? sh.max[i] : maxima[i], (uint32_t)i);
     }
   };
-  uint64_t top = 0;
-  blocks([&](uint64_t key, uint32_t) { top = key > top ? key : top; });
+  uint32_t top = 0;
+  blocks([&](int b, float x, uint32_t) {
+    top = max(top, (uint32_t)(order_key(sh.s[b] + ((double)x - sh.lse[b])) >> 32));
+  });
   sh.lane_key[wave][lane] = top;
   __syncthreads();
   if (wave == 0) {
-    for (int w = 1; w < kPickWaves; ++w) top = sh.lane_key[w][lane] > top ? sh.lane_key[w][lane] : top;
-    sh.lane_key[0][lane] = top;
-  }
-  __syncthreads();
-  if (wave == 0) {
-    int above = 0;
-    for (int j = 0; j < 64; ++j) above += sh.lane_key[0][j] > top ? 1 : 0;
-    // the least of those that fewer than n lie above
-    uint64_t least = above < n ? top : ~0ull;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint64_t o = __shfl_xor(least, d);
-      least = o < least ? o : least;
-    }
-    if (lane == 0) sh.least = least > 1 ? least : 1;
-  }
-  __syncthreads();
-  const int n_best = pick(sh, n, sh.least, blocks);
-  // every element of these blocks from the last one's largest on
-  uint32_t mine[kMaxSelected / kPickWaves];
-#pragma unroll
-  for (int i = 0; i < kMaxSelected / kPickWaves; ++i) {
-    const int q = i * kPickWaves + wave;
-    mine[i] = q < n_best ? sh.best_at[q] : 0;
-  }
-  const uint64_t least = n_best == n ? sh.best_key[n - 1] : 1;
-  __syncthreads();
-  auto elements = [&](auto f) {
+    for (int w = 1; w < WAVES; ++w) top = max(top, sh.lane_key[w][lane]);
+    uint32_t least = 0;                      // the largest value that n lanes reach
 #pragma unroll 4
-    for (int i = 0; i < kMaxSelected / kPickWaves; ++i) {
-      if (i * kPickWaves + wave >= n_best) break;
-      const int b = mine[i] / a.n_blocks, c = (mine[i] - b * a.n_blocks) * 64 + lane;
-      const Row<T> r(a, row0 + b);
-      const u32x4_t v = r.load(c, a.vocab);
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t t = least | 1u << bit;
+      if (__popcll(__ballot(top >= t)) >= n) least = t;
+    }
+    if (lane == 0) sh.least = least > 0 ? (uint64_t)least << 32 : 1;
+  }
+  __syncthreads();
+  const int n_best = pick(sh, n, a.n_beams, sh.least, blocks);
+  // every logit of these blocks from the last one's largest on
+  const int n_chunks = n_best * CHUNKS;
+  const bool logits_held = n_best <= kHeldBlocks;
+  const uint64_t least = n_best == n ? sh.best_key[n - 1] : 1;
+  if (threadIdx.x < n_best) {
+    const int at = sh.best_at[threadIdx.x];
+    sh.block_beam[threadIdx.x] = (uint16_t)(at / a.n_blocks);
+    sh.block_in[threadIdx.x] = (uint16_t)(at % a.n_blocks);
+  }
+  __syncthreads();
+  const auto load = [&](int i) {
+    const int q = i / CHUNKS;
+    return Row<T>(a, row0 + sh.block_beam[q]).load(sh.block_in[q] * CHUNKS + i % CHUNKS, a.vocab);
+  };
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n_chunks && logits_held; i += kPickThreads) sh.logits[i] = load(i);
+  // (a thread reads what it has written)
+  auto elements = [&](auto f) {
+    for (int i = threadIdx.x; i < n_chunks; i += kPickThreads) {
+      const u32x4_t v = logits_held ? sh.logits[i] : load(i);
+      const int q = i / CHUNKS, b = sh.block_beam[q];
+      const uint32_t place = (uint32_t)b * (uint32_t)a.vocab + (uint32_t)(sh.block_in[q] * kBlock + i % CHUNKS * N);
+      
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        f(key_of(b, element<T>(v, e)), (uint32_t)b * (uint32_t)a.vocab + (uint32_t)(c * N + e));
+      for (int e = 0; e < N; ++e) f(b, element<T>(v, e), place + e);
     }
   };
-  const int found = n_best > 0 ? pick(sh, n, least, elements) : 0;
+  const int found = n_best > 0 ? pick(sh, n, a.n_beams, least, elements) : 0;
   if (threadIdx.x < n) {
     const int i = threadIdx.x;
     const int64_t o = (int64_t)blockIdx.x * n + i;
     const bool some = i < found;
     const uint32_t at = some ? sh.best_at[i] : 0;
-    a.out_scores[o] = some ? key_score(sh.best_key[i]) : -kInf;
+    a.out_scores[o] = some ? (float)key_score(sh.best_key[i]) : -kInf;
     a.out_parents[o] = some ? (int32_t)(row0 + at / a.vocab) : -1;
     a.out_tokens[o] = some ? (int32_t)(at % a.vocab) : -1;
   }
@@ -378,19 +438,17 @@ __global__ __launch_bounds__(kPickWaves * 64) void beam_pick(BeamArgs a) {
 
 template <int T>
 hipError_t launch(const BeamArgs &a, int64_t n_groups, hipStream_t s) {
-  hipLaunchKernelGGL(beam_scan<T>, dim3((unsigned)(n_groups * a.n_beams * a.n_splits)), dim3(kScanWaves * 64), 0, s, a);
+  const dim3 grid((unsigned)(n_groups * a.n_beams * a.n_splits)), threads(kScanWaves * 64);
+  hipLaunchKernelGGL((beam_scan<T, 4 / kBlockChunks<T>>), grid, threads, 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(beam_pick<T>, dim3((unsigned)n_groups), dim3(kPickWaves * 64), 0, s, a);
+  hipLaunchKernelGGL(beam_pick<T>, dim3((unsigned)n_groups), dim3(kPickThreads), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int32_t beam_blocks(int32_t type, int32_t vocab) {
-  const int n = 64 * (type == HWKV_LOGITS_F32 ? 4 : 8);
-  return (vocab + n - 1) / n;
-}
+int32_t beam_blocks(int32_t vocab) { return (vocab + kBlock - 1) / kBlock; }
 
 // Workgroups a row: enough for every CU, each with a block or more for every wave.
 int32_t beam_splits(int64_t n_rows, int32_t n_blocks) {

@@ -100,7 +100,6 @@ void decode_shared(SharedArgs a) {
   constexpr bool ALONE = CW == 1;      // a wave reads only what it has loaded
   constexpr int EB = KvFormat<F>::kBytes;
   constexpr int WAVES = shared_threads(CW) / 64;
-  constexpr int RW = CW == 4 ? 2 : 4;  // waves of a column group
   constexpr int NC = D / 8;            // chunks of a row
   constexpr int KS = D / 32;           // products over the channels
   constexpr int VB = D / 16;           // channel blocks
@@ -112,8 +111,8 @@ void decode_shared(SharedArgs a) {
   constexpr int STAGE = NT * TB, BUFS = ALONE ? 1 : 2;
   constexpr int LDS = NT * KB / 1024 / WAVES;    // a wave's loads of K, and of V, of a stage
   constexpr int LOADS = 2 * LDS + (I8 ? NT : 0);
-  constexpr int SUB = NT * 4 / RW;     // 16-row parts of a stage that a wave computes,
-  constexpr int P = ALONE ? SUB : SUB > 1 && ROW < 512 ? 2 : 1;   //   at a time
+  constexpr int PARTS = NT * 4;        // 16-row parts of a stage,
+  constexpr int P = ALONE ? NT : 2;    // that a wave computes at a time
   constexpr int CB = 16 * CW;          // columns
   static_assert(BUFS * STAGE >= WAVES * 16 * D * 4, "16 columns of acc a wave, at the end");
   static_assert(STAGE >= CB * D * 2, "the columns of q");
@@ -123,7 +122,6 @@ void decode_shared(SharedArgs a) {
   __shared__ float sml[WAVES][2][16];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int cw = wave / RW, rw = wave % RW;
   const int g4 = lane >> 4, l16 = lane & 15;
   // ---- the item
   const int rank = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.wg_begin[lane] <= (int)blockIdx.x)) - 1);
@@ -160,7 +158,12 @@ void decode_shared(SharedArgs a) {
     if (j >= nwg) return;              // uniform: a shorter sequence
   }
   const int ncols = count * a.group;
-  const bool busy = 16 * cw < ncols;   // whether the wave has columns
+  // Waves share out the columns in groups of 16, and with those of their group the
+  // parts: RW waves take `per` each, wave rw from part rw * per on.
+  const int RW = ALONE ? 4 : ncols <= 16 ? 8 : ncols <= 32 ? 4 : 2;
+  const int cw = wave / RW, rw = wave % RW;
+  const int per = ALONE ? NT : max(PARTS / RW, 1);
+  const bool busy = ALONE || (16 * cw < ncols && rw * per < PARTS);
   const int tile0 = row0 / 64, n_tiles = (end - row0 + 63) / 64;
   const int b0 = a.seq[first];
   const int pto = hd.page0 >= 0 ? hd.page0 + b0 * a.max_pages : -1;
@@ -170,14 +173,23 @@ void decode_shared(SharedArgs a) {
   const uint8_t *const kbase = cache + (hd.k_off + rows0 * D) * EB, *const vbase = cache + (hd.v_off + rows0 * D) * EB;
   const uint8_t *const sbase = I8 ? cache + (int64_t)hd.s_off128 * 128 + rows0 * kRowScaleBytes : cache;
 
+  // The workgroup's i-th tile is tile0 + j + i nwg.  Lane i mod 64 holds its page (a
+  // lookup for every tile, in front of its loads, is a round trip to the L2 each).
+  int pages = 0;
+  auto look_up = [&](int i0) {
+    const int t = tile0 + min(j + (i0 + lane) * nwg, n_tiles - 1);
+    if (pto >= 0) pages = a.page_table[pto + t / (kPageTokens / 64)];
+    // (waited for here, once in 64 tiles, and not wherever it is read)
+    asm volatile("" : "+v"(pages));
+  };
   struct Tile {
     const uint8_t *k, *v, *s;
   };
-  auto tile = [&](int t) -> Tile {
+  auto tile = [&](int i) -> Tile {
     constexpr int TPP = kPageTokens / 64;
+    const int t = tile0 + j + i * nwg;
     if (pto >= 0) {
-      // (a scalar load: a vector one would wait for every load in flight)
-      const int64_t pg = ((const __attribute__((address_space(4))) int32_t *)a.page_table)[pto + t / TPP];
+      const int64_t pg = __builtin_amdgcn_readlane(pages, i & 63);
       const uint8_t *const p = pool + pg * page_elems<F>(D) * EB;
       return {p + t % TPP * KB, p + kPageTokens * ROW + t % TPP * KB,
               p + 2 * kPageTokens * ROW + t % TPP * 64 * kRowScaleBytes};
@@ -208,16 +220,25 @@ void decode_shared(SharedArgs a) {
   for (int n = 0; n < LDS; ++n)
     vl[n] = ALONE ? 16 * wave * ROW + v_offset(n % (LDS / NT)) : v_offset((wave + WAVES * n) % TK);
   const int sl = lane < 32 ? 4 * lane : 1 << 20;
-  auto issue = [&](int lt0, int buf) {
+  // The loads of tiles i0 .. i0 + NT - 1; of those past the last nothing is read.
+  auto issue = [&](int i0, int buf) {
+    if (i0 % 64 == 0 && j + i0 * nwg < n_tiles) look_up(i0);
     const uint32_t to = area0 + buf * STAGE;
-    auto has = [&](int t) { return lt0 + t * nwg < n_tiles; };
-    auto at = [&](int t) { return tile0 + (has(t) ? lt0 + t * nwg : j); };
+    struct Part {
+      Tile at;
+      int rows;
+    };
+    auto of = [&](int t) -> Part {
+      const int lt = j + (i0 + t) * nwg;
+      const Tile at = tile(i0 + t);
+      return {at, lt < n_tiles ? min(64, end - 64 * (tile0 + lt)) : 0};
+    };
     if constexpr (ALONE) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const Tile x = tile(at(t));
-        const __amdgpu_buffer_rsrc_t kr = make_rsrc(x.k, has(t) ? (uint32_t)KB : 0u);
-        const __amdgpu_buffer_rsrc_t vr = make_rsrc(x.v, has(t) ? (uint32_t)(min(64, end - 64 * at(t)) * ROW) : 0u);
+        const Part x = of(t);
+        const __amdgpu_buffer_rsrc_t kr = make_rsrc(x.at.k, x.rows > 0 ? (uint32_t)KB : 0u);
+        const __amdgpu_buffer_rsrc_t vr = make_rsrc(x.at.v, (uint32_t)(x.rows * ROW));
         const uint32_t into = to + t * TB + wave * (KB / 4);
 #pragma unroll
         for (int n = 0; n < TK / 4; ++n) stage_lds<false>(kr, into + n * 1024, kl, n * 4096);
@@ -225,15 +246,16 @@ void decode_shared(SharedArgs a) {
         for (int n = 0; n < TK / 4; ++n) stage_lds<false>(vr, into + KB + n * 1024, vl[n], 0);
         // (every wave has the tile's pairs, in a place of its own)
         if constexpr (I8)
-          stage_lds<true>(make_rsrc(x.s, has(t) ? 64u * kRowScaleBytes : 0u), to + t * TB + 2 * KB + wave * 256, sl, 0);
+          stage_lds<true>(make_rsrc(x.at.s, x.rows > 0 ? 64u * kRowScaleBytes : 0u), to + t * TB + 2 * KB + wave * 256, sl,
+                          0);
       }
     } else {
 #pragma unroll
       for (int n = 0; n < LDS; ++n) {
         const int t = __builtin_amdgcn_readfirstlane((wave + WAVES * n) / TK), i = (wave + WAVES * n) % TK;
-        const Tile x = tile(at(t));
-        const __amdgpu_buffer_rsrc_t kr = make_rsrc(x.k, has(t) ? (uint32_t)KB : 0u);
-        const __amdgpu_buffer_rsrc_t vr = make_rsrc(x.v, has(t) ? (uint32_t)(min(64, end - 64 * at(t)) * ROW) : 0u);
+        const Part x = of(t);
+        const __amdgpu_buffer_rsrc_t kr = make_rsrc(x.at.k, x.rows > 0 ? (uint32_t)KB : 0u);
+        const __amdgpu_buffer_rsrc_t vr = make_rsrc(x.at.v, (uint32_t)(x.rows * ROW));
         const uint32_t into = __builtin_amdgcn_readfirstlane(to + t * TB + i * 1024);
         stage_lds<false>(kr, into, kl, __builtin_amdgcn_readfirstlane(i * 1024));
         stage_lds<false>(vr, into + KB, vl[n], 0);
@@ -242,11 +264,13 @@ void decode_shared(SharedArgs a) {
       // waves have equal numbers of loads)
       if constexpr (I8)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-          stage_lds<true>(make_rsrc(tile(at(t)).s, has(t) ? 64u * kRowScaleBytes : 0u), to + t * TB + 2 * KB, sl, 0);
+        for (int t = 0; t < NT; ++t) {
+          const Part x = of(t);
+          stage_lds<true>(make_rsrc(x.at.s, x.rows > 0 ? 64u * kRowScaleBytes : 0u), to + t * TB + 2 * KB, sl, 0);
+        }
     }
   };
-  issue(j, 0);
+  issue(0, 0);
 
   // ---- q: column c is q head c mod G of the block's member c / G.  Over binary16
   // and int8 rows a column is scaled by a power of two, that of its largest |q|: to
@@ -300,7 +324,7 @@ void decode_shared(SharedArgs a) {
   if constexpr (!ALONE) {
     wait_reads();
     meet();
-    issue(j + NT * nwg, 1);
+    issue(NT, 1);
   }
 
   // ---- the walk.  m: running shift of the lane's column (base 2), raised where a
@@ -311,15 +335,13 @@ void decode_shared(SharedArgs a) {
 #pragma unroll
   for (int vb = 0; vb < VB; ++vb) o[vb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   int buf = 0;
-  for (int lt0 = j; lt0 < n_tiles; lt0 += NT * nwg) {
+  for (int i0 = 0; j + i0 * nwg < n_tiles; i0 += NT) {
     wait_all_but<(BUFS - 1) * LOADS>();
     if constexpr (!ALONE) meet();
     const uint8_t *const sp = area + buf * STAGE;
-#pragma unroll
-    for (int s0 = 0; s0 < SUB; s0 += P) {
-      if (!ALONE && !busy) break;
-      // parts s0 .. s0 + P - 1: rows [16 part, + 16) of tile t
-      constexpr int PT = 4 / RW;       // parts of a tile
+    for (int s0 = 0; busy && s0 < per; s0 += P) {
+      // its parts s0 .. s0 + P - 1: rows [16 part, + 16) of tile t (ALONE: part `wave`
+      // of every tile)
       u32x4_t kf[CODES ? 1 : P][KS];
       u32x2_t kc[CODES ? P : 1][KS];
       u32x2_t vf[CODES ? 1 : P][VB];
@@ -328,10 +350,11 @@ void decode_shared(SharedArgs a) {
       int left[P];                     // of the lane's rows, from its first on
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        const int t = (s0 + p) / PT, part = rw * PT + (s0 + p) % PT;
+        const int x = rw * per + min(s0 + p, per - 1);
+        const int t = ALONE ? p : x / 4, part = ALONE ? wave : x % 4;
         const uint8_t *const at = sp + t * TB;
-        const int lt = lt0 + t * nwg;
-        left[p] = lt < n_tiles ? end - (64 * (tile0 + lt) + 16 * part + 4 * g4) : 0;
+        const int lt = j + (i0 + t) * nwg;
+        left[p] = lt < n_tiles && s0 + p < per ? end - (64 * (tile0 + lt) + 16 * part + 4 * g4) : 0;
         if constexpr (I8)
           pairs[p] = *reinterpret_cast<const u32x2_t *>(at + 2 * KB + (ALONE ? wave * 256 : 0) + 32 * part + 8 * g4);
         const uint8_t *const v = at + KB + part * (KB / 4);
@@ -363,20 +386,29 @@ void decode_shared(SharedArgs a) {
       }
       if constexpr (ALONE) {
         wait_reads();
-        issue(lt0 + NT * nwg, 0);
+        issue(i0 + NT, 0);
       }
 
-      // logits
-      f32x4_t z[P];
+      // logits (a product that adds to the one before it waits out its latency: two
+      // sums where there is one part)
+      constexpr int CH = P == 1 ? 2 : 1;
+      f32x4_t z[P], zz[P][CH];
 #pragma unroll
-      for (int p = 0; p < P; ++p) z[p] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) zz[p][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < KS; ++i)
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-          if constexpr (CODES) z[p] = product<F>(widen_codes<F>(kc[p][i]), q[i], z[p]);
-          else z[p] = product<F>(kf[p][i], q[i], z[p]);
+          if constexpr (CODES) zz[p][i % CH] = product<F>(widen_codes<F>(kc[p][i]), q[i], zz[p][i % CH]);
+          else zz[p][i % CH] = product<F>(kf[p][i], q[i], zz[p][i % CH]);
         }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        z[p] = zz[p][0];
+        if constexpr (CH == 2) z[p] += zz[p][1];
+      }
       // (rows past the item's end have no weight)
       float top = -FLT_MAX;
 #pragma unroll
@@ -403,7 +435,7 @@ void decode_shared(SharedArgs a) {
         float w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          w[i] = exp2f(z[p][i] - m);
+          w[i] = __builtin_amdgcn_exp2f(z[p][i] - m);
           lsum += w[i];
           if constexpr (F16) w[i] *= 0x1p7f;       // clear of binary16's subnormals
           // 2^-12 centres the range of weights times row scales
@@ -430,55 +462,56 @@ void decode_shared(SharedArgs a) {
           }
         }
       }
-      // values
-      auto add = [&](int vb, const u32x2_t (&v)[P]) {
+      // values: term by term over two parts; of a single part, the first two terms over
+      // the same V, then the third.  (The product of 16 places takes as long as that of
+      // 32; and compiled right behind one of 32 into the same accumulator, with no wait
+      // between, it gave wrong sums.)
+      constexpr int TERMS = F16 ? 2 : 3, STEPS = P == 1 ? TERMS - 1 : TERMS;
+      auto add = [&](int step, int vb, const u32x2_t (&v)[P]) {
+        if constexpr (P == 1) {
+          const u32x2_t x = term[0][2 * step], y = step == 0 ? term[0][1] : u32x2_t{0u, 0u};
+          o[vb] = product<F>(u32x4_t{v[0].x, v[0].y, v[0].x, v[0].y}, u32x4_t{x.x, x.y, y.x, y.y}, o[vb]);
+        } else {
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const u32x2_t x = term[p][0], y = term[p][1];
-          o[vb] = product<F>(u32x4_t{v[p].x, v[p].y, v[p].x, v[p].y}, u32x4_t{x.x, x.y, y.x, y.y}, o[vb]);
-        }
-        if constexpr (!F16) {
-          // (The product of 16 places takes as long as that of 32; and compiled right
-          // behind one of 32 into the same accumulator, with no wait between, it gave
-          // wrong sums.)
-          if constexpr (P == 1) {
-            const u32x2_t x = term[0][2];
-            o[vb] = product<F>(u32x4_t{v[0].x, v[0].y, v[0].x, v[0].y}, u32x4_t{x.x, x.y, 0u, 0u}, o[vb]);
-          } else {
-#pragma unroll
-            for (int p = 0; p < P; p += 2) {
-              const u32x2_t x = term[p][2], y = term[p + 1][2];
-              o[vb] = product<F>(u32x4_t{v[p].x, v[p].y, v[p + 1].x, v[p + 1].y}, u32x4_t{x.x, x.y, y.x, y.y}, o[vb]);
-            }
+          for (int p = 0; p < P; p += 2) {
+            const u32x2_t x = term[p][step], y = term[p + 1][step];
+            o[vb] = product<F>(u32x4_t{v[p].x, v[p].y, v[p + 1].x, v[p + 1].y}, u32x4_t{x.x, x.y, y.x, y.y}, o[vb]);
           }
         }
       };
       if constexpr (CODES) {
         static_for<4>([&](auto ec) {
           constexpr int e = decltype(ec)::value;
+          u32x2_t v[D / 64][P];
 #pragma unroll
-          for (int i = 0; i < D / 64; ++i) {
-            u32x2_t v[P];
+          for (int i = 0; i < D / 64; ++i)
 #pragma unroll
             for (int p = 0; p < P; ++p)
-              v[p] = u32x2_t{pair_of_codes<F, e>(vc[p][i][0], vc[p][i][1]), pair_of_codes<F, e>(vc[p][i][2], vc[p][i][3])};
-            add(4 * i + e, v);
-          }
+              v[i][p] = u32x2_t{pair_of_codes<F, e>(vc[p][i][0], vc[p][i][1]), pair_of_codes<F, e>(vc[p][i][2], vc[p][i][3])};
+#pragma unroll
+          for (int step = 0; step < STEPS; ++step)
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) add(step, 4 * i + e, v[i]);
         });
       } else {
+        u32x2_t v[VB][P];
 #pragma unroll
-        for (int vb = 0; vb < VB; ++vb) {
-          u32x2_t v[P];
+        for (int vb = 0; vb < VB; ++vb)
 #pragma unroll
-          for (int p = 0; p < P; ++p) v[p] = vf[p][vb];
-          add(vb, v);
-        }
+          for (int p = 0; p < P; ++p) v[vb][p] = vf[p][vb];
+        // (in runs of 8 blocks: a product that adds to the one before it waits)
+#pragma unroll
+        for (int v0 = 0; v0 < VB; v0 += 8)
+#pragma unroll
+          for (int step = 0; step < STEPS; ++step)
+#pragma unroll
+            for (int vb = v0; vb < VB && vb < v0 + 8; ++vb) add(step, vb, v[vb]);
       }
     }
     if constexpr (!ALONE) {
       wait_reads();
       meet();                          // nobody reads this stage any more
-      issue(lt0 + 2 * NT * nwg, buf);
+      issue(i0 + 2 * NT, buf);
       buf ^= 1;
     }
   }
@@ -519,11 +552,10 @@ void decode_shared(SharedArgs a) {
   for (int idx = threadIdx.x; idx < ncols * (D / 4); idx += WAVES * 64) {
     const int col = idx / (D / 4), at = idx % (D / 4), c = col % 16, w0 = col / 16 * RW;
     float M = sml[w0][0][c];
-#pragma unroll
     for (int w = 1; w < RW; ++w) M = fmaxf(M, sml[w0 + w][0][c]);
     float L = 0.f;
     f32x4_t A = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+#pragma unroll 4
     for (int w = 0; w < RW; ++w) {
       const float f = exp2f(sml[w0 + w][0][c] - M);
       L += sml[w0 + w][1][c] * f;

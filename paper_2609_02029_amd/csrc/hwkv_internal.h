@@ -350,7 +350,7 @@ struct BeamArgs {
   int32_t *out_parents, *out_tokens;
   int32_t vocab, n_beams, n_out, n_blocks, n_splits;
 };
-int32_t beam_blocks(int32_t type, int32_t vocab);
+int32_t beam_blocks(int32_t vocab);   // of a row
 int32_t beam_splits(int64_t n_rows, int32_t n_blocks);
 hipError_t launch_beam_select(int32_t type, const BeamArgs &a, int64_t n_groups, hipStream_t s);
 
