@@ -30,6 +30,7 @@ constexpr double kLog2e = 0x1.71547652b82fep+0;
 constexpr float kInf = __builtin_inff();
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef u32x4_t __attribute__((aligned(2))) chunk_t;
 
 template <int T>
@@ -49,6 +50,15 @@ __device__ __forceinline__ float element(const u32x4_t &c, int e) {
     if constexpr (T == HWKV_LOGITS_BF16) return __uint_as_float(u << 16);
     return (float)__builtin_bit_cast(_Float16, (uint16_t)u);
   }
+}
+
+// Token t of a row.
+template <int T>
+__device__ __forceinline__ float logit(const BeamArgs &a, int64_t row, uint32_t t) {
+  const uint8_t *const at = static_cast<const uint8_t *>(a.logits) + (row * a.stride + t) * kBytes<T>;
+  if constexpr (T == HWKV_LOGITS_F32) return *reinterpret_cast<const float *>(at);
+  const u32x4_t v = {*reinterpret_cast<const uint16_t *>(at), 0u, 0u, 0u};
+  return element<T>(v, 0);
 }
 
 // A row's chunks of 16 bytes, from its first logit on.  (Rows of an odd vocabulary
@@ -224,213 +234,242 @@ __device__ __forceinline__ double key_score(uint64_t key) {
 }
 
 constexpr int kPickThreads = 512, kListed = 1024;
-constexpr int kHeldMax = 8192;       // block maxima that a workgroup keeps in LDS,
-constexpr int kHeldBlocks = 16;      //   and blocks of logits
+constexpr int kHeld = 8192;          // logits that a workgroup keeps in LDS
 
-struct PickShared {
-  double s[kMaxBeams], lse[kMaxBeams];       // lse NaN: a beam without candidates
-  float bound[kMaxBeams];                    // below every logit of the beam that is asked for
-  uint64_t key[kListed];
-  uint32_t at[kListed];
-  uint32_t lane_key[kPickThreads / 64][64];
-  uint64_t best_key[kMaxSelected];
-  uint32_t best_at[kMaxSelected];
-  uint16_t block_beam[kMaxSelected];         // of the blocks whose logits are read
-  uint16_t block_in[kMaxSelected];
-  uint64_t least;
-  int listed, hits[kPickThreads / 64];
-  union {
-    float max[kHeldMax];
-    u32x4_t logits[kHeldBlocks * kBlock / 4];
-  };
+// A run of a search's list: consecutive places of one beam.
+struct Run {
+  uint32_t beam, place;
+  float bound;                       // below every logit that is asked for
+  uint32_t unused;
 };
 
-// The n first items in the order (key falling, place rising) of those that `visit`
-// gives (its argument is called with a beam, a logit and a place), into best_key /
-// best_at; returns how many there are.  `least`: a key that at least n items reach (or
-// 1).  The items from there on are listed and counted against each other; a bound for
-// the beam's logits keeps all others out with one comparison.  Where the list does not
-// hold them (long runs of equal or rising logits), the n-th key, how many lie above it
-// and then the n-th item's place are found bit by bit first.
+// Grid: one workgroup a group.  Two searches for the n first of a list, in the order
+// (score falling, place rising): of the beams' block maxima, then of the logits of the
+// n blocks found; each list goes into LDS, as far as it fits, in quads.  A score that n
+// items reach is known before a search (of 64 sets' largest maxima the n-th largest;
+// the n-th block's), so one comparison of logits with a bound keeps nearly all out,
+// and what passes is listed, given its 64-bit key, and counted against each other.
+// Where the list does not hold them (long runs of equal or rising logits), the n-th
+// key, how many lie above it and then the n-th item's place are found bit by bit first.
 //
-// (One visit in a loop, whatever it is for: the kernel runs through its code once.
-// With a visit for each purpose, unrolled, it took 13 to 23 us; so 11 to 24, of which
-// half went into the keys of logits that the bound now keeps out.)
-template <typename V>
-__device__ __forceinline__ int pick(PickShared &sh, int n, int n_beams, uint64_t least, V visit) {
-  enum { kList, kKey, kAbove, kPlace, kLast };
-  int mode = kList, bit = 0, more = 0;
-  uint32_t last = 0xffffffffu;               // the last place of items with key `least`
-  for (;;) {
-    // items above `over`, and those at `equal` up to place `upto`
-    uint64_t over = least, equal = least;
-    uint32_t upto = last;
-    if (mode == kKey) over = least | 1ull << bit, equal = over, upto = 0xffffffffu;
-    if (mode == kAbove) equal = ~0ull;
-    if (mode == kPlace) over = ~0ull, upto = (last | 1u << bit) - 1;
-    const bool listing = mode == kList || mode == kLast;
-    if (threadIdx.x < n_beams) {
-      // score >= that of `least`: x >= score - s + lse, less what fp64 and fp32 round
-      float bound = -kInf;
-      if (listing && least > 1) {
-        const int b = threadIdx.x;
-        const double t = key_score(least), at = t - sh.s[b] + sh.lse[b];
-        const double off = (__builtin_fabs(t) + __builtin_fabs(sh.s[b]) + __builtin_fabs(sh.lse[b])) * 0x1p-48 +
-                           __builtin_fabs(at) * 0x1p-22;
-        bound = (float)(at - off);
-      }
-      sh.bound[threadIdx.x] = bound;
-    }
-    if (listing && threadIdx.x == 0) sh.listed = 0;
-    __syncthreads();
-    int hits = 0;
-    visit([&](int b, float x, uint32_t at) {
-      if (x < sh.bound[b]) return;
-      const uint64_t key = order_key(sh.s[b] + ((double)x - sh.lse[b]));
-      if (!(key > over || (key == equal && at <= upto))) return;
-      ++hits;
-      if (!listing) return;
-      const int i = atomicAdd(&sh.listed, 1);
-      if (i < kListed) {
-        sh.key[i] = key;
-        sh.at[i] = at;
-      }
-    });
-    if (!listing) {
-      hits = over_wave(hits, [](int a, int b) { return a + b; });
-      if ((threadIdx.x & 63) == 0) sh.hits[threadIdx.x >> 6] = hits;
-    }
-    __syncthreads();
-    if (listing) {
-      if (sh.listed <= kListed || mode == kLast) break;
-      mode = kKey;
-      bit = 63;
-      least = 0;
-      __syncthreads();
-      continue;
-    }
-    hits = 0;
-    for (int w = 0; w < kPickThreads / 64; ++w) hits += sh.hits[w];
-    if (mode == kKey) {
-      if (hits >= n) least = over;
-      if (--bit < 0) mode = kAbove;
-    } else if (mode == kAbove) {
-      more = n - hits;                       // items at `least` that are taken
-      mode = kPlace;
-      bit = 31;
-      last = 0;
-    } else {
-      if (hits < more) last |= 1u << bit;
-      if (--bit < 0) mode = kLast;
-    }
-  }
-  const int all = min(sh.listed, kListed);
-  for (int i = threadIdx.x; i < all; i += kPickThreads) {
-    const uint64_t key = sh.key[i];
-    const uint32_t at = sh.at[i];
-    int before = 0;
-#pragma unroll 4
-    for (int j = 0; j < all; ++j) before += sh.key[j] > key || (sh.key[j] == key && sh.at[j] < at) ? 1 : 0;
-    if (before < n) {
-      sh.best_key[before] = key;
-      sh.best_at[before] = at;
-    }
-  }
-  __syncthreads();
-  return min(all, n);
-}
-
-// Grid: one workgroup a group.  What bounds it: latency, a chain of two reads (each
-// whole into LDS first, as far as it fits) and four short searches.
+// What bounds it: latency, of two reads of what other XCDs wrote or left in memory
+// (about 1.5 us each) and some twenty steps through LDS.  24 groups of 4 beams, 131,072
+// logits: with keys formed for every logit and a visit's code for each purpose 15 us,
+// one visit for all purposes 13.6, a bound in front of the keys 9.5.
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
-  constexpr int N = kPerChunk<T>, CHUNKS = kBlock / N, WAVES = kPickThreads / 64;
-  __shared__ __attribute__((aligned(16))) PickShared sh;
+  constexpr int N = kPerChunk<T>, WAVES = kPickThreads / 64;
+  __shared__ double s_s[kMaxBeams], lse_s[kMaxBeams];        // lse NaN: a beam without candidates
+  __shared__ __attribute__((aligned(16))) Run run_s[kMaxBeams];
+  __shared__ float x_s[kListed];
+  __shared__ uint32_t beam_s[kListed], at_s[kListed];
+  __shared__ uint64_t key_s[kListed];
+  __shared__ float lane_top[WAVES][64];
+  __shared__ uint64_t best_key[kMaxSelected];
+  __shared__ uint32_t best_at[kMaxSelected];
+  __shared__ float floor_s;
+  __shared__ int listed, hits_s[WAVES];
+  __shared__ __attribute__((aligned(16))) float value_s[kHeld];
+  static_assert(kMaxSelected <= kMaxBeams, "a run per beam, or per block");
+
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int64_t row0 = (int64_t)blockIdx.x * a.n_beams;
   const int n = a.n_out;
 
-  const float *const maxima = a.block_max + row0 * a.n_blocks;
-  const int n_max = a.n_beams * a.n_blocks;
-  const bool max_held = n_max <= kHeldMax;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n_max && max_held; i += kPickThreads) sh.max[i] = maxima[i];
-  for (int b = wave; b < a.n_beams; b += WAVES) {
+  // sums and block maxima
+  int runs = a.n_beams, items = a.n_blocks;  // of the list, and the items of each
+  int quads = (items + 3) / 4;
+  bool held = runs * quads * 4 <= kHeld;
+  // an item of a list that is not held, or is to be
+  const auto maximum = [&](int r, int j) {
+    return j < a.n_blocks ? a.block_max[(row0 + r) * a.n_blocks + j] : -kInf;
+  };
+  double part_sum = 0.0, part_base = kNone, part_s = 0.0;
+  const auto load_parts = [&](int b) {
     const double *const part = a.part + ((row0 + b) * a.n_splits + lane) * 2;
-    const double sum = lane < a.n_splits ? part[0] : 0.0, base = lane < a.n_splits ? part[1] : kNone;
-    const double s = (double)a.scores[row0 + b];
-    const double top = over_wave(base, [](double x, double y) { return fmax(x, y); });
-    const double all = wave_sum(sum * exp(base - top));
-    const bool some = all > 0.0 && all < __builtin_inf() && __builtin_fabs(s) < __builtin_inf();
+    if (lane < a.n_splits) part_sum = part[0], part_base = part[1];
+    part_s = (double)a.scores[row0 + b];
+  };
+  if (wave < a.n_beams) load_parts(wave);
+  if (held) {
+#pragma unroll 2
+    for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
+      const int r = i / quads, j = (i - r * quads) * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) value_s[4 * i + e] = maximum(r, j + e);
+    }
+  }
+  for (int b = wave; b < a.n_beams; b += WAVES) {
+    if (b != wave) load_parts(b);
+    const double top = over_wave(part_base, [](double x, double y) { return fmax(x, y); });
+    const double all = wave_sum(part_sum * exp(part_base - top));
+    const bool some = all > 0.0 && all < __builtin_inf() && __builtin_fabs(part_s) < __builtin_inf();
     if (lane == 0) {
-      sh.s[b] = some ? s : 0.0;
-      sh.lse[b] = some ? top + log(all) : __builtin_nan("");
+      s_s[b] = some ? part_s : 0.0;
+      lse_s[b] = some ? top + log(all) : __builtin_nan("");
+      run_s[b].beam = b;
+      run_s[b].place = b * a.n_blocks;
     }
   }
   __syncthreads();
+  const auto score_of = [&](int b, float x) { return s_s[b] + ((double)x - lse_s[b]); };
 
-  // The n-th largest of 64 sets' largest block maxima: n blocks reach it.  By the upper
-  // half of the keys, which is enough for a key that they reach.
-  auto blocks = [&](auto f) {
-    int b = 0, j = threadIdx.x;
-    for (int i = threadIdx.x; i < n_max; i += kPickThreads, j += kPickThreads) {
-      for (; j >= a.n_blocks; j -= a.n_blocks) ++b;
-      f(b, max_held ? sh.max[i] : maxima[i], (uint32_t)i);
+  // A score that n blocks reach, from fp32 roundings: the n-th largest of 64 sets'
+  // largest (minus infinity: fewer have one).
+  {
+    float top = -kInf;
+    for (int i = threadIdx.x, r = 0, j = threadIdx.x; i < runs * quads; i += kPickThreads, j += kPickThreads) {
+      for (; j >= quads; j -= quads) ++r;
+      const f32x4_t v = held ? *reinterpret_cast<const f32x4_t *>(value_s + 4 * i)
+                             : f32x4_t{maximum(r, 4 * j), maximum(r, 4 * j + 1), maximum(r, 4 * j + 2), maximum(r, 4 * j + 3)};
+      // (fmaxf passes over the NaN of a beam without candidates)
+      top = fmaxf(top, (float)score_of(r, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))));
     }
-  };
-  uint32_t top = 0;
-  blocks([&](int b, float x, uint32_t) {
-    top = max(top, (uint32_t)(order_key(sh.s[b] + ((double)x - sh.lse[b])) >> 32));
-  });
-  sh.lane_key[wave][lane] = top;
-  __syncthreads();
-  if (wave == 0) {
+    lane_top[wave][lane] = top;
+    __syncthreads();
+    if (wave == 0) {
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) top = max(top, sh.lane_key[w][lane]);
-    uint32_t least = 0;                      // the largest value that n lanes reach
-#pragma unroll 4
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t t = least | 1u << bit;
-      if (__popcll(__ballot(top >= t)) >= n) least = t;
-    }
-    if (lane == 0) sh.least = least > 0 ? (uint64_t)least << 32 : 1;
-  }
-  __syncthreads();
-  const int n_best = pick(sh, n, a.n_beams, sh.least, blocks);
-  // every logit of these blocks from the last one's largest on
-  const int n_chunks = n_best * CHUNKS;
-  const bool logits_held = n_best <= kHeldBlocks;
-  const uint64_t least = n_best == n ? sh.best_key[n - 1] : 1;
-  if (threadIdx.x < n_best) {
-    const int at = sh.best_at[threadIdx.x];
-    sh.block_beam[threadIdx.x] = (uint16_t)(at / a.n_blocks);
-    sh.block_in[threadIdx.x] = (uint16_t)(at % a.n_blocks);
-  }
-  __syncthreads();
-  const auto load = [&](int i) {
-    const int q = i / CHUNKS;
-    return Row<T>(a, row0 + sh.block_beam[q]).load(sh.block_in[q] * CHUNKS + i % CHUNKS, a.vocab);
-  };
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n_chunks && logits_held; i += kPickThreads) sh.logits[i] = load(i);
-  // (a thread reads what it has written)
-  auto elements = [&](auto f) {
-    for (int i = threadIdx.x; i < n_chunks; i += kPickThreads) {
-      const u32x4_t v = logits_held ? sh.logits[i] : load(i);
-      const int q = i / CHUNKS, b = sh.block_beam[q];
-      const uint32_t place = (uint32_t)b * (uint32_t)a.vocab + (uint32_t)(sh.block_in[q] * kBlock + i % CHUNKS * N);
-      
+      for (int w = 1; w < WAVES; ++w) top = fmaxf(top, lane_top[w][lane]);
+      int above = 0;
 #pragma unroll
-      for (int e = 0; e < N; ++e) f(b, element<T>(v, e), place + e);
+      for (int l = 0; l < 64; ++l)
+        above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), l)) > top ? 1 : 0;
+      const float least = over_wave(above < n ? top : kInf, [](float x, float y) { return fminf(x, y); });
+      if (lane == 0) floor_s = least;
     }
-  };
-  const int found = n_best > 0 ? pick(sh, n, a.n_beams, least, elements) : 0;
+    __syncthreads();
+  }
+  double floor = (double)floor_s;            // (rounded: less a step)
+  floor -= __builtin_fabs(floor) * 0x1p-23;
+
+  int found = 0;
+  for (int search = 0;; ++search) {
+    // score >= floor: x >= floor - s + lse, less what fp64 and fp32 round
+    const auto set_bounds = [&](bool any) {
+      if (threadIdx.x < runs) {
+        const int b = run_s[threadIdx.x].beam;
+        const double s = s_s[b], lse = lse_s[b], x = floor - s + lse;
+        const double off = (__builtin_fabs(floor) + __builtin_fabs(s) + __builtin_fabs(lse)) * 0x1p-48 +
+                           __builtin_fabs(x) * 0x1p-22;
+        // (of a beam without candidates nothing, of a floor of minus infinity all)
+        run_s[threadIdx.x].bound = lse != lse ? kInf : any || floor == -__builtin_inf() ? -__FLT_MAX__ : (float)(x - off);
+      }
+      if (threadIdx.x == 0) listed = 0;
+      __syncthreads();
+    };
+    // every item that its run's bound lets pass
+    const auto visit = [&](auto f) {
+      for (int i = threadIdx.x, r = 0, j = threadIdx.x; i < runs * quads; i += kPickThreads, j += kPickThreads) {
+        for (; j >= quads; j -= quads) ++r;
+        const Run run = run_s[r];
+        f32x4_t v;
+        if (held) {
+          v = *reinterpret_cast<const f32x4_t *>(value_s + 4 * i);
+        } else {
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t t = run.place + 4 * j + e - run.beam * (uint32_t)a.vocab;
+            v[e] = search == 0 ? maximum(r, 4 * j + e) : t < (uint32_t)a.vocab ? logit<T>(a, row0 + run.beam, t) : -kInf;
+          }
+        }
+        if (!(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= run.bound)) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v[e] >= run.bound) f(run.beam, v[e], run.place + 4 * j + e);
+      }
+    };
+    const auto list = [&](int b, float x, uint32_t at) {
+      const int l = atomicAdd(&listed, 1);
+      if (l < kListed) {
+        x_s[l] = x;
+        beam_s[l] = b;
+        at_s[l] = at;
+      }
+    };
+    set_bounds(false);
+    visit(list);
+    __syncthreads();
+    if (listed > kListed) {
+      // the n-th key `least`, then the place `last` of the n-th item
+      __syncthreads();
+      set_bounds(true);
+      uint64_t least = 0;
+      uint32_t last = 0;
+      int more = 0;
+      for (int step = 0; step < 64 + 1 + 32; ++step) {
+        // items above `over`, and those at `equal` below place `upto`
+        uint64_t over = least, equal = ~0ull;
+        uint32_t upto = 0;
+        if (step < 64) over = (least | 1ull << (63 - step)) - 1;
+        if (step > 64) over = ~0ull, equal = least, upto = last | 1u << (96 - step);
+        int hits = 0;
+        visit([&](int b, float x, uint32_t at) {
+          const uint64_t key = order_key(score_of(b, x));
+          hits += key > over || (key == equal && at < upto) ? 1 : 0;
+        });
+        hits = over_wave(hits, [](int x, int y) { return x + y; });
+        __syncthreads();
+        if (lane == 0) hits_s[wave] = hits;
+        __syncthreads();
+        hits = 0;
+        for (int w = 0; w < WAVES; ++w) hits += hits_s[w];
+        if (step < 64) least = hits >= n ? over + 1 : least;
+        else if (step == 64) more = n - hits;          // items at `least` that are taken
+        else last = hits < more ? upto : last;
+      }
+      visit([&](int b, float x, uint32_t at) {
+        const uint64_t key = order_key(score_of(b, x));
+        if (key > least || (key == least && at <= last)) list(b, x, at);
+      });
+      __syncthreads();
+    }
+    const int all = min(listed, kListed);
+    for (int i = threadIdx.x; i < all; i += kPickThreads) key_s[i] = order_key(score_of(beam_s[i], x_s[i]));
+    __syncthreads();
+    for (int i = threadIdx.x; i < all; i += kPickThreads) {
+      const uint64_t key = key_s[i];
+      const uint32_t at = at_s[i];
+      int before = 0;
+#pragma unroll 4
+      for (int j = 0; j < all; ++j) {
+        const uint64_t k = key_s[j];
+        const uint32_t p = at_s[j];
+        before += (k > key) | ((k == key) & (p < at));
+      }
+      if (before < n) {
+        best_key[before] = key;
+        best_at[before] = at;
+      }
+    }
+    __syncthreads();
+    found = min(all, n);
+    if (search == 1 || found == 0) break;
+    // next: the logits of these blocks, from the last one's largest on
+    floor = found == n ? key_score(best_key[n - 1]) : -__builtin_inf();
+    runs = found;
+    quads = kBlock / 4;
+    held = runs * kBlock <= kHeld;
+    if (threadIdx.x < runs) {
+      const int at = best_at[threadIdx.x], b = at / a.n_blocks;
+      run_s[threadIdx.x].beam = b;
+      run_s[threadIdx.x].place = (uint32_t)b * a.vocab + (at - b * a.n_blocks) * kBlock;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int i = threadIdx.x; i < runs * (kBlock / N) && held; i += kPickThreads) {
+      const Run run = run_s[i / (kBlock / N)];
+      const u32x4_t v = Row<T>(a, row0 + run.beam)
+                            .load((int)(run.place - run.beam * (uint32_t)a.vocab) / N + i % (kBlock / N), a.vocab);
+#pragma unroll
+      for (int e = 0; e < N; ++e) value_s[i * N + e] = element<T>(v, e);
+    }
+    __syncthreads();
+  }
   if (threadIdx.x < n) {
     const int i = threadIdx.x;
     const int64_t o = (int64_t)blockIdx.x * n + i;
     const bool some = i < found;
-    const uint32_t at = some ? sh.best_at[i] : 0;
-    a.out_scores[o] = some ? (float)key_score(sh.best_key[i]) : -kInf;
+    const uint32_t at = some ? best_at[i] : 0;
+    a.out_scores[o] = some ? (float)key_score(best_key[i]) : -kInf;
     a.out_parents[o] = some ? (int32_t)(row0 + at / a.vocab) : -1;
     a.out_tokens[o] = some ? (int32_t)(at % a.vocab) : -1;
   }
