@@ -564,7 +564,7 @@ int hwkv_beam_workspace_bytes(int64_t n_groups, int32_t n_beams, int32_t vocab,
  * of row r = group * n_beams + beam and its running score s,
  *   lse[r] = log sum_t e^x[r][t],  score(r, t) = s[r] + (x[r][t] - lse[r]):
  * the n_out largest scores of the group's rows and tokens, falling; equal ones go
- * to the lowest (r, t).  Sums and scores are formed in 64 bits (lse to 2e-12) and
+ * to the lowest (r, t).  Sums and scores are formed in 64 bits (lse to 1e-10) and
  * order by these; the outputs are rounded to fp32.
  *   logits       device, n_groups * n_beams rows of vocab elements of `type`,
  *                `stride` elements apart, aligned to their elements

@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kScanWaves = 4;
 constexpr int kBlock = 512;          // logits of a block: 8 a lane
-constexpr double kLog2e = 0x1.71547652b82fep+0;
+constexpr double kLog2e = 0x1.71547652b82fep+0, kLn2 = 0x1.62e42fefa39efp-1;
 constexpr float kInf = __builtin_inff();
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -131,8 +131,9 @@ __device__ __forceinline__ V over_wave(V x, F op) {
   rows([](uint32_t u) { return __builtin_amdgcn_permlane32_swap(u, u, false, false); });
   return x;
 }
+__device__ __forceinline__ float most(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float wave_max(float x) {
-  return over_wave(x, [](float a, float b) { return fmaxf(a, b); });
+  return over_wave(x, [](float a, float b) { return most(a, b); });
 }
 __device__ __forceinline__ double wave_sum(double x) {
   return over_wave(x, [](double a, double b) { return a + b; });
@@ -140,19 +141,17 @@ __device__ __forceinline__ double wave_sum(double x) {
 
 // 2^f on [-1/2, 1/2].
 __device__ __forceinline__ double exp2_small(double f) {
-  double p = 0x1.63d1363930791p-20;
-  p = __builtin_fma(p, f, 0x1.00dc4a53395d3p-16);
-  p = __builtin_fma(p, f, 0x1.4308ac85a7718p-13);
-  p = __builtin_fma(p, f, 0x1.5d8745a72831bp-10);
-  p = __builtin_fma(p, f, 0x1.3b2ab7181b778p-7);
-  p = __builtin_fma(p, f, 0x1.c6b08dd6fd236p-5);
-  p = __builtin_fma(p, f, 0x1.ebfbdff823cedp-3);
-  p = __builtin_fma(p, f, 0x1.62e42fef84cf0p-1);
-  return __builtin_fma(p, f, 1.0);
+  double p = 0x1.00c0e4e155dc0p-16;
+  p = __builtin_fma(p, f, 0x1.446c79efd4eb1p-13);
+  p = __builtin_fma(p, f, 0x1.5d8775983506fp-10);
+  p = __builtin_fma(p, f, 0x1.3b29d8bb0b975p-7);
+  p = __builtin_fma(p, f, 0x1.c6b08da70cce3p-5);
+  p = __builtin_fma(p, f, 0x1.ebfbe0aa03df0p-3);
+  p = __builtin_fma(p, f, 0x1.62e42fef9cc69p-1);
+  return __builtin_fma(p, f, 0x1.ffffffffa7135p-1);
 }
 
-// A sum of e^x as sum * e^base, base a logit (kNone where there is none): x - base is
-// exact, also far from zero.
+// A sum of e^x as sum * e^base (base kNone where there is none).
 constexpr double kNone = -0x1p1000;
 struct Sum {
   double sum, base;
@@ -170,10 +169,14 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
   const Row<T> r(a, row);
   float *const block_max = a.block_max + row * a.n_blocks;
   const int step = kScanWaves * a.n_splits;
-  // e^(x - base), summed; the base is the largest logit of the first block that has
-  // one, and of a block whose largest passes it by 600.  A logit more than 690 below
-  // it counts as that (e^-690).
-  double sum = 0.0, base = kNone;
+  // e^(x - base), summed; the base is set by the largest logit of the first block that
+  // has one, and of a block whose largest passes it by 600, and a logit more than 690
+  // below it counts as that (e^-690).  Logits up to 2^16 take base = shift ln 2 with a
+  // whole shift, so that x log2 e needs no difference first; others a logit as their
+  // base, from which they differ exactly.
+  double sum = 0.0, base = kNone, shift = 0.0;
+  float lowest = 0.0f;                       // base - 690
+  bool near = true;
   for (int b0 = split * kScanWaves + wave; b0 < a.n_blocks; b0 += DEEP * step) {
     u32x4_t v[DEEP][C];
 #pragma unroll
@@ -187,9 +190,12 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
       float x[C * N];
 #pragma unroll
       for (int e = 0; e < C * N; ++e) x[e] = element<T>(v[i][e / N], e % N);
-      float top = x[0];
+      float top = x[0], low = x[0];
 #pragma unroll
-      for (int e = 1; e < C * N; ++e) top = __builtin_elementwise_maximum(top, x[e]);   // (NaN if any is)
+      for (int e = 1; e < C * N; ++e) {
+        top = most(top, x[e]);               // (NaN if any is)
+        low = __builtin_elementwise_minimum(low, x[e]);
+      }
       top = top == top ? top : kInf;
       top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wave_max(top))));
       if (lane == 0) block_max[b] = top;
@@ -199,16 +205,33 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
         continue;
       }
       if ((double)top > base + 600.0) {
-        sum *= exp(base - (double)top);
-        base = (double)top;
+        const double before = base;
+        near = __builtin_fabsf(top) <= 0x1p16f;
+        shift = rint((double)top * kLog2e);
+        base = near ? shift * kLn2 : (double)top;
+        lowest = (float)(base - 690.0);
+        sum *= exp(before - base);
       }
-#pragma unroll
-      for (int e = 0; e < C * N; ++e) {
-        // with 1.5 * 2^52 added, the low word is the whole part of d log2 e
-        const double d = fmax((double)x[e] - base, -690.0);
-        const double y = __builtin_fma(d, kLog2e, 0x1.8p52);
-        const double p = exp2_small(__builtin_fma(d, kLog2e, -(y - 0x1.8p52)));
+      // with 1.5 * 2^52 - shift added, the low word is the whole part less the shift
+      const double magic = 0x1.8p52 - shift;
+      const auto add = [&](float xe) {
+        const double d = (double)xe, y = __builtin_fma(d, kLog2e, magic);
+        const double p = exp2_small(__builtin_fma(d, kLog2e, -(y - magic)));
         sum += __hiloint2double(__double2hiint(p) + (__double2loint(y) << 20), __double2loint(p));
+      };
+      if (near && !__any(low < lowest)) {
+#pragma unroll
+        for (int e = 0; e < C * N; ++e) add(x[e]);
+      } else if (near) {
+#pragma unroll
+        for (int e = 0; e < C * N; ++e) add(fmaxf(x[e], lowest));
+      } else {
+#pragma unroll
+        for (int e = 0; e < C * N; ++e) {
+          const double d = fmax((double)x[e] - base, -690.0), y = __builtin_fma(d, kLog2e, 0x1.8p52);
+          const double p = exp2_small(__builtin_fma(d, kLog2e, -(y - 0x1.8p52)));
+          sum += __hiloint2double(__double2hiint(p) + (__double2loint(y) << 20), __double2loint(p));
+        }
       }
     }
   }
@@ -489,10 +512,13 @@ hipError_t launch(const BeamArgs &a, int64_t n_groups, hipStream_t s) {
 
 int32_t beam_blocks(int32_t vocab) { return (vocab + kBlock - 1) / kBlock; }
 
-// Workgroups a row: enough for every CU, each with a block or more for every wave.
+// Workgroups a row: those of all rows run at once (seven fit a CU), each with a block or
+// more for every wave, and no fewer blocks for some waves than need be.
 int32_t beam_splits(int64_t n_rows, int32_t n_blocks) {
-  const int64_t most = std::min((n_blocks + kScanWaves - 1) / kScanWaves, 64);
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, (kScanTarget + n_rows - 1) / n_rows));
+  const int64_t quads = (n_blocks + kScanWaves - 1) / kScanWaves;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(quads, 64), kScanTarget / n_rows));
+  const int64_t per_wave = (quads + most - 1) / most;
+  return (int32_t)((quads + per_wave - 1) / per_wave);
 }
 
 hipError_t launch_beam_select(int32_t type, const BeamArgs &a, int64_t n_groups, hipStream_t s) {

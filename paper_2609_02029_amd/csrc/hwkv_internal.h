@@ -339,7 +339,7 @@ hipError_t launch_page_move(const PageMoveArgs &a, hipStream_t s);
 
 // Beam search's selection (beam_kernels.hip).
 constexpr int kMaxBeams = 64, kMaxSelected = 64;
-constexpr int kScanTarget = 2048;  // workgroups that the scan of all rows aims at
+constexpr int kScanTarget = 1792;  // most workgroups of the scan of all rows (if not one a row)
 struct BeamArgs {
   const void *logits;            // rows stride elements apart
   int64_t stride;

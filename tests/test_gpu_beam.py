@@ -1,7 +1,7 @@
 """GPU tests of beam selection against scores formed in 64 bits on the host.
 
 Scores are 64-bit sums rounded once to fp32: off by half a step, 2^-24 of the
-value, by the error of lse (1.1e-12 a term, so at most 2e-12 in all), and in rows far
+value, by the error of lse (5.5e-11 a term, so at most 1e-10 in all), and in rows far
 from zero by the reference's own rounding of lse (half a step of 2^-52 of it, and as
 much again in x - lse)."""
 import numpy as np
@@ -67,7 +67,7 @@ def check(out, x, s, n):
     assert np.array_equal(got[0] == -np.inf, ~some)
     ref = val[some]
     far = np.nan_to_num(np.abs(x.double().cpu().numpy()), posinf=0.0, neginf=0.0).max()
-    assert np.all(np.abs(got[0][some] - ref) <= 2.0 ** -24 * np.abs(ref) + 4e-12 + 2.0 ** -52 * far)
+    assert np.all(np.abs(got[0][some] - ref) <= 2.0 ** -24 * np.abs(ref) + 1e-10 + 2.0 ** -52 * far)
 
 
 def inputs(G, B, V, t, seed=0, spread=2.5):
