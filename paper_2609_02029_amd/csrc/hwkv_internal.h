@@ -304,12 +304,22 @@ hipError_t launch_move_rows(const MoveArgs &a, hipStream_t s);
 // Workgroups of a unit for `rows` rows.
 int64_t move_workgroups(int64_t rows, int32_t row_bytes, int32_t pair_bytes);
 
-// Pages copied within a pool, and page-table entries installed.
-constexpr int kMaxPageCopies = 120, kMaxEntries = 240;
+// The page table's rows under the same moves, for every full unit: pages[i] entries of
+// each row.
+struct TableMoveArgs {
+  uint16_t src[kMaxMoves], dst[kMaxMoves];
+  int32_t pages[kMaxMoves];
+  int32_t *table;                // [unit][sequence][max_pages]
+  int32_t n_moves, most, batch, max_pages;
+};
+hipError_t launch_table_move(const TableMoveArgs &a, int n_units, hipStream_t s);
+
+// Pages copied within a pool, each with its table entry, and entries alone.
+constexpr int kMaxPageCopies = 192, kMaxEntries = 180;
 struct PageCopyArgs {
-  int32_t src[kMaxPageCopies], dst[kMaxPageCopies];
-  int32_t rows[kMaxPageCopies];  // that src holds
+  int32_t src[kMaxPageCopies], dst[kMaxPageCopies], at[kMaxPageCopies];
   int32_t idx[kMaxEntries], page[kMaxEntries];
+  uint8_t rows[kMaxPageCopies];  // that src holds (< 256)
   int32_t n_copies, n_entries;
   uint8_t *pool;
   int32_t *table;
@@ -580,6 +590,7 @@ static_assert(sizeof(hwkv::AppendRopeArgs) <= 4096, "append rope kernarg too lar
 static_assert(sizeof(hwkv::PageUpdateArgs) <= 4096, "page update kernarg too large");
 static_assert(sizeof(hwkv::SharedArgs) <= 4096, "shared decode kernarg too large");
 static_assert(sizeof(hwkv::MoveArgs) <= 4096, "move kernarg too large");
+static_assert(sizeof(hwkv::TableMoveArgs) <= 4096, "table move kernarg too large");
 static_assert(sizeof(hwkv::PageCopyArgs) <= 4096, "page copy kernarg too large");
 static_assert(sizeof(hwkv::PageMoveArgs) <= 4096, "page move kernarg too large");
 static_assert(sizeof(hwkv::StageArgs) <= 4096, "stage kernarg too large");

@@ -113,11 +113,37 @@ __global__ __launch_bounds__(256) void page_copy(PageCopyArgs a) {
   const int i = blockIdx.x / kPageParts;
   if (i == a.n_copies) {
     for (int e = threadIdx.x; e < a.n_entries; e += 256) a.table[a.idx[e]] = a.page[e];
+    for (int e = threadIdx.x; e < a.n_copies; e += 256) a.table[a.at[e]] = a.dst[e];
     return;
   }
   const int64_t page = page_bytes(a.row_bytes, a.pair_bytes);
   copy_page(a.pool + a.src[i] * page, a.pool + a.dst[i] * page, blockIdx.x % kPageParts, a.rows[i], a.row_bytes,
             a.pair_bytes);
+}
+
+// move_rows for the page table: a thread holds entry j of every row of a unit.  Grid:
+// (entries / 256, units).
+__global__ __launch_bounds__(256) void table_move(TableMoveArgs a) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  int32_t *const rows = a.table + (int64_t)blockIdx.y * a.batch * a.max_pages + j;
+  int32_t carry = 0;
+  for (int r = 0; r < a.n_moves; r += kMoveRound) {
+    int32_t x[kMoveRound] = {};
+#pragma unroll
+    for (int i = 0; i < kMoveRound; ++i) {
+      const int src = a.src[r + i];
+      if (j < a.pages[r + i]) x[i] = src == kMoveCarry ? carry : rows[(int64_t)src * a.max_pages];
+    }
+#pragma unroll
+    for (int i = 0; i < kMoveRound; ++i) {
+      const int dst = a.dst[r + i];
+      if (j >= a.pages[r + i]) continue;
+      if (dst == kMoveCarry)
+        carry = x[i];
+      else
+        rows[(int64_t)dst * a.max_pages] = x[i];
+    }
+  }
 }
 
 // Grid: kPageParts workgroups a page.
@@ -151,9 +177,13 @@ hipError_t launch_move_rows(const MoveArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
+hipError_t launch_table_move(const TableMoveArgs &a, int n_units, hipStream_t s) {
+  hipLaunchKernelGGL(table_move, dim3((unsigned)((a.most + 255) / 256), (unsigned)n_units), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t s) {
-  const int wgs = a.n_copies * kPageParts + (a.n_entries > 0 ? 1 : 0);
-  if (wgs == 0) return hipSuccess;
+  const int wgs = a.n_copies * kPageParts + 1;
   hipLaunchKernelGGL(page_copy, dim3((unsigned)wgs), dim3(256), 0, s, a);
   return hipGetLastError();
 }

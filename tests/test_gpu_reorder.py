@@ -203,6 +203,47 @@ def test_shared_pages_are_counted():
     r.check_pages()
 
 
+@pytest.mark.parametrize("parents", [
+    [9, 0, 1, 2, 3, 4, 5, 6, 7, 8],          # one cycle, longer than a round of moves
+    [3, 3, 3, 3, 3, 3, 3, 3, 3, 3],
+    [1, 0, 0, 1, -1, 2, 2, 9, 9, 8],
+])
+def test_long_page_tables(parents):
+    """More table entries than lists of them hold: the kernels see the new chains.
+    Logits are sums of 64 products of about 8 in all, off by 64 x 2^-24 x 8 = 3e-5, and
+    rows reach 4.5: 1.4e-4.  One page of another sequence in eleven moves an output by
+    about 1e-2."""
+    lens = [2600, 2561, 2500, 2816, 2815, 1, 2560, 2700, 300, 2305]
+    r = Held([[1, 1, 0, 1], [1, 0, 1, 1], [1, 1, 1, 1]], lens, D=64, max_ctx=2900, pages=1000)
+    q = torch.randn((10, 4, 64), generator=r.gen, device=DEV).to(torch.bfloat16)
+    out = torch.empty((10, 4, 64), dtype=torch.float32, device=DEV)
+    for _ in range(2):
+        stored = r.read()
+        r.reorder(parents)
+        same(stored, r.read(), parents)
+        r.check_pages()
+        for _ in range(2):
+            r.append()
+        r.check_pages()
+        ws = torch.empty(hwkv.decode_workspace_bytes(r.cache), dtype=torch.uint8, device=DEV)
+        want = torch.stack([reference(r, b, q[b]) for b in range(10)])
+        for layer in range(3):
+            hwkv.decode_attn(r.cache, layer, q, 0.125, out, ws)
+            assert (out.cpu().double() - want[:, layer]).abs().max() < 1.4e-4
+
+
+def reference(r, b, q):
+    """Attention of one sequence over the rows it holds, in 64 bits, [layer][head][D]."""
+    out = []
+    for layer in range(r.L):
+        for h in range(r.H):
+            k, v, n = hwkv.cache_read_unit(r.cache, layer, h, b)
+            k, v = (torch.from_numpy(x[:n].astype(np.uint16).astype(np.int32) << 16).view(torch.float32).double() for x in (k, v))
+            z = k @ q[h].double().cpu() * 0.125
+            out.append(torch.softmax(z, 0) @ v)
+    return torch.stack(out).view(r.L, r.H, r.D)
+
+
 def test_a_short_pool_changes_nothing():
     """Three copies of a partly filled page; the pool has one, and nobody leaves one."""
     r = Held([[1, 0]], [300, 300, 0, 0, 0], pages=5, seed=3)
