@@ -5,7 +5,7 @@
 // The sequences of a fork hold the same pages up to where they parted.  An item of
 // work is a run of rows of one KV head and the query columns that see all of them:
 //   a block   the pages that a group of sequences shares, with the q heads of all of
-//             its members (up to 64 columns), so that a row is read once for them;
+//             its members, in groups of 16 columns;
 //   an own    a sequence's rows from there on, a window's rows, or all the rows of
 //             a sequence that shares nothing, with its own q heads.
 // Every item is split over workgroups, workgroup j of n taking its tiles of 64 rows
@@ -13,9 +13,8 @@
 // every q head of a sequence, the parts of its block and its own:
 //     out = sum_j acc_j 2^(m_j - M) / sum_j l_j 2^(m_j - M),  M = max m_j.
 //
-// A wavefront has 16 columns (so that its accumulators take 64 registers at head_dim
-// 256, whatever the block) and a part of every tile's rows, with an online softmax of
-// its own; the waves of a column group meet in LDS at the end.
+// A workgroup has one column group; a wavefront has a quarter of every tile's rows,
+// with an online softmax of its own, and the four meet in LDS at the end.
 //   z = K q   v_mfma_f32_16x16x32: A = K (16 rows x 32 channels; lane (g, r) holds
 //             8 channels of row r as they lie in the K tile), B = the columns of q.
 //             Lane (g, c) ends with rows 4g .. 4g + 3 of column c.
@@ -26,11 +25,9 @@
 //             binary16 over binary16 values (2^-22).  The 32 places of a product hold
 //             two terms of 16 rows over the same V, or the third of two times 16 rows.
 // Rows go from memory straight into LDS, 64 KB of K and V at a time (a stage of one to
-// four tiles).  With one column group (CW = 1) four waves share out a tile's rows and
-// each loads, and reads into registers whole, its own: no barrier falls inside the
-// walk, the next stage's loads are issued before anything is computed, and two
-// workgroups fit a CU.  With two or four (32, 64 columns) eight waves share the rows,
-// in two stages that barriers hand over, one workgroup per CU.
+// four tiles).  Each wave loads, and reads into registers whole, its own rows: no
+// barrier falls inside the walk, the next stage's loads are issued before anything is
+// computed, and two workgroups fit a CU.
 #pragma once
 
 #include <cfloat>
@@ -81,89 +78,76 @@ __device__ __forceinline__ u32x4_t widen_codes(u32x2_t c) {
 // Tiles of a stage.
 constexpr int shared_tiles(int row_bytes) { return row_bytes >= 512 ? 1 : row_bytes >= 256 ? 2 : 4; }
 
-// All but the last N vector memory operations of the wave are done.
-template <int N>
-__device__ __forceinline__ void wait_all_but() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 // The wave's LDS reads are done.
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 // A barrier that leaves loads in flight.
 __device__ __forceinline__ void meet() { asm volatile("s_barrier" ::: "memory"); }
 
-constexpr int shared_threads(int CW) { return CW == 1 ? 256 : 512; }
-
-template <int D, int F, int CW>
-__global__ __launch_bounds__(shared_threads(CW)) __attribute__((amdgpu_waves_per_eu(2)))
+template <int D, int F>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void decode_shared(SharedArgs a) {
   constexpr bool CODES = KvFormat<F>::kBytes == 1, I8 = F == HWKV_KV_I8, F16 = F == HWKV_KV_F16;
-  constexpr bool ALONE = CW == 1;      // a wave reads only what it has loaded
   constexpr int EB = KvFormat<F>::kBytes;
-  constexpr int WAVES = shared_threads(CW) / 64;
   constexpr int NC = D / 8;            // chunks of a row
   constexpr int KS = D / 32;           // products over the channels
   constexpr int VB = D / 16;           // channel blocks
   constexpr int ROW = D * EB;
   constexpr int PCS = ROW / 16;        // 16-byte pieces of a V row
-  constexpr int NT = shared_tiles(ROW);
+  constexpr int P = shared_tiles(ROW); // tiles of a stage; a wave has 16 rows of each
   constexpr int KB = 64 * ROW;         // K, or V, of a tile
   constexpr int TB = 2 * KB + (I8 ? 1024 : 0);   // and scale pairs
-  constexpr int STAGE = NT * TB, BUFS = ALONE ? 1 : 2;
-  constexpr int LDS = NT * KB / 1024 / WAVES;    // a wave's loads of K, and of V, of a stage
-  constexpr int LOADS = 2 * LDS + (I8 ? NT : 0);
-  constexpr int PARTS = NT * 4;        // 16-row parts of a stage,
-  constexpr int P = ALONE ? NT : 2;    // that a wave computes at a time
-  constexpr int CB = 16 * CW;          // columns
-  static_assert(BUFS * STAGE >= WAVES * 16 * D * 4, "16 columns of acc a wave, at the end");
-  static_assert(STAGE >= CB * D * 2, "the columns of q");
-  __shared__ __attribute__((aligned(1024))) uint8_t area[BUFS * STAGE];
-  __shared__ __attribute__((aligned(16))) u32x4_t q_s[ALONE ? KS * 64 : 1];
-  __shared__ float back_s[CB][2];      // what a column's logits are multiplied by
-  __shared__ float sml[WAVES][2][16];
+  static_assert(kWaves == 4, "16 rows of a tile a wave");
+  static_assert(P * TB >= kWaves * 16 * D * 4, "16 columns of acc a wave, at the end");
+  __shared__ __attribute__((aligned(1024))) uint8_t area[P * TB];
+  __shared__ __attribute__((aligned(16))) u32x4_t q_s[KS * 64];
+  __shared__ float back_s[16][2];      // what a column's logits are multiplied by
+  __shared__ float sml[kWaves][2][16];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g4 = lane >> 4, l16 = lane & 15;
   // ---- the item
-  const int rank = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.wg_begin[lane] <= (int)blockIdx.x)) - 1);
-  const ItemHead &hd = a.head[rank];
-  const int h = a.head_id[rank];
-  const int local = blockIdx.x - a.wg_begin[rank];
-  int first, count, row0, end, j, nwg;
-  bool block = false;
+  int rank = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.wg_begin[lane] <= (int)blockIdx.x)) - 1);
+  const bool block = rank < 0;
+  int first, count = 1, row0 = 0, end, j, nwg, col0 = 0;
   if (rank < a.n_full) {
+    const int local = block ? (int)blockIdx.x : blockIdx.x - a.wg_begin[rank] + a.block_wgs;
+    const int heads = block ? a.n_full : 1;      // that share item_begin's range
     int item = -1;
 #pragma unroll
     for (int i = 0; i < kSharedItems; i += 64)
-      item += __popcll(__ballot((int)a.item_begin[i + lane] <= local));
+      item += __popcll(__ballot(a.item_begin[i + lane] * heads <= local));
     item = __builtin_amdgcn_readfirstlane(item);
-    j = local - a.item_begin[item];
     nwg = a.item_begin[item + 1] - a.item_begin[item];
-    block = item < a.n_blocks;
-    first = block ? a.block_first[item] : item - a.n_blocks;
-    count = block ? a.block_count[item] : 1;
-    row0 = 0;
-    end = a.len[first];
+    j = local - a.item_begin[item] * heads;
     if (block) {
+      // (the heads' workgroups in one row, eight of a column group after eight of
+      // another)
+      first = a.block_first[item];
+      count = a.block_count[item];
       end = a.block_pages[item] * kPageTokens;
-    } else if (a.seq_block[first] != kNoBlock) {
-      row0 = a.block_pages[a.seq_block[first]] * kPageTokens;
+      const int groups = (count * a.group + 15) / 16, round = j / (8 * groups), at = j - round * 8 * groups;
+      nwg /= groups;
+      const int n = min(8, nwg * heads - 8 * round);
+      j = 8 * round + at % n;
+      col0 = at / n * 16;
+      rank = j / nwg;
+      j -= rank * nwg;
+    } else {
+      first = item - a.n_blocks;
+      end = a.len[first];
+      if (a.seq_block[first] != kNoBlock) row0 = a.block_pages[a.seq_block[first]] * kPageTokens;
     }
   } else {
+    const int local = blockIdx.x - a.wg_begin[rank];
     first = local % a.n_seqs;
     j = local / a.n_seqs;
-    count = 1;
-    row0 = 0;
-    end = min(a.len[first], hd.cap);
+    end = min(a.len[first], a.head[rank].cap);
     nwg = ((end + 63) / 64 + a.tiles_per_wg - 1) / a.tiles_per_wg;
     if (j >= nwg) return;              // uniform: a shorter sequence
   }
-  const int ncols = count * a.group;
-  // Waves share out the columns in groups of 16, and with those of their group the
-  // parts: RW waves take `per` each, wave rw from part rw * per on.
-  const int RW = ALONE ? 4 : ncols <= 16 ? 8 : ncols <= 32 ? 4 : 2;
-  const int cw = wave / RW, rw = wave % RW;
-  const int per = ALONE ? NT : max(PARTS / RW, 1);
-  const bool busy = ALONE || (16 * cw < ncols && rw * per < PARTS);
+  const ItemHead &hd = a.head[rank];
+  const int h = a.head_id[rank];
+  const int ncols = min(16, count * a.group - col0);
   const int tile0 = row0 / 64, n_tiles = (end - row0 + 63) / 64;
   const int b0 = a.seq[first];
   const int pto = hd.page0 >= 0 ? hd.page0 + b0 * a.max_pages : -1;
@@ -196,92 +180,57 @@ void decode_shared(SharedArgs a) {
     }
     return {kbase + (int64_t)t * KB, vbase + (int64_t)t * KB, sbase + t * 64 * kRowScaleBytes};
   };
-  // ---- loads, 1 KB each.  K as it lies in the tile; ALONE, the wave's 16 rows of every
-  // chunk, chunk by chunk.  V row by row, each row's pieces turned (by 32 bytes from row
-  // to row at 16 bits) so that the rows that are read together lie in different banks;
-  // of codes, LDS row 4i + g of 16 holds row 4g + i.
+  // ---- loads, 1 KB each: the wave's 16 rows of every chunk of K, chunk by chunk, and
+  // its rows of V, each row's pieces turned (by 32 bytes from row to row at 16 bits) so
+  // that the rows that are read together lie in different banks; of codes, LDS row
+  // 4i + g of 16 holds row 4g + i.
   auto piece_xor = [](int r) {
     if constexpr (CODES) return D == 256 ? 4 * (r & 3) : D == 128 ? 4 * ((r & 3) >> 1) : 0;
     return D == 64 ? 2 * (r >> 1 & 3) : 2 * (r & 7);
   };
   constexpr int RPL = 1024 / ROW;      // V rows of a load
-  constexpr int TK = KB / 1024;        // loads of a tile's K, or V
-  const uint32_t area0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)area;
-  // the lane's place in load n of a tile's V (ALONE: of its 16 rows)
-  auto v_offset = [&](int n) {
-    const int r = n * RPL + lane / PCS;
-    const int at = CODES ? (r & ~15) + 4 * (r & 3) + (r >> 2 & 3) : r;
-    return at * ROW + ((lane % PCS) ^ piece_xor(r)) * 16;
-  };
-  const int kl = !ALONE ? lane * 16
-                 : CODES ? lane / 8 * 512 + 128 * wave + lane % 8 * 16 : g4 * 1024 + (16 * wave + l16) * 16;
-  int vl[LDS];
+  constexpr int LOADS = KB / 4096;     // the wave's loads of a tile's K, or V
+  const uint32_t area0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)area + wave * (KB / 4);
+  const int kl = CODES ? lane / 8 * 512 + 128 * wave + lane % 8 * 16 : g4 * 1024 + (16 * wave + l16) * 16;
+  int vl[LOADS];
 #pragma unroll
-  for (int n = 0; n < LDS; ++n)
-    vl[n] = ALONE ? 16 * wave * ROW + v_offset(n % (LDS / NT)) : v_offset((wave + WAVES * n) % TK);
+  for (int n = 0; n < LOADS; ++n) {
+    const int r = n * RPL + lane / PCS, row = CODES ? 4 * (r & 3) + (r >> 2) : r;
+    vl[n] = (16 * wave + row) * ROW + ((lane % PCS) ^ piece_xor(r)) * 16;
+  }
   const int sl = lane < 32 ? 4 * lane : 1 << 20;
-  // The loads of tiles i0 .. i0 + NT - 1; of those past the last nothing is read.
-  auto issue = [&](int i0, int buf) {
+  // The loads of tiles i0 .. i0 + P - 1; of those past the last nothing is read.
+  auto issue = [&](int i0) {
     if (i0 % 64 == 0 && j + i0 * nwg < n_tiles) look_up(i0);
-    const uint32_t to = area0 + buf * STAGE;
-    struct Part {
-      Tile at;
-      int rows;
-    };
-    auto of = [&](int t) -> Part {
-      const int lt = j + (i0 + t) * nwg;
+#pragma unroll
+    for (int t = 0; t < P; ++t) {
+      const int lt = j + (i0 + t) * nwg, rows = lt < n_tiles ? min(64, end - 64 * (tile0 + lt)) : 0;
       const Tile at = tile(i0 + t);
-      return {at, lt < n_tiles ? min(64, end - 64 * (tile0 + lt)) : 0};
-    };
-    if constexpr (ALONE) {
+      const __amdgpu_buffer_rsrc_t kr = make_rsrc(at.k, rows > 0 ? (uint32_t)KB : 0u);
+      const __amdgpu_buffer_rsrc_t vr = make_rsrc(at.v, (uint32_t)(rows * ROW));
+      const uint32_t into = area0 + t * TB;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const Part x = of(t);
-        const __amdgpu_buffer_rsrc_t kr = make_rsrc(x.at.k, x.rows > 0 ? (uint32_t)KB : 0u);
-        const __amdgpu_buffer_rsrc_t vr = make_rsrc(x.at.v, (uint32_t)(x.rows * ROW));
-        const uint32_t into = to + t * TB + wave * (KB / 4);
+      for (int n = 0; n < LOADS; ++n) stage_lds<false>(kr, into + n * 1024, kl, n * 4096);
 #pragma unroll
-        for (int n = 0; n < TK / 4; ++n) stage_lds<false>(kr, into + n * 1024, kl, n * 4096);
-#pragma unroll
-        for (int n = 0; n < TK / 4; ++n) stage_lds<false>(vr, into + KB + n * 1024, vl[n], 0);
-        // (every wave has the tile's pairs, in a place of its own)
-        if constexpr (I8)
-          stage_lds<true>(make_rsrc(x.at.s, x.rows > 0 ? 64u * kRowScaleBytes : 0u), to + t * TB + 2 * KB + wave * 256, sl,
-                          0);
-      }
-    } else {
-#pragma unroll
-      for (int n = 0; n < LDS; ++n) {
-        const int t = __builtin_amdgcn_readfirstlane((wave + WAVES * n) / TK), i = (wave + WAVES * n) % TK;
-        const Part x = of(t);
-        const __amdgpu_buffer_rsrc_t kr = make_rsrc(x.at.k, x.rows > 0 ? (uint32_t)KB : 0u);
-        const __amdgpu_buffer_rsrc_t vr = make_rsrc(x.at.v, (uint32_t)(x.rows * ROW));
-        const uint32_t into = __builtin_amdgcn_readfirstlane(to + t * TB + i * 1024);
-        stage_lds<false>(kr, into, kl, __builtin_amdgcn_readfirstlane(i * 1024));
-        stage_lds<false>(vr, into + KB, vl[n], 0);
-      }
-      // (every wave loads all pairs, the same bytes to the same place, so that the
-      // waves have equal numbers of loads)
+      for (int n = 0; n < LOADS; ++n) stage_lds<false>(vr, into + KB + n * 1024, vl[n], 0);
+      // (every wave has the tile's pairs, in a place of its own)
       if constexpr (I8)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const Part x = of(t);
-          stage_lds<true>(make_rsrc(x.at.s, x.rows > 0 ? 64u * kRowScaleBytes : 0u), to + t * TB + 2 * KB, sl, 0);
-        }
+        stage_lds<true>(make_rsrc(at.s, rows > 0 ? 64u * kRowScaleBytes : 0u),
+                        into - wave * (KB / 4 - 256) + 2 * KB, sl, 0);
     }
   };
-  issue(0, 0);
+  issue(0);
 
   // ---- q: column c is q head c mod G of the block's member c / G.  Over binary16
   // and int8 rows a column is scaled by a power of two, that of its largest |q|: to
   // [2^14, 2^15), so that binary16 holds it, or to [1, 2), so that sums over codes
   // stay in fp32's range.
-  u32x4_t *const q_at = ALONE ? q_s : reinterpret_cast<u32x4_t *>(area + (BUFS - 1) * STAGE);
-  for (int i = threadIdx.x; i < CB * NC; i += WAVES * 64) {
+  for (int i = threadIdx.x; i < 16 * NC; i += kWaves * 64) {
     const int c = i / NC, ch = i % NC;
     uint4 x = make_uint4(0u, 0u, 0u, 0u);
     if (c < ncols) {
-      const int64_t row = (int64_t)a.seq[first + c / a.group] * a.n_q_heads + h * a.group + c % a.group;
+      const int col = col0 + c;
+      const int64_t row = (int64_t)a.seq[first + col / a.group] * a.n_q_heads + h * a.group + col % a.group;
       x = *reinterpret_cast<const uint4 *>(a.q + row * D + ch * 8);
     }
     u32x4_t y = {x.x, x.y, x.z, x.w};
@@ -308,7 +257,7 @@ void decode_shared(SharedArgs a) {
     } else if constexpr (F == HWKV_KV_FP8_E4M3) {
       near *= hd.k_scale;
     }
-    q_at[(c / 16 * KS + ch / 4) * 64 + ch % 4 * 16 + c % 16] = y;
+    q_s[ch / 4 * 64 + ch % 4 * 16 + c] = y;
     if (ch == 0) {
       back_s[c][0] = near;
       back_s[c][1] = rest;
@@ -319,13 +268,8 @@ void decode_shared(SharedArgs a) {
   meet();
   u32x4_t q[KS];
 #pragma unroll
-  for (int i = 0; i < KS; ++i) q[i] = q_at[(cw * KS + i) * 64 + lane];
-  const float near = back_s[16 * cw + l16][0], rest = back_s[16 * cw + l16][1];
-  if constexpr (!ALONE) {
-    wait_reads();
-    meet();
-    issue(NT, 1);
-  }
+  for (int i = 0; i < KS; ++i) q[i] = q_s[i * 64 + lane];
+  const float near = back_s[l16][0], rest = back_s[l16][1];
 
   // ---- the walk.  m: running shift of the lane's column (base 2), raised where a
   // logit passes it by 8, so that weights stay below 2^8; it begins below every
@@ -334,185 +278,163 @@ void decode_shared(SharedArgs a) {
   f32x4_t o[VB];
 #pragma unroll
   for (int vb = 0; vb < VB; ++vb) o[vb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  int buf = 0;
-  for (int i0 = 0; j + i0 * nwg < n_tiles; i0 += NT) {
-    wait_all_but<(BUFS - 1) * LOADS>();
-    if constexpr (!ALONE) meet();
-    const uint8_t *const sp = area + buf * STAGE;
-    for (int s0 = 0; busy && s0 < per; s0 += P) {
-      // its parts s0 .. s0 + P - 1: rows [16 part, + 16) of tile t (ALONE: part `wave`
-      // of every tile)
-      u32x4_t kf[CODES ? 1 : P][KS];
-      u32x2_t kc[CODES ? P : 1][KS];
-      u32x2_t vf[CODES ? 1 : P][VB];
-      uint32_t vc[CODES ? P : 1][CODES ? D / 64 : 1][4];
-      u32x2_t pairs[P];
-      int left[P];                     // of the lane's rows, from its first on
+  for (int i0 = 0; j + i0 * nwg < n_tiles; i0 += P) {
+    wait_loads();
+    u32x4_t kf[CODES ? 1 : P][KS];
+    u32x2_t kc[CODES ? P : 1][KS];
+    u32x2_t vf[CODES ? 1 : P][VB];
+    uint32_t vc[CODES ? P : 1][CODES ? D / 64 : 1][4];
+    u32x2_t pairs[P];
+    int left[P];                       // of the lane's rows, from its first on
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int x = rw * per + min(s0 + p, per - 1);
-        const int t = ALONE ? p : x / 4, part = ALONE ? wave : x % 4;
-        const uint8_t *const at = sp + t * TB;
-        const int lt = j + (i0 + t) * nwg;
-        left[p] = lt < n_tiles && s0 + p < per ? end - (64 * (tile0 + lt) + 16 * part + 4 * g4) : 0;
-        if constexpr (I8)
-          pairs[p] = *reinterpret_cast<const u32x2_t *>(at + 2 * KB + (ALONE ? wave * 256 : 0) + 32 * part + 8 * g4);
-        const uint8_t *const v = at + KB + part * (KB / 4);
-        if constexpr (CODES) {
-#pragma unroll
-          for (int i = 0; i < KS; ++i)
-            kc[p][i] = *reinterpret_cast<const u32x2_t *>(
-                ALONE ? at + wave * (KB / 4) + (4 * i + g4) * 128 + l16 * 8 : at + (4 * i + g4) * 512 + part * 128 + l16 * 8);
-#pragma unroll
-          for (int i = 0; i < D / 64; ++i)
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-              vc[p][i][n] = *reinterpret_cast<const uint32_t *>(v + (4 * n + g4) * D +
-                                                                ((4 * i + l16 / 4) ^ piece_xor(g4)) * 16 + l16 % 4 * 4);
-        } else {
-#pragma unroll
-          for (int i = 0; i < KS; ++i)
-            kf[p][i] = *reinterpret_cast<const u32x4_t *>(
-                ALONE ? at + wave * (KB / 4) + i * 1024 + lane * 16 : at + (4 * i + g4) * 1024 + part * 256 + l16 * 16);
-          // (16 lanes read 4 rows of 16 channels, 8 bytes each, and receive 4 rows of one)
-          const int r = 4 * g4 + l16 / 4;
-#pragma unroll
-          for (int vb = 0; vb < VB; ++vb)
-            vf[p][vb] = __builtin_bit_cast(
-                u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                             (lds_s16x4_t *)(uint8_t __attribute__((address_space(3))) *)(
-                                 v + r * ROW + ((2 * vb) ^ piece_xor(r)) * 16 + l16 % 4 * 8)));
-        }
-      }
-      if constexpr (ALONE) {
-        wait_reads();
-        issue(i0 + NT, 0);
-      }
-
-      // logits (a product that adds to the one before it waits out its latency: two
-      // sums where there is one part)
-      constexpr int CH = P == 1 ? 2 : 1;
-      f32x4_t z[P], zz[P][CH];
-#pragma unroll
-      for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int c = 0; c < CH; ++c) zz[p][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < KS; ++i)
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-          if constexpr (CODES) zz[p][i % CH] = product<F>(widen_codes<F>(kc[p][i]), q[i], zz[p][i % CH]);
-          else zz[p][i % CH] = product<F>(kf[p][i], q[i], zz[p][i % CH]);
-        }
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        z[p] = zz[p][0];
-        if constexpr (CH == 2) z[p] += zz[p][1];
-      }
-      // (rows past the item's end have no weight)
-      float top = -FLT_MAX;
-#pragma unroll
-      for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = z[p][i] * near;
-          if constexpr (I8) x *= __uint_as_float(((i < 2 ? pairs[p].x : pairs[p].y) >> (16 * (i & 1)) & 255u) << 23);
-          if constexpr (I8 || F16) x *= rest;
-          z[p][i] = i < left[p] ? x : -INFINITY;
-          top = fmaxf(top, z[p][i]);
-        }
-      top = max_of_rows(top);
-      if (__any(top > m + 8.0f)) {
-        const float mn = fmaxf(m, top), f = exp2f(m - mn);
-        m = mn;
-        lsum *= f;
-#pragma unroll
-        for (int vb = 0; vb < VB; ++vb) o[vb] *= f;
-      }
-      u32x2_t term[P][F16 ? 2 : 3];
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        float w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[i] = __builtin_amdgcn_exp2f(z[p][i] - m);
-          lsum += w[i];
-          if constexpr (F16) w[i] *= 0x1p7f;       // clear of binary16's subnormals
-          // 2^-12 centres the range of weights times row scales
-          if constexpr (I8) {
-            const uint32_t pr = (i < 2 ? pairs[p].x : pairs[p].y) >> (16 * (i & 1));
-            w[i] = i < left[p] ? w[i] * 0x1p-12f * __uint_as_float((pr << 15) & 0x7f800000u) : 0.f;
-          }
-        }
-        if constexpr (F16) {
-          const f16x2_t a0 = {(_Float16)w[0], (_Float16)w[1]}, a1 = {(_Float16)w[2], (_Float16)w[3]};
-          const f16x2_t r0 = {(_Float16)(w[0] - (float)a0.x), (_Float16)(w[1] - (float)a0.y)},
-                        r1 = {(_Float16)(w[2] - (float)a1.x), (_Float16)(w[3] - (float)a1.y)};
-          term[p][0] = u32x2_t{__builtin_bit_cast(uint32_t, a0), __builtin_bit_cast(uint32_t, a1)};
-          term[p][1] = u32x2_t{__builtin_bit_cast(uint32_t, r0), __builtin_bit_cast(uint32_t, r1)};
-        } else {
-#pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            const u32x2_t x = {pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])};
-            term[p][k] = x;
-            w[0] -= bf_lo(x.x);
-            w[1] -= bf_hi(x.x);
-            w[2] -= bf_lo(x.y);
-            w[3] -= bf_hi(x.y);
-          }
-        }
-      }
-      // values: term by term over two parts; of a single part, the first two terms over
-      // the same V, then the third.  (The product of 16 places takes as long as that of
-      // 32; and compiled right behind one of 32 into the same accumulator, with no wait
-      // between, it gave wrong sums.)
-      constexpr int TERMS = F16 ? 2 : 3, STEPS = P == 1 ? TERMS - 1 : TERMS;
-      auto add = [&](int step, int vb, const u32x2_t (&v)[P]) {
-        if constexpr (P == 1) {
-          const u32x2_t x = term[0][2 * step], y = step == 0 ? term[0][1] : u32x2_t{0u, 0u};
-          o[vb] = product<F>(u32x4_t{v[0].x, v[0].y, v[0].x, v[0].y}, u32x4_t{x.x, x.y, y.x, y.y}, o[vb]);
-        } else {
-#pragma unroll
-          for (int p = 0; p < P; p += 2) {
-            const u32x2_t x = term[p][step], y = term[p + 1][step];
-            o[vb] = product<F>(u32x4_t{v[p].x, v[p].y, v[p + 1].x, v[p + 1].y}, u32x4_t{x.x, x.y, y.x, y.y}, o[vb]);
-          }
-        }
-      };
+    for (int p = 0; p < P; ++p) {
+      const uint8_t *const k = area + p * TB + wave * (KB / 4), *const v = k + KB;
+      const int lt = j + (i0 + p) * nwg;
+      left[p] = lt < n_tiles ? end - (64 * (tile0 + lt) + 16 * wave + 4 * g4) : 0;
+      if constexpr (I8)
+        pairs[p] = *reinterpret_cast<const u32x2_t *>(area + p * TB + 2 * KB + wave * 256 + 32 * wave + 8 * g4);
       if constexpr (CODES) {
-        static_for<4>([&](auto ec) {
-          constexpr int e = decltype(ec)::value;
-          u32x2_t v[D / 64][P];
 #pragma unroll
-          for (int i = 0; i < D / 64; ++i)
+        for (int i = 0; i < KS; ++i) kc[p][i] = *reinterpret_cast<const u32x2_t *>(k + (4 * i + g4) * 128 + l16 * 8);
 #pragma unroll
-            for (int p = 0; p < P; ++p)
-              v[i][p] = u32x2_t{pair_of_codes<F, e>(vc[p][i][0], vc[p][i][1]), pair_of_codes<F, e>(vc[p][i][2], vc[p][i][3])};
+        for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-          for (int step = 0; step < STEPS; ++step)
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) add(step, 4 * i + e, v[i]);
-        });
+          for (int n = 0; n < 4; ++n)
+            vc[p][i][n] = *reinterpret_cast<const uint32_t *>(v + (4 * n + g4) * D +
+                                                              ((4 * i + l16 / 4) ^ piece_xor(g4)) * 16 + l16 % 4 * 4);
       } else {
-        u32x2_t v[VB][P];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) kf[p][i] = *reinterpret_cast<const u32x4_t *>(k + i * 1024 + lane * 16);
+        // (16 lanes read 4 rows of 16 channels, 8 bytes each, and receive 4 rows of one)
+        const int r = 4 * g4 + l16 / 4;
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb)
-#pragma unroll
-          for (int p = 0; p < P; ++p) v[vb][p] = vf[p][vb];
-        // (in runs of 8 blocks: a product that adds to the one before it waits)
-#pragma unroll
-        for (int v0 = 0; v0 < VB; v0 += 8)
-#pragma unroll
-          for (int step = 0; step < STEPS; ++step)
-#pragma unroll
-            for (int vb = v0; vb < VB && vb < v0 + 8; ++vb) add(step, vb, v[vb]);
+          vf[p][vb] = __builtin_bit_cast(
+              u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                           (lds_s16x4_t *)(uint8_t __attribute__((address_space(3))) *)(
+                               v + r * ROW + ((2 * vb) ^ piece_xor(r)) * 16 + l16 % 4 * 8)));
       }
     }
-    if constexpr (!ALONE) {
-      wait_reads();
-      meet();                          // nobody reads this stage any more
-      issue(i0 + 2 * NT, buf);
-      buf ^= 1;
+    wait_reads();
+    issue(i0 + P);
+
+    // logits (a product that adds to the one before it waits out its latency: two
+    // sums where there is one part)
+    constexpr int CH = P == 1 ? 2 : 1;
+    f32x4_t z[P], zz[P][CH];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int c = 0; c < CH; ++c) zz[p][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        if constexpr (CODES) zz[p][i % CH] = product<F>(widen_codes<F>(kc[p][i]), q[i], zz[p][i % CH]);
+        else zz[p][i % CH] = product<F>(kf[p][i], q[i], zz[p][i % CH]);
+      }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      z[p] = zz[p][0];
+      if constexpr (CH == 2) z[p] += zz[p][1];
+    }
+    // (rows past the item's end have no weight)
+    float top = -FLT_MAX;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x = z[p][i] * near;
+        if constexpr (I8) x *= __uint_as_float(((i < 2 ? pairs[p].x : pairs[p].y) >> (16 * (i & 1)) & 255u) << 23);
+        if constexpr (I8 || F16) x *= rest;
+        z[p][i] = i < left[p] ? x : -INFINITY;
+        top = fmaxf(top, z[p][i]);
+      }
+    top = max_of_rows(top);
+    if (__any(top > m + 8.0f)) {
+      const float mn = fmaxf(m, top), f = exp2f(m - mn);
+      m = mn;
+      lsum *= f;
+#pragma unroll
+      for (int vb = 0; vb < VB; ++vb) o[vb] *= f;
+    }
+    u32x2_t term[P][F16 ? 2 : 3];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      float w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(z[p][i] - m);
+        lsum += w[i];
+        if constexpr (F16) w[i] *= 0x1p7f;       // clear of binary16's subnormals
+        // 2^-12 centres the range of weights times row scales
+        if constexpr (I8) {
+          const uint32_t pr = (i < 2 ? pairs[p].x : pairs[p].y) >> (16 * (i & 1));
+          w[i] = i < left[p] ? w[i] * 0x1p-12f * __uint_as_float((pr << 15) & 0x7f800000u) : 0.f;
+        }
+      }
+      if constexpr (F16) {
+        const f16x2_t a0 = {(_Float16)w[0], (_Float16)w[1]}, a1 = {(_Float16)w[2], (_Float16)w[3]};
+        const f16x2_t r0 = {(_Float16)(w[0] - (float)a0.x), (_Float16)(w[1] - (float)a0.y)},
+                      r1 = {(_Float16)(w[2] - (float)a1.x), (_Float16)(w[3] - (float)a1.y)};
+        term[p][0] = u32x2_t{__builtin_bit_cast(uint32_t, a0), __builtin_bit_cast(uint32_t, a1)};
+        term[p][1] = u32x2_t{__builtin_bit_cast(uint32_t, r0), __builtin_bit_cast(uint32_t, r1)};
+      } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          const u32x2_t x = {pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])};
+          term[p][k] = x;
+          w[0] -= bf_lo(x.x);
+          w[1] -= bf_hi(x.x);
+          w[2] -= bf_lo(x.y);
+          w[3] -= bf_hi(x.y);
+        }
+      }
+    }
+    // values: term by term over two parts; of a single part, the first two terms over
+    // the same V, then the third.  (The product of 16 places takes as long as that of
+    // 32; and compiled right behind one of 32 into the same accumulator, with no wait
+    // between, it gave wrong sums.)
+    constexpr int TERMS = F16 ? 2 : 3, STEPS = P == 1 ? TERMS - 1 : TERMS;
+    auto add = [&](int step, int vb, const u32x2_t (&v)[P]) {
+      if constexpr (P == 1) {
+        const u32x2_t x = term[0][2 * step], y = step == 0 ? term[0][1] : u32x2_t{0u, 0u};
+        o[vb] = product<F>(u32x4_t{v[0].x, v[0].y, v[0].x, v[0].y}, u32x4_t{x.x, x.y, y.x, y.y}, o[vb]);
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; p += 2) {
+          const u32x2_t x = term[p][step], y = term[p + 1][step];
+          o[vb] = product<F>(u32x4_t{v[p].x, v[p].y, v[p + 1].x, v[p + 1].y}, u32x4_t{x.x, x.y, y.x, y.y}, o[vb]);
+        }
+      }
+    };
+    if constexpr (CODES) {
+      static_for<4>([&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        u32x2_t v[D / 64][P];
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+          for (int p = 0; p < P; ++p)
+            v[i][p] = u32x2_t{pair_of_codes<F, e>(vc[p][i][0], vc[p][i][1]), pair_of_codes<F, e>(vc[p][i][2], vc[p][i][3])};
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step)
+#pragma unroll
+          for (int i = 0; i < D / 64; ++i) add(step, 4 * i + e, v[i]);
+      });
+    } else {
+      u32x2_t v[VB][P];
+#pragma unroll
+      for (int vb = 0; vb < VB; ++vb)
+#pragma unroll
+        for (int p = 0; p < P; ++p) v[vb][p] = vf[p][vb];
+      // (in runs of 8 blocks: a product that adds to the one before it waits)
+#pragma unroll
+      for (int v0 = 0; v0 < VB; v0 += 8)
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step)
+#pragma unroll
+          for (int vb = v0; vb < VB && vb < v0 + 8; ++vb) add(step, vb, v[vb]);
     }
   }
 
@@ -548,55 +470,46 @@ void decode_shared(SharedArgs a) {
   __syncthreads();
   const float back = I8 ? 0x1p6f : F16 ? 0x1p-7f : F == HWKV_KV_FP8_E4M3 ? hd.v_scale : 1.0f;
   const bool whole = nwg == 1 && !block && (rank >= a.n_full || a.seq_block[first] == kNoBlock);
-  const size_t part = block ? (size_t)rank * a.block_wgs + local : blockIdx.x;
-  for (int idx = threadIdx.x; idx < ncols * (D / 4); idx += WAVES * 64) {
-    const int col = idx / (D / 4), at = idx % (D / 4), c = col % 16, w0 = col / 16 * RW;
-    float M = sml[w0][0][c];
-    for (int w = 1; w < RW; ++w) M = fmaxf(M, sml[w0 + w][0][c]);
+  const size_t part = blockIdx.x;
+  for (int idx = threadIdx.x; idx < ncols * (D / 4); idx += kWaves * 64) {
+    const int c = idx / (D / 4), at = idx % (D / 4);
+    float M = sml[0][0][c];
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sml[w][0][c]);
     float L = 0.f;
     f32x4_t A = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int w = 0; w < RW; ++w) {
-      const float f = exp2f(sml[w0 + w][0][c] - M);
-      L += sml[w0 + w][1][c] * f;
-      A += reinterpret_cast<const f32x4_t *>(area + (w0 + w) * AW)[at * 16 + (c ^ (at & 15))] * f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = exp2f(sml[w][0][c] - M);
+      L += sml[w][1][c] * f;
+      A += reinterpret_cast<const f32x4_t *>(area + w * AW)[at * 16 + (c ^ (at & 15))] * f;
     }
     if (whole) {
-      const int64_t row = (int64_t)b0 * a.n_q_heads + h * a.group + col;
+      const int64_t row = (int64_t)b0 * a.n_q_heads + h * a.group + c;
       *reinterpret_cast<f32x4_t *>(a.out + row * D + 4 * at) = A * (back / L);
       continue;
     }
-    const size_t row = block ? part * CB + col : part * a.group + col;
+    const size_t row = part * (block ? 16 : a.group) + c;
     *reinterpret_cast<f32x4_t *>((block ? a.block_acc : a.own_acc) + row * D + 4 * at) = A * back;
     if (at == 0) *reinterpret_cast<f32x2_t *>((block ? a.block_ml : a.own_ml) + row * 2) = f32x2_t{M, L};
   }
 }
 
-template <int D, int F, int CW>
+template <int D, int F>
 hipError_t launch_shared(const SharedArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((decode_shared<D, F, CW>), dim3((unsigned)a.wg_begin[a.n_heads]), dim3(shared_threads(CW)), 0, s,
-                     a);
+  hipLaunchKernelGGL((decode_shared<D, F>), dim3((unsigned)a.wg_begin[a.n_heads]), dim3(kWaves * 64), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 template <int F>
-hipError_t launch_decode_shared_fmt(int D, int n_col_groups, const SharedArgs &a, hipStream_t s) {
-#define HWKV_SHARED(DD)                                              \
-  switch (n_col_groups) {                                            \
-    case 1: return launch_shared<DD, F, 1>(a, s);                    \
-    case 2: return launch_shared<DD, F, 2>(a, s);                    \
-    case 4: return launch_shared<DD, F, 4>(a, s);                    \
-    default: return hipErrorInvalidValue;                            \
-  }
+hipError_t launch_decode_shared_fmt(int D, const SharedArgs &a, hipStream_t s) {
   switch (D) {
-    case 64: HWKV_SHARED(64)
-    case 128: HWKV_SHARED(128)
-    case 256: HWKV_SHARED(256)
+    case 64: return launch_shared<64, F>(a, s);
+    case 128: return launch_shared<128, F>(a, s);
+    case 256: return launch_shared<256, F>(a, s);
     default: return hipErrorInvalidValue;
   }
-#undef HWKV_SHARED
 }
 
 }  // namespace hwkv

@@ -3,5 +3,5 @@
 #include "decode_shared.h"
 
 namespace hwkv {
-template hipError_t launch_decode_shared_fmt<HWKV_KV_FP8_E4M3>(int, int, const SharedArgs &, hipStream_t);
+template hipError_t launch_decode_shared_fmt<HWKV_KV_FP8_E4M3>(int, const SharedArgs &, hipStream_t);
 }  // namespace hwkv

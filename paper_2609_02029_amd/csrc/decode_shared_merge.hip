@@ -7,12 +7,17 @@
 namespace hwkv {
 
 // Instantiated in the per-format sources.
-extern template hipError_t launch_decode_shared_fmt<HWKV_KV_BF16>(int, int, const SharedArgs &, hipStream_t);
-extern template hipError_t launch_decode_shared_fmt<HWKV_KV_F16>(int, int, const SharedArgs &, hipStream_t);
-extern template hipError_t launch_decode_shared_fmt<HWKV_KV_FP8_E4M3>(int, int, const SharedArgs &, hipStream_t);
-extern template hipError_t launch_decode_shared_fmt<HWKV_KV_I8>(int, int, const SharedArgs &, hipStream_t);
+extern template hipError_t launch_decode_shared_fmt<HWKV_KV_BF16>(int, const SharedArgs &, hipStream_t);
+extern template hipError_t launch_decode_shared_fmt<HWKV_KV_F16>(int, const SharedArgs &, hipStream_t);
+extern template hipError_t launch_decode_shared_fmt<HWKV_KV_FP8_E4M3>(int, const SharedArgs &, hipStream_t);
+extern template hipError_t launch_decode_shared_fmt<HWKV_KV_I8>(int, const SharedArgs &, hipStream_t);
 
 namespace {
+
+// Workgroup j of n of column group cg, among all of a block's.
+__device__ __forceinline__ int block_wg(int j, int cg, int n, int groups) {
+  return (j & ~7) * groups + cg * min(8, n - (j & ~7)) + (j & 7);
+}
 
 // One workgroup per (sequence, q head): rows of D / 4 lanes take every R-th part, a
 // lane 4 channels, and meet in LDS.
@@ -24,16 +29,19 @@ __global__ __launch_bounds__(512) void shared_merge(SharedArgs a) {
   __shared__ float m_s[R], l_s[R];
   const int i = blockIdx.x, rank = blockIdx.y / a.group, g = blockIdx.y % a.group;
   // parts: of the sequence's block, then its own
-  int nb = 0, no, own0, step = 1;
-  size_t block0 = 0;
+  int nb = 0, no, own0, step = 1, groups = 1, cg = 0, block0 = 0, col = 0;
   if (rank < a.n_full) {
     const int b = a.seq_block[i];
     if (b != kNoBlock) {
-      nb = a.item_begin[b + 1] - a.item_begin[b];
-      block0 = ((size_t)rank * a.block_wgs + a.item_begin[b]) * (16 * a.n_col_groups) + (i - a.block_first[b]) * a.group + g;
+      col = (i - a.block_first[b]) * a.group + g;
+      groups = (a.block_count[b] * a.group + 15) / 16;
+      cg = col / 16;
+      nb = (a.item_begin[b + 1] - a.item_begin[b]) / groups;
+      block0 = a.item_begin[b] * a.n_full;
     }
     own0 = a.item_begin[a.n_blocks + i];
     no = a.item_begin[a.n_blocks + i + 1] - own0;
+    own0 -= a.block_wgs;
   } else {
     const int tiles = (min(a.len[i], a.head[rank].cap) + 63) / 64;
     no = (tiles + a.tiles_per_wg - 1) / a.tiles_per_wg;
@@ -52,7 +60,7 @@ __global__ __launch_bounds__(512) void shared_merge(SharedArgs a) {
     for (int k = 0; k < U; ++k) {
       const int j = min(j0 + k * R, n - 1);
       const bool of_block = j < nb;
-      const size_t p = of_block ? block0 + (size_t)j * (16 * a.n_col_groups)
+      const size_t p = of_block ? (size_t)(block0 + block_wg(rank * nb + j, cg, nb * a.n_full, groups)) * 16 + col % 16
                                 : (size_t)(a.wg_begin[rank] + own0 + (j - nb) * step) * a.group + g;
       ml[k] = *reinterpret_cast<const f32x2_t *>((of_block ? a.block_ml : a.own_ml) + p * 2);
       x[k] = *reinterpret_cast<const f32x4_t *>((of_block ? a.block_acc : a.own_acc) + p * D + c);
@@ -97,10 +105,10 @@ __global__ __launch_bounds__(512) void shared_merge(SharedArgs a) {
 
 hipError_t launch_decode_shared(int fmt, int D, const SharedArgs &a, hipStream_t s) {
   switch (fmt) {
-    case HWKV_KV_BF16: return launch_decode_shared_fmt<HWKV_KV_BF16>(D, a.n_col_groups, a, s);
-    case HWKV_KV_F16: return launch_decode_shared_fmt<HWKV_KV_F16>(D, a.n_col_groups, a, s);
-    case HWKV_KV_FP8_E4M3: return launch_decode_shared_fmt<HWKV_KV_FP8_E4M3>(D, a.n_col_groups, a, s);
-    case HWKV_KV_I8: return launch_decode_shared_fmt<HWKV_KV_I8>(D, a.n_col_groups, a, s);
+    case HWKV_KV_BF16: return launch_decode_shared_fmt<HWKV_KV_BF16>(D, a, s);
+    case HWKV_KV_F16: return launch_decode_shared_fmt<HWKV_KV_F16>(D, a, s);
+    case HWKV_KV_FP8_E4M3: return launch_decode_shared_fmt<HWKV_KV_FP8_E4M3>(D, a, s);
+    case HWKV_KV_I8: return launch_decode_shared_fmt<HWKV_KV_I8>(D, a, s);
     default: return hipErrorInvalidValue;
   }
 }

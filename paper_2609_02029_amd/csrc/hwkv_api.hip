@@ -3158,23 +3158,25 @@ int64_t find_families(const hwkv_cache *c, int32_t layer, int32_t unit, const st
   return whole;
 }
 
-// The column groups of 16 that the kernel is compiled for.
-int32_t column_groups(int64_t columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
+// Groups of 16 query columns.
+int64_t column_groups(int64_t columns) { return (columns + 15) / 16; }
 
 // Workgroups that a launch aims at: as many as run at once.
-int64_t shared_target(int32_t n_col_groups) { return (n_col_groups == 1 ? 2 : 1) * hwkv::device_cu_count(); }
+int64_t shared_target() { return 2 * hwkv::device_cu_count(); }
 
 // Most workgroups, and workgroups of blocks, of a launch of n_heads heads (n_full of
-// them full and paged) and n_seqs sequences.
-void shared_bounds(int64_t n_heads, int64_t n_full, int64_t n_seqs, int64_t *wgs, int64_t *block_wgs) {
+// them full and paged) and n_seqs sequences of G q heads: the target, or one for every
+// item (and column group of a block).
+void shared_bounds(int64_t n_heads, int64_t n_full, int64_t n_seqs, int64_t G, int64_t *wgs, int64_t *block_wgs) {
   const int64_t blocks = n_full > 0 ? std::min<int64_t>(hwkv::kSharedBlocks, n_seqs / 2) : 0;
-  *wgs = std::max(shared_target(1), n_heads * n_seqs + n_full * blocks);
-  *block_wgs = blocks > 0 ? std::max(shared_target(1), n_full * blocks) : 0;
+  const int64_t groups = blocks > 0 ? n_seqs * G / 16 + blocks : 0;
+  *wgs = std::max(shared_target(), n_heads * n_seqs + n_full * groups);
+  *block_wgs = blocks > 0 ? std::max(shared_target(), n_full * groups) : 0;
 }
 
 // Bytes of the parts of so many workgroups: acc and (m, l) of the blocks', then of all.
-size_t shared_part_bytes(const hwkv_policy &p, int64_t wgs, int64_t block_wgs, int32_t n_col_groups) {
-  const size_t rows = (size_t)block_wgs * 16 * n_col_groups + (size_t)wgs * (size_t)group_size(p);
+size_t shared_part_bytes(const hwkv_policy &p, int64_t wgs, int64_t block_wgs) {
+  const size_t rows = (size_t)block_wgs * 16 + (size_t)wgs * (size_t)group_size(p);
   return rows * (size_t)(p.head_dim + 2) * sizeof(float);
 }
 
@@ -3201,11 +3203,11 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
   }
   std::sort(families.begin(), families.end(),
             [](const Family &x, const Family &y) { return x.members[0] < y.members[0]; });
-  // blocks of at most kSharedColumns columns, and the sequences of none as one each
+  // blocks that a launch holds, and the sequences of none as one each
   std::vector<char> taken(B, 0);
   std::vector<Family> blocks;
   for (const Family &f : families) {
-    const int64_t n = (int64_t)f.members.size(), most = hwkv::kSharedColumns / G;
+    const int64_t n = (int64_t)f.members.size(), most = hwkv::kSharedSeqs;
     const int64_t parts = (n + most - 1) / most, per = (n + parts - 1) / parts;
     for (int64_t i = 0; i < n; i += per) {
       const auto at = f.members.begin() + i;
@@ -3225,7 +3227,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
   for (size_t next = 0; next < blocks.size();) {
     hwkv::SharedArgs a;
     std::memset(&a, 0, sizeof a);
-    int64_t columns = 0;
+    std::vector<int64_t> groups;                 // of a block's columns
     std::vector<int64_t> own;                    // tiles of a sequence's own rows in a full unit
     while (next < blocks.size() && a.n_seqs + blocks[next].members.size() <= (size_t)hwkv::kSharedSeqs) {
       const Family &f = blocks[next];
@@ -3234,7 +3236,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         a.block_pages[a.n_blocks] = f.pages;
         a.block_first[a.n_blocks] = (uint8_t)a.n_seqs;
         a.block_count[a.n_blocks] = (uint8_t)f.members.size();
-        columns = std::max<int64_t>(columns, (int64_t)f.members.size() * G);
+        groups.push_back(column_groups((int64_t)f.members.size() * G));
       }
       for (int32_t b : f.members) {
         a.seq[a.n_seqs] = (uint16_t)b;
@@ -3253,7 +3255,6 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
     a.n_q_heads = p.n_q_heads;
     a.group = (int32_t)G;
     a.max_pages = (int32_t)c->max_pages;
-    a.n_col_groups = column_groups(std::max(columns, G));
     a.scale_log2 = scale * 1.4426950408889634f;
     int64_t longest_len = 0;
     for (int32_t i = 0; i < a.n_seqs; ++i) longest_len = std::max<int64_t>(longest_len, a.len[i]);
@@ -3270,7 +3271,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
       const auto count = [&](int64_t T) {
         int64_t n = 0;
         if (a.n_full > 0) {
-          for (int32_t i = 0; i < a.n_blocks; ++i) n += (a.block_pages[i] * 4 + T - 1) / T;
+          for (int32_t i = 0; i < a.n_blocks; ++i) n += (a.block_pages[i] * 4 + T - 1) / T * groups[i];
           for (int64_t t : own) n += (t + T - 1) / T;
           n *= a.n_full;
         }
@@ -3278,7 +3279,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         return n;
       };
       for (int32_t i = 0; i < a.n_blocks && a.n_full > 0; ++i) {
-        total += (int64_t)a.block_pages[i] * 4 * a.n_full;
+        total += (int64_t)a.block_pages[i] * 4 * groups[i] * a.n_full;
         longest = std::max<int64_t>(longest, a.block_pages[i] * 4);
       }
       for (int64_t t : own) {
@@ -3289,7 +3290,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         total += window_tiles(r) * a.n_seqs;
         longest = std::max(longest, window_tiles(r));
       }
-      const int64_t target = shared_target(a.n_col_groups);
+      const int64_t target = shared_target();
       int64_t T = std::max<int64_t>(1, (total + target - 1) / target);
       while (T < longest && count(T) > target) T += 1 + T / 64;
       T = std::min(T, longest);
@@ -3299,7 +3300,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         int32_t k = 0;
         for (int32_t i = 0; i < a.n_blocks; ++i) {
           a.item_begin[k++] = (uint16_t)begin;
-          begin += (a.block_pages[i] * 4 + T - 1) / T;
+          begin += (a.block_pages[i] * 4 + T - 1) / T * groups[i];
         }
         a.block_wgs = (int32_t)begin;
         for (int64_t t : own) {
@@ -3311,8 +3312,8 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
       } else {
         a.block_wgs = 0;
       }
-      int64_t begin = 0;
       const int32_t items = a.n_blocks + a.n_seqs;
+      int64_t begin = (int64_t)a.n_full * a.block_wgs;
       for (int32_t r = 0; r < a.n_heads; ++r) {
         const int32_t h = heads[h0 + r], u = layer * H + h;
         hwkv::ItemHead &hd = a.head[r];
@@ -3327,18 +3328,18 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         else hd.k_scale = c->k_scale[u];
         a.head_id[r] = (uint8_t)h;
         a.wg_begin[r] = (int32_t)begin;
-        begin += r < a.n_full ? a.item_begin[items] : (window_tiles(r) + T - 1) / T * a.n_seqs;
+        begin += r < a.n_full ? a.item_begin[items] - a.block_wgs : (window_tiles(r) + T - 1) / T * a.n_seqs;
       }
       for (int32_t r = a.n_heads; r < hwkv::kMaxItems; ++r) a.wg_begin[r] = r == a.n_heads ? (int32_t)begin : INT32_MAX;
       launches.push_back({a, begin, (int64_t)a.n_full * a.block_wgs});
-      need = std::max(need, shared_part_bytes(p, begin, launches.back().block_wgs, a.n_col_groups));
+      need = std::max(need, shared_part_bytes(p, begin, launches.back().block_wgs));
     }
   }
   if (!ws || ws_bytes < need)
     return fail(HWKV_EINVAL, "workspace missing or too small (need " + std::to_string(need) + " bytes)");
   for (Launch &L : launches) {                   // (they use the workspace in turn)
     hwkv::SharedArgs &a = L.a;
-    const size_t cols = (size_t)L.block_wgs * 16 * a.n_col_groups, rows = (size_t)L.wgs * G;
+    const size_t cols = (size_t)L.block_wgs * 16, rows = (size_t)L.wgs * G;
     a.block_acc = static_cast<float *>(ws);
     a.own_acc = a.block_acc + cols * D;
     a.block_ml = a.own_acc + rows * D;
@@ -3364,10 +3365,9 @@ int hwkv_decode_shared_workspace_bytes(const hwkv_cache *c, size_t *bytes) {
     int64_t n_full = 0;
     for (int32_t h = 0; h < H && c->paged; ++h) n_full += c->full_index[l * H + h] >= 0 ? 1 : 0;
     int64_t wgs = 0, block_wgs = 0;
-    shared_bounds(std::min<int64_t>(hwkv::kSharedHeads, H), std::min<int64_t>(hwkv::kSharedHeads, n_full), seqs, &wgs,
-                  &block_wgs);
-    const int64_t columns = std::min<int64_t>(hwkv::kSharedColumns, seqs * G);
-    most = std::max(most, shared_part_bytes(p, wgs, block_wgs, column_groups(columns)));
+    shared_bounds(std::min<int64_t>(hwkv::kSharedHeads, H), std::min<int64_t>(hwkv::kSharedHeads, n_full), seqs, G,
+                  &wgs, &block_wgs);
+    most = std::max(most, shared_part_bytes(p, wgs, block_wgs));
   }
   *bytes = most;
   return ok();

@@ -242,22 +242,23 @@ struct PageUpdateArgs {
 };
 
 // Decode of sequences that share pages (decode_shared.h): one launch for up to
-// kSharedSeqs sequences and kSharedHeads KV heads.  Full units of a paged cache come
-// first; their items are the blocks (sequences [block_first, + block_count) share the
-// pages [0, block_pages)), then the sequences, each from its block's pages on.  The
-// other units have every sequence's rows as an item, splits[] workgroups each, split
-// by split (of which a shorter sequence leaves the last ones empty).
+// kSharedSeqs sequences and kSharedHeads KV heads.  First come the blocks (sequences
+// [block_first, + block_count) share the pages [0, block_pages)), each of all full and
+// paged heads in turn; then, head by head, the sequences' rows from their block's pages
+// on; then the other heads, of which every sequence has as many workgroups as the
+// longest, split by split (a shorter one leaves its last ones empty).
 constexpr int kSharedSeqs = 96, kSharedBlocks = 48, kSharedHeads = 32, kSharedItems = 192;
-constexpr int kSharedColumns = 64;   // of a block, at most
 constexpr uint8_t kNoBlock = 255;
 static_assert(kSharedItems > kSharedSeqs + kSharedBlocks, "an entry past the last item");
 struct SharedArgs {
   ItemHead head[kSharedHeads];       // in launch order
-  int32_t wg_begin[kMaxItems];       // first workgroup; [n_heads]: all; INT32_MAX past that
+  int32_t wg_begin[kMaxItems];       // first workgroup behind the blocks'; [n_heads]: all;
+                                     //   INT32_MAX past that
   int32_t len[kSharedSeqs];
   int32_t block_pages[kSharedBlocks];
   uint16_t seq[kSharedSeqs];         // the cache's sequence
-  uint16_t item_begin[kSharedItems]; // of a full unit's workgroups; UINT16_MAX past the last
+  uint16_t item_begin[kSharedItems]; // of a full head's workgroups: blocks, then sequences;
+                                     //   UINT16_MAX past the last
   uint8_t head_id[kSharedHeads];     // the KV head
   uint8_t block_first[kSharedBlocks], block_count[kSharedBlocks];
   uint8_t seq_block[kSharedSeqs];    // or kNoBlock
@@ -265,16 +266,16 @@ struct SharedArgs {
   const int32_t *page_table;
   const uint16_t *q;                 // [batch][Hq][D]
   float *out;
-  float *block_acc, *block_ml;       // [n_full * block_wgs][16 n_col_groups][D], [2]
+  float *block_acc, *block_ml;       // [n_full * block_wgs][16][D], [2]
   float *own_acc, *own_ml;           // [workgroup][G][D], [2]
   int64_t pool_off;
   int32_t n_heads, n_full, n_seqs, n_blocks, block_wgs, n_q_heads, group, max_pages;
-  int32_t tiles_per_wg, n_col_groups;
+  int32_t tiles_per_wg;
   float scale_log2;
 };
 hipError_t launch_decode_shared(int fmt, int D, const SharedArgs &a, hipStream_t s);
 template <int F>
-hipError_t launch_decode_shared_fmt(int D, int n_col_groups, const SharedArgs &a, hipStream_t s);
+hipError_t launch_decode_shared_fmt(int D, const SharedArgs &a, hipStream_t s);
 hipError_t launch_shared_merge(int D, const SharedArgs &a, hipStream_t s);
 
 // Rows of whole sequences copied within a cache, or from one buffer into another of
