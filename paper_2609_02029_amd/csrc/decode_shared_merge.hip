@@ -14,9 +14,9 @@ extern template hipError_t launch_decode_shared_fmt<HWKV_KV_I8>(int, const Share
 
 namespace {
 
-// Workgroup j of n of column group cg, among all of a block's.
-__device__ __forceinline__ int block_wg(int j, int cg, int n, int groups) {
-  return (j & ~7) * groups + cg * min(8, n - (j & ~7)) + (j & 7);
+// Workgroup j of n of turn `turn`, among all of a block's.
+__device__ __forceinline__ int block_wg(int j, int turn, int n, int turns) {
+  return (j & ~7) * turns + turn * min(8, n - (j & ~7)) + (j & 7);
 }
 
 // One workgroup per (sequence, q head): rows of D / 4 lanes take every R-th part, a
@@ -29,14 +29,15 @@ __global__ __launch_bounds__(512) void shared_merge(SharedArgs a) {
   __shared__ float m_s[R], l_s[R];
   const int i = blockIdx.x, rank = blockIdx.y / a.group, g = blockIdx.y % a.group;
   // parts: of the sequence's block, then its own
-  int nb = 0, no, own0, step = 1, groups = 1, cg = 0, block0 = 0, col = 0;
+  const int width = 16 * a.col_groups;
+  int nb = 0, no, own0, step = 1, turns = 1, turn = 0, block0 = 0, col = 0;
   if (rank < a.n_full) {
     const int b = a.seq_block[i];
     if (b != kNoBlock) {
       col = (i - a.block_first[b]) * a.group + g;
-      groups = (a.block_count[b] * a.group + 15) / 16;
-      cg = col / 16;
-      nb = (a.item_begin[b + 1] - a.item_begin[b]) / groups;
+      turns = (a.block_count[b] * a.group + width - 1) / width;
+      turn = col / width;
+      nb = (a.item_begin[b + 1] - a.item_begin[b]) / turns;
       block0 = a.item_begin[b] * a.n_full;
     }
     own0 = a.item_begin[a.n_blocks + i];
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(512) void shared_merge(SharedArgs a) {
     for (int k = 0; k < U; ++k) {
       const int j = min(j0 + k * R, n - 1);
       const bool of_block = j < nb;
-      const size_t p = of_block ? (size_t)(block0 + block_wg(rank * nb + j, cg, nb * a.n_full, groups)) * 16 + col % 16
+      const size_t p = of_block ? (size_t)(block0 + block_wg(rank * nb + j, turn, nb * a.n_full, turns)) * width + col % width
                                 : (size_t)(a.wg_begin[rank] + own0 + (j - nb) * step) * a.group + g;
       ml[k] = *reinterpret_cast<const f32x2_t *>((of_block ? a.block_ml : a.own_ml) + p * 2);
       x[k] = *reinterpret_cast<const f32x4_t *>((of_block ? a.block_acc : a.own_acc) + p * D + c);

@@ -3161,8 +3161,20 @@ int64_t find_families(const hwkv_cache *c, int32_t layer, int32_t unit, const st
 // Groups of 16 query columns.
 int64_t column_groups(int64_t columns) { return (columns + 15) / 16; }
 
-// Workgroups that a launch aims at: as many as run at once.
-int64_t shared_target() { return 2 * hwkv::device_cu_count(); }
+// Workgroups that a launch aims at: as many as run at once (column groups that share a
+// workgroup take its registers and LDS for themselves).
+int64_t shared_target(int32_t col_groups) { return (col_groups == 1 ? 2 : 1) * hwkv::device_cu_count(); }
+
+// What a tile of a block costs a workgroup, in 16ths of one of 16 columns: with more
+// column groups it takes the same bytes and more products.  (One full head of four,
+// 256 x 6, 8 sequences over 112,000 shared rows, weights of 1 / 1.25 / 1.5 / 2 / 3: bf16
+// 91.3 / 82.9 / 82.8 / 85.0 / 90.0 us, fp8 65.5 / 60.8 / 56.0 / 51.9 / 54.8, int8 75.8 /
+// 69.9 / 64.0 / 58.3 / 63.2; 5 sequences, two groups: bf16 66.2 / 63.7 / 65.2 / 68.4,
+// fp8 44.4 / 42.8 / 40.9 / 43.2, int8 50.2 / 48.0 / 45.8 / 47.7 for 1 / 1.25 / 1.5 / 2.)
+int64_t block_tile_weight(int fmt, int32_t col_groups) {
+  const bool codes = fmt == HWKV_KV_FP8_E4M3 || fmt == HWKV_KV_I8;
+  return 16 + (codes ? 8 : 3) * (col_groups - 1);
+}
 
 // Most workgroups, and workgroups of blocks, of a launch of n_heads heads (n_full of
 // them full and paged) and n_seqs sequences of G q heads: the target, or one for every
@@ -3170,13 +3182,14 @@ int64_t shared_target() { return 2 * hwkv::device_cu_count(); }
 void shared_bounds(int64_t n_heads, int64_t n_full, int64_t n_seqs, int64_t G, int64_t *wgs, int64_t *block_wgs) {
   const int64_t blocks = n_full > 0 ? std::min<int64_t>(hwkv::kSharedBlocks, n_seqs / 2) : 0;
   const int64_t groups = blocks > 0 ? n_seqs * G / 16 + blocks : 0;
-  *wgs = std::max(shared_target(), n_heads * n_seqs + n_full * groups);
-  *block_wgs = blocks > 0 ? std::max(shared_target(), n_full * groups) : 0;
+  *wgs = std::max(shared_target(1), n_heads * n_seqs + n_full * groups);
+  *block_wgs = blocks > 0 ? std::max(shared_target(1), n_full * groups) : 0;
 }
 
-// Bytes of the parts of so many workgroups: acc and (m, l) of the blocks', then of all.
-size_t shared_part_bytes(const hwkv_policy &p, int64_t wgs, int64_t block_wgs) {
-  const size_t rows = (size_t)block_wgs * 16 + (size_t)wgs * (size_t)group_size(p);
+// Bytes of the parts of so many workgroups: acc and (m, l) of the blocks' (of
+// col_groups x 16 columns), then of all.
+size_t shared_part_bytes(const hwkv_policy &p, int64_t wgs, int64_t block_wgs, int32_t col_groups) {
+  const size_t rows = (size_t)block_wgs * 16 * col_groups + (size_t)wgs * (size_t)group_size(p);
   return rows * (size_t)(p.head_dim + 2) * sizeof(float);
 }
 
@@ -3227,7 +3240,8 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
   for (size_t next = 0; next < blocks.size();) {
     hwkv::SharedArgs a;
     std::memset(&a, 0, sizeof a);
-    std::vector<int64_t> groups;                 // of a block's columns
+    std::vector<int64_t> turns;                  // of a block: workgroups that read a tile
+    int64_t groups = 1;                          // most of a block's columns
     std::vector<int64_t> own;                    // tiles of a sequence's own rows in a full unit
     while (next < blocks.size() && a.n_seqs + blocks[next].members.size() <= (size_t)hwkv::kSharedSeqs) {
       const Family &f = blocks[next];
@@ -3236,7 +3250,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         a.block_pages[a.n_blocks] = f.pages;
         a.block_first[a.n_blocks] = (uint8_t)a.n_seqs;
         a.block_count[a.n_blocks] = (uint8_t)f.members.size();
-        groups.push_back(column_groups((int64_t)f.members.size() * G));
+        groups = std::max(groups, column_groups((int64_t)f.members.size() * G));
       }
       for (int32_t b : f.members) {
         a.seq[a.n_seqs] = (uint16_t)b;
@@ -3256,6 +3270,10 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
     a.group = (int32_t)G;
     a.max_pages = (int32_t)c->max_pages;
     a.scale_log2 = scale * 1.4426950408889634f;
+    const int64_t most_turns = (groups + hwkv::kSharedGroups - 1) / hwkv::kSharedGroups;
+    a.col_groups = (int32_t)((groups + most_turns - 1) / most_turns);
+    for (int32_t i = 0; i < a.n_blocks; ++i)
+      turns.push_back((column_groups(a.block_count[i] * G) + a.col_groups - 1) / a.col_groups);
     int64_t longest_len = 0;
     for (int32_t i = 0; i < a.n_seqs; ++i) longest_len = std::max<int64_t>(longest_len, a.len[i]);
     for (int32_t h0 = 0; h0 < H; h0 += hwkv::kSharedHeads) {
@@ -3265,13 +3283,18 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
       // tiles per workgroup: the least at which the launch has no more workgroups than
       // it aims at, or one for every item
       int64_t total = 0, longest = 1;
+      const int64_t weight = block_tile_weight(c->fmt, a.col_groups);
+      const auto block_splits = [&](int32_t i, int64_t T) {
+        const int64_t tiles = (int64_t)a.block_pages[i] * 4;
+        return std::min(tiles, (tiles * weight + 16 * T - 1) / (16 * T));
+      };
       const auto window_tiles = [&](int32_t r) {
         return tiles_for(std::min(longest_len, c->cap[layer * H + heads[h0 + r]]));
       };
       const auto count = [&](int64_t T) {
         int64_t n = 0;
         if (a.n_full > 0) {
-          for (int32_t i = 0; i < a.n_blocks; ++i) n += (a.block_pages[i] * 4 + T - 1) / T * groups[i];
+          for (int32_t i = 0; i < a.n_blocks; ++i) n += block_splits(i, T) * turns[i];
           for (int64_t t : own) n += (t + T - 1) / T;
           n *= a.n_full;
         }
@@ -3279,8 +3302,8 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         return n;
       };
       for (int32_t i = 0; i < a.n_blocks && a.n_full > 0; ++i) {
-        total += (int64_t)a.block_pages[i] * 4 * groups[i] * a.n_full;
-        longest = std::max<int64_t>(longest, a.block_pages[i] * 4);
+        total += (int64_t)a.block_pages[i] * 4 * weight / 16 * turns[i] * a.n_full;
+        longest = std::max<int64_t>(longest, (int64_t)a.block_pages[i] * 4 * weight / 16);
       }
       for (int64_t t : own) {
         total += a.n_full > 0 ? t * a.n_full : 0;
@@ -3290,7 +3313,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         total += window_tiles(r) * a.n_seqs;
         longest = std::max(longest, window_tiles(r));
       }
-      const int64_t target = shared_target();
+      const int64_t target = shared_target(a.col_groups);
       int64_t T = std::max<int64_t>(1, (total + target - 1) / target);
       while (T < longest && count(T) > target) T += 1 + T / 64;
       T = std::min(T, longest);
@@ -3300,7 +3323,7 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
         int32_t k = 0;
         for (int32_t i = 0; i < a.n_blocks; ++i) {
           a.item_begin[k++] = (uint16_t)begin;
-          begin += (a.block_pages[i] * 4 + T - 1) / T * groups[i];
+          begin += block_splits(i, T) * turns[i];
         }
         a.block_wgs = (int32_t)begin;
         for (int64_t t : own) {
@@ -3332,14 +3355,14 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
       }
       for (int32_t r = a.n_heads; r < hwkv::kMaxItems; ++r) a.wg_begin[r] = r == a.n_heads ? (int32_t)begin : INT32_MAX;
       launches.push_back({a, begin, (int64_t)a.n_full * a.block_wgs});
-      need = std::max(need, shared_part_bytes(p, begin, launches.back().block_wgs));
+      need = std::max(need, shared_part_bytes(p, begin, launches.back().block_wgs, a.col_groups));
     }
   }
   if (!ws || ws_bytes < need)
     return fail(HWKV_EINVAL, "workspace missing or too small (need " + std::to_string(need) + " bytes)");
   for (Launch &L : launches) {                   // (they use the workspace in turn)
     hwkv::SharedArgs &a = L.a;
-    const size_t cols = (size_t)L.block_wgs * 16, rows = (size_t)L.wgs * G;
+    const size_t cols = (size_t)L.block_wgs * 16 * a.col_groups, rows = (size_t)L.wgs * G;
     a.block_acc = static_cast<float *>(ws);
     a.own_acc = a.block_acc + cols * D;
     a.block_ml = a.own_acc + rows * D;
@@ -3367,7 +3390,7 @@ int hwkv_decode_shared_workspace_bytes(const hwkv_cache *c, size_t *bytes) {
     int64_t wgs = 0, block_wgs = 0;
     shared_bounds(std::min<int64_t>(hwkv::kSharedHeads, H), std::min<int64_t>(hwkv::kSharedHeads, n_full), seqs, G,
                   &wgs, &block_wgs);
-    most = std::max(most, shared_part_bytes(p, wgs, block_wgs));
+    most = std::max(most, shared_part_bytes(p, wgs, block_wgs, hwkv::kSharedGroups));
   }
   *bytes = most;
   return ok();

@@ -248,6 +248,7 @@ struct PageUpdateArgs {
 // on; then the other heads, of which every sequence has as many workgroups as the
 // longest, split by split (a shorter one leaves its last ones empty).
 constexpr int kSharedSeqs = 96, kSharedBlocks = 48, kSharedHeads = 32, kSharedItems = 192;
+constexpr int kSharedGroups = 3;
 constexpr uint8_t kNoBlock = 255;
 static_assert(kSharedItems > kSharedSeqs + kSharedBlocks, "an entry past the last item");
 struct SharedArgs {
@@ -266,11 +267,12 @@ struct SharedArgs {
   const int32_t *page_table;
   const uint16_t *q;                 // [batch][Hq][D]
   float *out;
-  float *block_acc, *block_ml;       // [n_full * block_wgs][16][D], [2]
+  float *block_acc, *block_ml;       // [n_full * block_wgs][16 col_groups][D], [2]
   float *own_acc, *own_ml;           // [workgroup][G][D], [2]
   int64_t pool_off;
   int32_t n_heads, n_full, n_seqs, n_blocks, block_wgs, n_q_heads, group, max_pages;
-  int32_t tiles_per_wg;
+  int32_t tiles_per_wg, col_groups;  // col_groups: of 16 columns a workgroup of a block, 1 to
+                                     //   kSharedGroups
   float scale_log2;
 };
 hipError_t launch_decode_shared(int fmt, int D, const SharedArgs &a, hipStream_t s);
