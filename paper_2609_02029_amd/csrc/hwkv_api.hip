@@ -2648,16 +2648,36 @@ struct Move {
   int32_t src, dst;
   int64_t rows;
 };
-int launch_moves(const hwkv_cache *c, const Move *moves, size_t n, const uint8_t *from, uint8_t *to,
+// Moves in rounds of kMoveRound (rows 0: none) and launches of kMaxMoves; at the places in
+// `parts`, and at every launch, begins a run of rounds that touches no sequence of the
+// launch's others.
+struct MovePlan {
+  std::vector<Move> moves;
+  std::vector<size_t> parts;
+  size_t launch_end(size_t i) const { return std::min(moves.size(), i + hwkv::kMaxMoves); }
+  // The parts of the launch from i on, as rounds of it.
+  int32_t rounds(size_t i, uint8_t *part) const {
+    const size_t end = launch_end(i), R = hwkv::kMoveRound;
+    int32_t n = 0;
+    part[n++] = 0;
+    for (auto at = std::upper_bound(parts.begin(), parts.end(), i); at != parts.end() && *at < end; ++at)
+      part[n++] = (uint8_t)((*at - i) / R);
+    part[n] = (uint8_t)((end - i + R - 1) / R);
+    return n;
+  }
+};
+
+int launch_moves(const hwkv_cache *c, const MovePlan &plan, size_t first, const uint8_t *from, uint8_t *to,
                  hipStream_t s) {
-  if (n == 0) return HWKV_OK;
+  const Move *const moves = &plan.moves[first];
+  const size_t n = plan.launch_end(first) - first;
   hwkv::MoveArgs a;
   std::memset(&a, 0, sizeof a);
   a.from = from;
   a.to = to;
   a.row_bytes = row_bytes(c);
   a.pair_bytes = (int32_t)row_scale_bytes(c->fmt);
-  a.n_moves = (int32_t)((n + hwkv::kMoveRound - 1) / hwkv::kMoveRound * hwkv::kMoveRound);
+  a.n_parts = plan.rounds(first, a.part);
   int64_t most = 0;
   for (size_t i = 0; i < n; ++i) {
     a.src[i] = (uint16_t)moves[i].src;
@@ -2692,53 +2712,76 @@ int launch_moves(const hwkv_cache *c, const Move *moves, size_t n, const uint8_t
   return HWKV_OK;
 }
 
-// The moves parent[b] -> b of the sequences that change (and whose parent has
-// rows), in an order in which no source is overwritten before it has been read:
-// sequences without a child that is still to be written first, then the cycles
-// that are left.  Within a round all is read before anything is written, so a cycle
-// lies in one round, or starts one and goes through the carry.  EINVAL where a cycle
-// is longer than a launch.
-int plan_moves(const hwkv_cache *c, const int32_t *parent, std::vector<Move> *out) {
+// The moves parent[b] -> b of the sequences that change, in an order in which no source
+// is overwritten before it has been read: of the sequences that hang together (by
+// parents), first those without a child that is still to be written, then the cycle
+// that is left.  Within a round all is read before anything is written, so a cycle lies
+// in one round, or starts one and goes through the carry.  Those that hang together
+// begin a part where they begin a round, and do so where they would not fit the one
+// before.  EINVAL where a cycle is longer than a launch.
+int plan_moves(const hwkv_cache *c, const int32_t *parent, MovePlan *out) {
   const int32_t B = c->batch;
+  const size_t R = hwkv::kMoveRound, M = hwkv::kMaxMoves;
   std::vector<int32_t> waits(B, 0), ready;       // children of b still to be written
   std::vector<char> todo(B, 0);
-  ready.reserve(B);
-  out->reserve(2 * (size_t)B + 4 * hwkv::kMoveRound);
+  // the sequences that hang together: b's first one, and the next one behind b
+  std::vector<int32_t> root(B), next(B, -1), last(B), size(B, 0);
+  for (int32_t b = 0; b < B; ++b) root[b] = b;
+  const auto find = [&](int32_t b) {
+    while (root[b] != b) b = root[b] = root[root[b]];
+    return b;
+  };
   for (int32_t b = 0; b < B; ++b)
     if (parent[b] != b && parent[b] >= 0) {
       todo[b] = 1;
       ++waits[parent[b]];
+      const int32_t x = find(b), y = find(parent[b]);
+      root[std::max(x, y)] = std::min(x, y);
     }
-  for (int32_t b = 0; b < B; ++b)
-    if (todo[b] && waits[b] == 0) ready.push_back(b);
-  for (size_t i = 0; i < ready.size(); ++i) {
-    const int32_t b = ready[i], p = parent[b];
-    out->push_back({p, b, most_rows(c, p)});
-    todo[b] = 0;
-    if (--waits[p] == 0 && todo[p]) ready.push_back(p);
-  }
-  const auto end_round = [&]() {
-    while (out->size() % hwkv::kMoveRound != 0) out->push_back({0, 0, 0});
-  };
   for (int32_t b = 0; b < B; ++b) {
-    if (!todo[b]) continue;
-    size_t len = 0;
+    const int32_t x = find(b);
+    if (x != b) next[last[x]] = b;
+    last[x] = b;
+    size[x] += todo[b];
+  }
+  std::vector<Move> &moves = out->moves;
+  ready.reserve(B);
+  moves.reserve(2 * (size_t)B + M);
+  out->parts.reserve((size_t)B + 1);
+  const auto end_round = [&]() {
+    while (moves.size() % R != 0) moves.push_back({0, 0, 0});
+  };
+  for (int32_t first = 0; first < B; ++first) {
+    if (root[first] != first || size[first] == 0) continue;
+    if (moves.size() % R + (size_t)size[first] > R) end_round();
+    if (moves.size() % R == 0) out->parts.push_back(moves.size());
+    ready.clear();
+    for (int32_t b = first; b >= 0; b = next[b])
+      if (todo[b] && waits[b] == 0) ready.push_back(b);
+    for (size_t i = 0; i < ready.size(); ++i) {
+      const int32_t b = ready[i], p = parent[b];
+      moves.push_back({p, b, most_rows(c, p)});
+      todo[b] = 0;
+      if (--waits[p] == 0 && todo[p]) ready.push_back(p);
+    }
+    int32_t b = first;
+    while (b >= 0 && !todo[b]) b = next[b];
+    if (b < 0) continue;
+    size_t len = 0;                  // (one cycle: each sequence has one parent)
     for (int32_t x = b; len == 0 || x != b; x = parent[x]) ++len;
-    const size_t R = hwkv::kMoveRound;
     const bool carried = len > R;
-    if (len + 1 > (size_t)hwkv::kMaxMoves)
-      return fail(HWKV_EINVAL, "a cycle of " + std::to_string(len) + " sequences (at most " +
-                                   std::to_string(hwkv::kMaxMoves - 1) + ")");
-    if (carried || out->size() % R + len > R) end_round();
+    if (len + 1 > M)
+      return fail(HWKV_EINVAL, "a cycle of " + std::to_string(len) + " sequences (at most " + std::to_string(M - 1) + ")");
+    if (carried || moves.size() % R + len > R) end_round();
     // (a launch takes whole rounds, and a carry does not outlive it)
-    if (carried && out->size() % hwkv::kMaxMoves + len + 1 > (size_t)hwkv::kMaxMoves)
-      while (out->size() % hwkv::kMaxMoves != 0) out->push_back({0, 0, 0});
+    if (carried && moves.size() % M + len + 1 > M)
+      while (moves.size() % M != 0) moves.push_back({0, 0, 0});
     const int64_t first_rows = most_rows(c, b);
-    if (carried) out->push_back({b, hwkv::kMoveCarry, first_rows});
+    if (carried) moves.push_back({b, hwkv::kMoveCarry, first_rows});
     int32_t x = b;
     do {
       const int32_t p = parent[x];
-      out->push_back({carried && p == b ? (int32_t)hwkv::kMoveCarry : p, x, p == b ? first_rows : most_rows(c, p)});
+      moves.push_back({carried && p == b ? (int32_t)hwkv::kMoveCarry : p, x, p == b ? first_rows : most_rows(c, p)});
       todo[x] = 0;
       x = p;
     } while (x != b);
@@ -2909,8 +2952,9 @@ int reorder_pages(hwkv_cache *c, const int32_t *parent, PagePlan *P) {
 // Copies the pages of a reorder and brings the device's table in line: by its changed
 // entries, or, where these are many, row by row as the sequences move (a fork of 30,000
 // tokens, 128 full units, eight ways: 105,000 entries, 435 us against 1,784 as lists;
-// 384 sequences permuted, 4,600 entries: 230 us against 263).
-int launch_page_copies(const hwkv_cache *c, const PagePlan &P, const std::vector<Move> &moves, hipStream_t s) {
+// 384 sequences permuted, 4,600 entries: 217 us against 263).
+int launch_page_copies(const hwkv_cache *c, const PagePlan &P, const MovePlan &plan, hipStream_t s) {
+  const std::vector<Move> &moves = plan.moves;
   size_t i = 0, e = 0;
   if (P.entries.size() > 2 * hwkv::kMaxEntries && P.n_full <= UINT16_MAX) {
     e = P.entries.size();
@@ -2920,8 +2964,8 @@ int launch_page_copies(const hwkv_cache *c, const PagePlan &P, const std::vector
     t.batch = c->batch;
     t.max_pages = (int32_t)c->max_pages;
     for (size_t m = 0; m < moves.size(); m += hwkv::kMaxMoves) {
-      const size_t n = std::min<size_t>(hwkv::kMaxMoves, moves.size() - m);
-      t.n_moves = (int32_t)((n + hwkv::kMoveRound - 1) / hwkv::kMoveRound * hwkv::kMoveRound);
+      const size_t n = plan.launch_end(m) - m;
+      t.n_parts = plan.rounds(m, t.part);
       t.most = 0;
       for (size_t k = 0; k < hwkv::kMaxMoves; ++k) {
         t.src[k] = k < n ? (uint16_t)moves[m + k].src : 0;
@@ -2957,8 +3001,8 @@ int launch_page_copies(const hwkv_cache *c, const PagePlan &P, const std::vector
 }
 
 int reorder_impl(hwkv_cache *c, const int32_t *parent, hipStream_t s) {
-  std::vector<Move> moves;
-  int rc = plan_moves(c, parent, &moves);
+  MovePlan plan;
+  int rc = plan_moves(c, parent, &plan);
   if (rc != HWKV_OK) return rc;
   PagePlan P;
   std::vector<int64_t> n(c->n);
@@ -2967,9 +3011,9 @@ int reorder_impl(hwkv_cache *c, const int32_t *parent, hipStream_t s) {
   for (int32_t l = 0; l < c->pol.n_layers; ++l)
     for (int32_t b = 0; b < c->batch; ++b)
       c->n[(size_t)l * c->batch + b] = parent[b] < 0 ? 0 : n[(size_t)l * c->batch + parent[b]];
-  rc = launch_page_copies(c, P, moves, s);
-  for (size_t i = 0; rc == HWKV_OK && i < moves.size(); i += hwkv::kMaxMoves)
-    rc = launch_moves(c, &moves[i], std::min<size_t>(hwkv::kMaxMoves, moves.size() - i), c->base, c->base, s);
+  rc = launch_page_copies(c, P, plan, s);
+  for (size_t i = 0; rc == HWKV_OK && i < plan.moves.size(); i += hwkv::kMaxMoves)
+    rc = launch_moves(c, plan, i, c->base, c->base, s);
   return rc;
 }
 
@@ -3007,9 +3051,12 @@ int move_impl(hwkv_cache *c, int64_t n_pages, void *dev_buf, size_t buf_bytes, h
     return fail(HWKV_ENOMEM, "a pool of " + std::to_string(n_pages) + " pages for " + std::to_string(used) +
                                  " pages in use");
   for (int64_t i = n_pages - 1; c->paged && i >= used; --i) to.free_list.push_back((int32_t)i);
-  std::vector<Move> moves;
-  for (int32_t b = 0; b < B; ++b)
-    if (most_rows(c, b) > 0) moves.push_back({b, b, most_rows(c, b)});
+  MovePlan plan;
+  for (int32_t b = 0; b < B; ++b) {
+    if (most_rows(c, b) == 0) continue;
+    if (plan.moves.size() % hwkv::kMoveRound == 0) plan.parts.push_back(plan.moves.size());
+    plan.moves.push_back({b, b, most_rows(c, b)});
+  }
 
   const bool owned = dev_buf == nullptr;
   if (!owned) {
@@ -3046,8 +3093,8 @@ int move_impl(hwkv_cache *c, int64_t n_pages, void *dev_buf, size_t buf_bytes, h
     for (; k < hwkv::kMaxRuns; ++k) a.run[k].begin = INT32_MAX;
     rc = check_device(hwkv::launch_page_move(a, s), "page move launch");
   }
-  for (size_t i = 0; rc == HWKV_OK && i < moves.size(); i += hwkv::kMaxMoves)
-    rc = launch_moves(c, &moves[i], std::min<size_t>(hwkv::kMaxMoves, moves.size() - i), c->base, base, s);
+  for (size_t i = 0; rc == HWKV_OK && i < plan.moves.size(); i += hwkv::kMaxMoves)
+    rc = launch_moves(c, plan, i, c->base, base, s);
   if (rc == HWKV_OK && c->owned) {
     rc = check_device(hipStreamSynchronize(s), "hipStreamSynchronize");
     if (rc == HWKV_OK) rc = check_device(hipFree(c->base), "hipFree");

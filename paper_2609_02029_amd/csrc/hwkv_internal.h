@@ -284,10 +284,12 @@ hipError_t launch_shared_merge(int D, const SharedArgs &a, hipStream_t s);
 // the same layout (reorder_kernels.hip): moves src -> dst in rounds of kMoveRound,
 // each reading all its sources before it writes.  A cycle longer than a round keeps
 // its first sequence's rows in registers (dst kMoveCarry) until its last move (src
-// kMoveCarry).  Every unit with a region: workgroups [wg_begin, that of the next
+// kMoveCarry).  Rounds come in parts that touch different sequences, one grid row each.
+// Every unit with a region: workgroups [wg_begin, that of the next
 // unit) take kMoveChunks x 256 chunks of 16 bytes each, of K, then V, then scale
 // pairs.
 constexpr int kMaxMoves = 192, kMoveRound = 8, kMoveChunks = 2;
+constexpr int kMaxRounds = kMaxMoves / kMoveRound;
 constexpr uint16_t kMoveCarry = 0xffff;
 struct MoveUnit {
   int64_t k_off, v_off, s_off;   // byte offsets of sequence 0
@@ -298,9 +300,10 @@ struct MoveArgs {
   int32_t wg_begin[kMaxItems + 1];   // INT32_MAX past the last
   int32_t n[kMaxMoves];          // rows of src below its capacity (0: no move)
   uint16_t src[kMaxMoves], dst[kMaxMoves];
+  uint8_t part[kMaxRounds + 1];  // first round; [n_parts]: all
   const uint8_t *from;           // cache bases
   uint8_t *to;
-  int32_t n_moves, most;         // moves, whole rounds; the most rows of any
+  int32_t n_parts, most;         // the most rows of any move
   int32_t row_bytes, pair_bytes; // of a K or V row, and of a row's scale pair (0: none)
 };
 hipError_t launch_move_rows(const MoveArgs &a, hipStream_t s);
@@ -312,8 +315,9 @@ int64_t move_workgroups(int64_t rows, int32_t row_bytes, int32_t pair_bytes);
 struct TableMoveArgs {
   uint16_t src[kMaxMoves], dst[kMaxMoves];
   int32_t pages[kMaxMoves];
+  uint8_t part[kMaxRounds + 1];
   int32_t *table;                // [unit][sequence][max_pages]
-  int32_t n_moves, most, batch, max_pages;
+  int32_t n_parts, most, batch, max_pages;
 };
 hipError_t launch_table_move(const TableMoveArgs &a, int n_units, hipStream_t s);
 
