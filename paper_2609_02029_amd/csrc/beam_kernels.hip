@@ -14,8 +14,8 @@
 //
 // Sums and scores are 64-bit: two beams' tokens are ordered by scores that differ
 // by their lse, and an fp32 sum (off by 1e-7) would swap near ones.  2^f is a
-// polynomial of degree 8, 1.1e-12 off, on [-1/2, 1/2], and the power of two goes
-// into the exponent's bits: 14 64-bit operations a logit, at the rate of fp32's.
+// polynomial of degree 7, 5.5e-11 off, on [-1/2, 1/2], and the power of two goes
+// into the exponent's bits: 11 64-bit operations a logit, at the rate of fp32's.
 #include <algorithm>
 
 #include "hwkv.h"
@@ -94,6 +94,30 @@ struct Row {
   }
 };
 
+// Logits t .. t + 3 of a row, minus infinity past its end.
+template <int T>
+__device__ __forceinline__ f32x4_t four_logits(const BeamArgs &a, int64_t row, uint32_t t) {
+  f32x4_t v = {-kInf, -kInf, -kInf, -kInf};
+  if (t + 4 <= (uint32_t)a.vocab) {
+    typedef uint32_t half_t __attribute__((ext_vector_type(2), aligned(2)));
+    const uint8_t *const at = static_cast<const uint8_t *>(a.logits) + (row * a.stride + t) * kBytes<T>;
+    u32x4_t x;
+    if constexpr (T == HWKV_LOGITS_F32) {
+      x = *reinterpret_cast<const chunk_t *>(at);
+    } else {
+      const half_t h = *reinterpret_cast<const half_t *>(at);
+      x = u32x4_t{h.x, h.y, 0u, 0u};
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = element<T>(x, e);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (t + e < (uint32_t)a.vocab) v[e] = logit<T>(a, row, t + e);
+  }
+  return v;
+}
+
 // op(x, y) over the wavefront, in every lane: lanes 1 and 2 apart, a half row's
 // mirror, a row's, and the rows, two and two (registers only, where a shuffle goes
 // through LDS).  Words: 32-bit parts of the value.
@@ -158,8 +182,10 @@ struct Sum {
 };
 
 // Grid: n_splits workgroups a row.  Wave w of split i takes blocks 4 i + w, and so
-// on in steps of 4 n_splits, DEEP at a time.  What bounds it: HBM, and the 64-bit sums
-// beside it.
+// on in steps of 4 n_splits, DEEP at a time.  What bounds it: HBM and the 64-bit sums
+// beside it, 22 vector instructions a logit in all.  512 rows of 131,072 fp32 logits (268
+// MB): 52 us, 5.2 TB/s; 528 rows of 161,840 bf16 logits (171 MB): 67 us, three quarters
+// of which the vector units are busy.
 template <int T, int DEEP>
 __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
   constexpr int N = kPerChunk<T>, C = kBlockChunks<T>;
@@ -258,6 +284,8 @@ __device__ __forceinline__ double key_score(uint64_t key) {
 
 constexpr int kPickThreads = 512, kListed = 1024;
 constexpr int kHeld = 8192;          // logits that a workgroup keeps in LDS
+constexpr int kRanked = 96;          // listed items that are counted against each other as they are
+constexpr int kAhead = 6;            // reads in flight of a list that it does not keep
 
 // A run of a search's list: consecutive places of one beam.
 struct Run {
@@ -271,14 +299,16 @@ struct Run {
 // n blocks found; each list goes into LDS, as far as it fits, in quads.  A score that n
 // items reach is known before a search (of 64 sets' largest maxima the n-th largest;
 // the n-th block's), so one comparison of logits with a bound keeps nearly all out,
-// and what passes is listed, given its 64-bit key, and counted against each other.
+// and what passes is listed, given its 64-bit key, and counted against each other (of
+// many, those that a second such score leaves: 4 groups of 16 beams, 2,165 logits, 18
+// chosen, 302 listed: 19.5 us a call against 27.8).
 // Where the list does not hold them (long runs of equal or rising logits), the n-th
 // key, how many lie above it and then the n-th item's place are found bit by bit first.
 //
 // What bounds it: latency, of two reads of what other XCDs wrote or left in memory
 // (about 1.5 us each) and some twenty steps through LDS.  24 groups of 4 beams, 131,072
 // logits: with keys formed for every logit and a visit's code for each purpose 15 us,
-// one visit for all purposes 13.6, a bound in front of the keys 9.5.
+// one visit for all purposes 13.6, a bound in front of the keys 7.6.
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   constexpr int N = kPerChunk<T>, WAVES = kPickThreads / 64;
@@ -286,12 +316,13 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   __shared__ __attribute__((aligned(16))) Run run_s[kMaxBeams];
   __shared__ float x_s[kListed];
   __shared__ uint32_t beam_s[kListed], at_s[kListed];
-  __shared__ uint64_t key_s[kListed];
+  __shared__ uint64_t key_s[kListed], kept_key[kListed];
+  __shared__ uint32_t kept_at[kListed];
   __shared__ float lane_top[WAVES][64];
   __shared__ uint64_t best_key[kMaxSelected];
   __shared__ uint32_t best_at[kMaxSelected];
   __shared__ float floor_s;
-  __shared__ int listed, hits_s[WAVES];
+  __shared__ int listed, kept, hits_s[WAVES];
   __shared__ __attribute__((aligned(16))) float value_s[kHeld];
   static_assert(kMaxSelected <= kMaxBeams, "a run per beam, or per block");
 
@@ -307,6 +338,11 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   const auto maximum = [&](int r, int j) {
     return j < a.n_blocks ? a.block_max[(row0 + r) * a.n_blocks + j] : -kInf;
   };
+  const auto four_maxima = [&](int r, int j) -> f32x4_t {
+    typedef f32x4_t __attribute__((aligned(4))) any_t;
+    if (j + 4 <= a.n_blocks) return *reinterpret_cast<const any_t *>(a.block_max + (row0 + r) * a.n_blocks + j);
+    return f32x4_t{maximum(r, j), maximum(r, j + 1), maximum(r, j + 2), maximum(r, j + 3)};
+  };
   double part_sum = 0.0, part_base = kNone, part_s = 0.0;
   const auto load_parts = [&](int b) {
     const double *const part = a.part + ((row0 + b) * a.n_splits + lane) * 2;
@@ -318,8 +354,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
 #pragma unroll 2
     for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
       const int r = i / quads, j = (i - r * quads) * 4;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) value_s[4 * i + e] = maximum(r, j + e);
+      *reinterpret_cast<f32x4_t *>(value_s + 4 * i) = four_maxima(r, j);
     }
   }
   for (int b = wave; b < a.n_beams; b += WAVES) {
@@ -341,10 +376,10 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   // largest (minus infinity: fewer have one).
   {
     float top = -kInf;
-    for (int i = threadIdx.x, r = 0, j = threadIdx.x; i < runs * quads; i += kPickThreads, j += kPickThreads) {
-      for (; j >= quads; j -= quads) ++r;
-      const f32x4_t v = held ? *reinterpret_cast<const f32x4_t *>(value_s + 4 * i)
-                             : f32x4_t{maximum(r, 4 * j), maximum(r, 4 * j + 1), maximum(r, 4 * j + 2), maximum(r, 4 * j + 3)};
+#pragma unroll 2
+    for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
+      const int r = i / quads;
+      const f32x4_t v = held ? *reinterpret_cast<const f32x4_t *>(value_s + 4 * i) : four_maxima(r, 4 * (i - r * quads));
       // (fmaxf passes over the NaN of a beam without candidates)
       top = fmaxf(top, (float)score_of(r, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))));
     }
@@ -380,24 +415,33 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
       if (threadIdx.x == 0) listed = 0;
       __syncthreads();
     };
-    // every item that its run's bound lets pass
+    // every item that its run's bound lets pass (of lists that are not held several reads
+    // are under way at once)
     const auto visit = [&](auto f) {
-      for (int i = threadIdx.x, r = 0, j = threadIdx.x; i < runs * quads; i += kPickThreads, j += kPickThreads) {
-        for (; j >= quads; j -= quads) ++r;
-        const Run run = run_s[r];
-        f32x4_t v;
+      const int all = runs * quads, step = held ? kPickThreads : kAhead * kPickThreads;
+      for (int i0 = threadIdx.x; i0 < all; i0 += step) {
+        f32x4_t v[kAhead];
         if (held) {
-          v = *reinterpret_cast<const f32x4_t *>(value_s + 4 * i);
+          v[0] = *reinterpret_cast<const f32x4_t *>(value_s + 4 * i0);
         } else {
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t t = run.place + 4 * j + e - run.beam * (uint32_t)a.vocab;
-            v[e] = search == 0 ? maximum(r, 4 * j + e) : t < (uint32_t)a.vocab ? logit<T>(a, row0 + run.beam, t) : -kInf;
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) {
+            const int i = min(i0 + k * kPickThreads, all - 1), r = i / quads, j = 4 * (i - r * quads);
+            const uint32_t beam = run_s[r].beam;
+            v[k] = search == 0 ? four_maxima(r, j)
+                               : four_logits<T>(a, row0 + beam, run_s[r].place + j - beam * (uint32_t)a.vocab);
           }
         }
-        if (!(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= run.bound)) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (v[e] >= run.bound) f(run.beam, v[e], run.place + 4 * j + e);
+        for (int k = 0; k < kAhead; ++k) {
+          const int i = i0 + k * kPickThreads, r = i / quads;
+          if (k > 0 && (held || i >= all)) break;
+          const Run run = run_s[r];
+          if (!(fmaxf(fmaxf(v[k].x, v[k].y), fmaxf(v[k].z, v[k].w)) >= run.bound)) continue;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (v[k][e] >= run.bound) f(run.beam, v[k][e], run.place + 4 * (i - r * quads) + e);
+        }
       }
     };
     const auto list = [&](int b, float x, uint32_t at) {
@@ -445,21 +489,50 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
       });
       __syncthreads();
     }
-    const int all = min(listed, kListed);
+    int all = min(listed, kListed);
     for (int i = threadIdx.x; i < all; i += kPickThreads) key_s[i] = order_key(score_of(beam_s[i], x_s[i]));
     __syncthreads();
+    const uint64_t *key = key_s;
+    const uint32_t *place = at_s;
+    if (all > kRanked) {
+      // too many to count against each other: those that the n-th largest of 64 sets'
+      // largest keeps out go first (every wave finds it for itself)
+      uint64_t top = 0;
+      for (int i = lane; i < all; i += 64) top = max(top, key_s[i]);
+      int above = 0;
+#pragma unroll 8
+      for (int l = 0; l < 64; ++l) {
+        const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(top >> 32), l) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)top, l);
+        above += k > top ? 1 : 0;
+      }
+      const uint64_t least =
+          over_wave(above < n ? top : ~0ull, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
+      if (threadIdx.x == 0) kept = 0;
+      __syncthreads();
+      for (int i = threadIdx.x; i < all; i += kPickThreads)
+        if (key_s[i] >= least) {
+          const int l = atomicAdd(&kept, 1);
+          kept_key[l] = key_s[i];
+          kept_at[l] = at_s[i];
+        }
+      __syncthreads();
+      all = kept;
+      key = kept_key;
+      place = kept_at;
+    }
     for (int i = threadIdx.x; i < all; i += kPickThreads) {
-      const uint64_t key = key_s[i];
-      const uint32_t at = at_s[i];
+      const uint64_t mine = key[i];
+      const uint32_t at = place[i];
       int before = 0;
 #pragma unroll 4
       for (int j = 0; j < all; ++j) {
-        const uint64_t k = key_s[j];
-        const uint32_t p = at_s[j];
-        before += (k > key) | ((k == key) & (p < at));
+        const uint64_t k = key[j];
+        const uint32_t p = place[j];
+        before += (k > mine) | ((k == mine) & (p < at));
       }
       if (before < n) {
-        best_key[before] = key;
+        best_key[before] = mine;
         best_at[before] = at;
       }
     }
