@@ -228,7 +228,7 @@ int hwkv_cache_pages(const hwkv_cache *cache, int64_t *total,
                      int64_t *free_pages);
 
 /* Release sequence `seq`: its length becomes 0 in every layer and the pages
- * of its full units return to the pool (host bookkeeping only: no device
+ * of its full units that no other sequence holds return to the pool (host bookkeeping only: no device
  * work, ordered with the cache's other calls as they are issued).  Valid on
  * any cache; a released sequence is filled again from position 0. */
 int hwkv_cache_reset_seq(hwkv_cache *cache, int32_t seq);
@@ -263,7 +263,7 @@ int hwkv_cache_reorder(hwkv_cache *cache, const int32_t *parents, void *stream);
  * is freed, for which the call waits for `stream` (not under stream capture).  A
  * kernel of an earlier call must be done, or on `stream`.  ENOMEM if the sequences
  * hold more than n_pages pages, or the buffer is too small; EINVAL if it is not
- * 16-byte aligned or overlaps the present one. */
+ * 16-byte aligned or overlaps the present one, and on more than 65534 sequences. */
 int hwkv_cache_move(hwkv_cache *cache, int64_t n_pages, void *dev_buf,
                     size_t buf_bytes, void *stream);
 

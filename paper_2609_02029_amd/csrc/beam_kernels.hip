@@ -184,10 +184,11 @@ struct Sum {
 // Grid: n_splits workgroups a row.  Wave w of split i takes blocks 4 i + w, and so
 // on in steps of 4 n_splits, DEEP at a time.  What bounds it: HBM and the 64-bit sums
 // beside it, 22 vector instructions a logit in all.  512 rows of 131,072 fp32 logits (268
-// MB): 52 us, 5.2 TB/s; 528 rows of 161,840 bf16 logits (171 MB): 67 us, three quarters
-// of which the vector units are busy.
+// MB): 52 us, 5.2 TB/s; 528 rows of 161,840 bf16 logits (171 MB): 68 us, three quarters
+// of which the vector units are busy.  (Registers for eight workgroups a CU: spills.)
 template <int T, int DEEP>
-__global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
+__global__ __launch_bounds__(kScanWaves * 64) __attribute__((amdgpu_waves_per_eu(7)))
+void beam_scan(BeamArgs a) {
   constexpr int N = kPerChunk<T>, C = kBlockChunks<T>;
   const int64_t row = blockIdx.x / a.n_splits;
   const int split = blockIdx.x % a.n_splits;

@@ -2694,7 +2694,7 @@ int launch_moves(const hwkv_cache *c, const MovePlan &plan, size_t first, const 
       if (c->k_off[u] < 0) continue;             // a paged unit
       const int64_t wgs =
           hwkv::move_workgroups(std::min(most, c->cap[u]), a.row_bytes, a.pair_bytes);
-      if (begin + wgs > INT32_MAX / 256) break;
+      if (k > 0 && begin + wgs > INT32_MAX / 256) break;
       a.unit[k].k_off = c->k_off[u] * c->elem;
       a.unit[k].v_off = c->v_off[u] * c->elem;
       a.unit[k].s_off = c->s_off[u];
@@ -3144,6 +3144,7 @@ int hwkv_cache_reorder(hwkv_cache *c, const int32_t *parents, void *stream) {
 
 int hwkv_cache_move(hwkv_cache *c, int64_t n_pages, void *dev_buf, size_t buf_bytes, void *stream) {
   if (!c) return fail(HWKV_EINVAL, "cache is null");
+  if (c->batch >= (int32_t)hwkv::kMoveCarry) return fail(HWKV_EINVAL, "more than 65534 sequences");
   if (!c->paged && n_pages != 0) return fail(HWKV_EINVAL, "n_pages must be 0 for a cache that is not paged");
   try {
     const int rc = move_impl(c, n_pages, dev_buf, buf_bytes, (hipStream_t)stream);

@@ -42,13 +42,13 @@ def values(cache, layer, h, b):
     return out
 
 
-def check(cache, layer, q, scale, out, seqs=None):
+def check(cache, layer, q, scale, out, seqs=None, heads=None):
     torch.cuda.synchronize()
     G = cache.n_q_heads // cache.n_kv_heads
     q, out = q.double().cpu().numpy(), out.double().cpu().numpy()
     worst = 0.0
     for b in range(cache.batch) if seqs is None else seqs:
-        for h in range(cache.n_kv_heads):
+        for h in range(cache.n_kv_heads) if heads is None else heads:
             k, v = values(cache, layer, h, b)
             for g in range(h * G, h * G + G):
                 z = (k @ q[b, g]) * scale
@@ -140,6 +140,21 @@ def test_long_shared_prompts():
     assert r.check(seqs=(0, 7)) < 5e-6
     r = Forked(128, 4, ((20000, 4), (9000, 4)), [100 * i for i in range(8)], fmt="f16")
     r.check(seqs=(0, 3, 4, 7))
+
+
+@pytest.mark.parametrize("count,G", [(2, 4), (6, 8)])
+def test_many_tiles_a_workgroup(count, G):
+    """More than the 64 tiles whose pages a workgroup looks up at once, in workgroups of
+    one column group and of three."""
+    r = Forked(64, G, ((70000, count),), [9 * i for i in range(count)], levels=(1,) * 32, max_ctx=70200)
+    r.check(seqs=(0, count - 1), heads=(0, 13, 31))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+def test_blocks_of_unequal_widths(fmt):
+    """Blocks of one to five column groups in one launch, beside sequences of none."""
+    Forked(64, 8, ((600, 10), (300, 2), (512, 5), (260, 3), (90, 2), (1024, 1)), [3 * i for i in range(23)], fmt=fmt).check()
+    Forked(128, 1, ((600, 50), (300, 17), (256, 2)), [i % 4 for i in range(69)], fmt=fmt).check()
 
 
 def test_families_within_a_prompt():

@@ -104,3 +104,49 @@ def test_move_refuses(hw, cache):
     assert f(h, 1, there, need, None) == hw.EINVAL
     assert f(h, 0, there, need, None) == hw.OK
     hw._lib.hwkv_cache_free(h)
+
+
+def test_batches_that_moves_cannot_name(hw):
+    """Sequences are named in 16 bits, and one name is taken."""
+    pol = hw.policy_set(1, 1, 1, 64, 0, [16], [[0]])
+    for batch, ok in ((65534, True), (65535, False)):
+        h = ctypes.c_void_p()
+        assert hw._lib.hwkv_cache_alloc_format(ctypes.byref(h), pol.handle, batch, 64, 0, None, None, FAKE, 1 << 42) == hw.OK
+        need = hw.cache_bytes(pol, batch, 64, "bf16")
+        parents = (ctypes.c_int32 * batch)(*range(1, batch), -1)
+        assert hw._lib.hwkv_cache_reorder(h, (ctypes.c_int32 * batch)(*range(batch)), None) == (hw.OK if ok else hw.EINVAL)
+        if not ok:
+            assert hw._lib.hwkv_cache_reorder(h, parents, None) == hw.EINVAL and "65534" in hw.last_error()
+        assert hw._lib.hwkv_cache_move(h, 0, FAKE + (1 << 43), need, None) == (hw.OK if ok else hw.EINVAL)
+        hw._lib.hwkv_cache_free(h)
+
+
+def test_shared_decode_refuses(hw, cache):
+    f = hw._lib.hwkv_decode_attn_shared
+    scale = ctypes.c_float(0.125)
+    q, out, ws = FAKE + (1 << 42), FAKE + (2 << 42), FAKE + (3 << 42)
+    assert f(None, 0, q, scale, out, ws, 1 << 30, None) == hw.EINVAL
+    for layer in (-1, 2):
+        assert f(cache.handle, layer, q, scale, out, ws, 1 << 30, None) == hw.EINVAL and "layer" in hw.last_error()
+    for a in ((None, out, ws), (q, None, ws)):
+        assert f(cache.handle, 0, a[0], scale, a[1], a[2], 1 << 30, None) == hw.EINVAL and "null" in hw.last_error()
+    for a in ((q + 8, out, ws), (q, out + 8, ws), (q, out, ws + 8)):
+        assert f(cache.handle, 0, a[0], scale, a[1], a[2], 1 << 30, None) == hw.EINVAL and "aligned" in hw.last_error()
+    for bad in (float("inf"), float("nan")):
+        assert f(cache.handle, 0, q, ctypes.c_float(bad), out, ws, 1 << 30, None) == hw.EINVAL and "finite" in hw.last_error()
+    assert f(cache.handle, 0, q, scale, out, ws, 1 << 30, None) == hw.EINVAL and "empty" in hw.last_error()
+
+
+def test_shared_decode_workspace(hw, cache):
+    f = hw._lib.hwkv_decode_shared_workspace_bytes
+    n = ctypes.c_size_t()
+    assert f(None, ctypes.byref(n)) == hw.EINVAL and f(cache.handle, None) == hw.EINVAL
+    assert f(cache.handle, ctypes.byref(n)) == hw.OK
+    assert n.value > 0 and n.value % 4 == 0
+    # a cache that shares nothing has no parts of blocks
+    pol = hw.policy_set(2, 2, 4, 64, 4, [128, 0], [[0, 1], [1, 1]])
+    h = ctypes.c_void_p()
+    assert hw._lib.hwkv_cache_alloc_format(ctypes.byref(h), pol.handle, 3, 1000, 0, None, None, FAKE, 1 << 40) == hw.OK
+    m = ctypes.c_size_t()
+    assert f(h, ctypes.byref(m)) == hw.OK and 0 < m.value < n.value
+    hw._lib.hwkv_cache_free(h)
