@@ -2643,7 +2643,7 @@ int64_t most_rows(const hwkv_cache *c, int32_t b) {
   return n;
 }
 
-// Launches the moves over every unit that has a region.
+// Sequences' rows to be copied.
 struct Move {
   int32_t src, dst;
   int64_t rows;
@@ -2667,49 +2667,71 @@ struct MovePlan {
   }
 };
 
-int launch_moves(const hwkv_cache *c, const MovePlan &plan, size_t first, const uint8_t *from, uint8_t *to,
-                 hipStream_t s) {
-  const Move *const moves = &plan.moves[first];
-  const size_t n = plan.launch_end(first) - first;
-  hwkv::MoveArgs a;
-  std::memset(&a, 0, sizeof a);
-  a.from = from;
-  a.to = to;
-  a.row_bytes = row_bytes(c);
-  a.pair_bytes = (int32_t)row_scale_bytes(c->fmt);
-  a.n_parts = plan.rounds(first, a.part);
+// The moves of a launch, without units.
+template <int N>
+void fill_moves(const hwkv_cache *c, const MovePlan &plan, size_t first, const uint8_t *from, uint8_t *to,
+                hwkv::MoveArgsOf<N> *a) {
+  std::memset(a, 0, sizeof *a);
+  a->from = from;
+  a->to = to;
+  a->row_bytes = row_bytes(c);
+  a->pair_bytes = (int32_t)row_scale_bytes(c->fmt);
+  a->n_parts = plan.rounds(first, a->part);
   int64_t most = 0;
-  for (size_t i = 0; i < n; ++i) {
-    a.src[i] = (uint16_t)moves[i].src;
-    a.dst[i] = (uint16_t)moves[i].dst;
-    a.n[i] = (int32_t)moves[i].rows;
-    most = std::max(most, moves[i].rows);
+  for (size_t i = first; i < plan.launch_end(first); ++i) {
+    a->src[i - first] = (uint16_t)plan.moves[i].src;
+    a->dst[i - first] = (uint16_t)plan.moves[i].dst;
+    a->n[i - first] = (int32_t)plan.moves[i].rows;
+    most = std::max(most, plan.moves[i].rows);
   }
-  a.most = (int32_t)most;
-  const int32_t U = (int32_t)c->cap.size();
-  for (int32_t u = 0; u < U;) {
-    int32_t k = 0;
-    int64_t begin = 0;
-    for (; u < U && k < hwkv::kMaxItems; ++u) {
-      if (c->k_off[u] < 0) continue;             // a paged unit
-      const int64_t wgs =
-          hwkv::move_workgroups(std::min(most, c->cap[u]), a.row_bytes, a.pair_bytes);
-      if (k > 0 && begin + wgs > INT32_MAX / 256) break;
-      a.unit[k].k_off = c->k_off[u] * c->elem;
-      a.unit[k].v_off = c->v_off[u] * c->elem;
-      a.unit[k].s_off = c->s_off[u];
-      a.unit[k].cap = (int32_t)c->cap[u];
-      a.unit[k].cap_pad = (int32_t)c->cap_pad[u];
-      a.wg_begin[k++] = (int32_t)begin;
-      begin += wgs;
+  a->most = (int32_t)most;
+}
+
+// The units with a region from u on, as many as a launch takes; the first one it leaves.
+template <int N>
+int32_t fill_units(const hwkv_cache *c, int32_t u, hwkv::MoveArgsOf<N> *a) {
+  int32_t k = 0;
+  int64_t begin = 0;
+  for (; u < (int32_t)c->cap.size() && k < hwkv::kMaxItems; ++u) {
+    if (c->k_off[u] < 0) continue;               // a paged unit
+    const int64_t wgs =
+        hwkv::move_workgroups(std::min<int64_t>(a->most, c->cap[u]), a->row_bytes, a->pair_bytes);
+    if (k > 0 && begin + wgs > INT32_MAX / 256) break;
+    a->unit[k].k_off = c->k_off[u] * c->elem;
+    a->unit[k].v_off = c->v_off[u] * c->elem;
+    a->unit[k].s_off = c->s_off[u];
+    a->unit[k].cap = (int32_t)c->cap[u];
+    a->unit[k].cap_pad = (int32_t)c->cap_pad[u];
+    a->wg_begin[k++] = (int32_t)begin;
+    begin += wgs;
+  }
+  a->wg_begin[k] = (int32_t)begin;
+  for (int32_t i = k + 1; i <= hwkv::kMaxItems; ++i) a->wg_begin[i] = INT32_MAX;
+  return u;
+}
+
+// Launches the moves over every unit that has a region.
+int launch_moves(const hwkv_cache *c, const MovePlan &plan, const uint8_t *from, uint8_t *to, hipStream_t s) {
+  for (size_t i = 0; i < plan.moves.size(); i = plan.launch_end(i)) {
+    hwkv::MoveArgs a;
+    fill_moves(c, plan, i, from, to, &a);
+    for (int32_t u = 0; u < (int32_t)c->cap.size();) {
+      u = fill_units(c, u, &a);
+      const int rc = check_device(hwkv::launch_move_rows(a, s), "move launch");
+      if (rc != HWKV_OK) return rc;
     }
-    a.wg_begin[k] = (int32_t)begin;
-    for (int32_t i = k + 1; i <= hwkv::kMaxItems; ++i) a.wg_begin[i] = INT32_MAX;
-    if (k == 0) continue;
-    const int rc = check_device(hwkv::launch_move_rows(a, s), "move launch");
-    if (rc != HWKV_OK) return rc;
   }
   return HWKV_OK;
+}
+
+// Whether rows and pages go into one launch of moderate size; fills the former.
+bool few_moves(const hwkv_cache *c, const MovePlan &plan, const uint8_t *from, uint8_t *to, hwkv::FewMoves *a) {
+  if (plan.moves.empty() || plan.moves.size() > (size_t)hwkv::kFewMoves) return false;
+  fill_moves(c, plan, 0, from, to, a);
+  if (fill_units(c, 0, a) < (int32_t)c->cap.size()) return false;
+  int32_t wgs = 0;
+  for (int32_t i = 0; i <= hwkv::kMaxItems && a->wg_begin[i] != INT32_MAX; ++i) wgs = a->wg_begin[i];
+  return wgs > 0 && wgs <= 1 << 16;
 }
 
 // The moves parent[b] -> b of the sequences that change, in an order in which no source
@@ -2949,6 +2971,25 @@ int reorder_pages(hwkv_cache *c, const int32_t *parent, PagePlan *P) {
   return HWKV_OK;
 }
 
+// Copies and entries from *i and *e on, as many as a launch takes.
+template <int N, int E>
+void fill_page_copies(const hwkv_cache *c, const PagePlan &P, size_t *i, size_t *e, hwkv::PageCopyArgsOf<N, E> *a) {
+  a->pool = c->base + c->pool_off * c->elem;
+  a->table = device_page_table(c);
+  a->row_bytes = row_bytes(c);
+  a->pair_bytes = (int32_t)row_scale_bytes(c->fmt);
+  for (a->n_copies = 0; a->n_copies < N && *i < P.copies.size(); ++*i, ++a->n_copies) {
+    a->src[a->n_copies] = P.copies[*i].src;
+    a->dst[a->n_copies] = P.copies[*i].dst;
+    a->at[a->n_copies] = P.copies[*i].pto + P.copies[*i].j;
+    a->rows[a->n_copies] = (uint8_t)P.copies[*i].rows;
+  }
+  for (a->n_entries = 0; a->n_entries < E && *e < P.entries.size(); ++*e, ++a->n_entries) {
+    a->idx[a->n_entries] = P.entries[*e].first;
+    a->page[a->n_entries] = P.entries[*e].second;
+  }
+}
+
 // Copies the pages of a reorder and brings the device's table in line: by its changed
 // entries, or, where these are many, row by row as the sequences move (a fork of 30,000
 // tokens, 128 full units, eight ways: 105,000 entries, 435 us against 1,784 as lists;
@@ -2979,21 +3020,8 @@ int launch_page_copies(const hwkv_cache *c, const PagePlan &P, const MovePlan &p
     }
   }
   hwkv::PageCopyArgs a;
-  a.pool = c->base + c->pool_off * c->elem;
-  a.table = device_page_table(c);
-  a.row_bytes = row_bytes(c);
-  a.pair_bytes = (int32_t)row_scale_bytes(c->fmt);
   while (i < P.copies.size() || e < P.entries.size()) {
-    for (a.n_copies = 0; a.n_copies < hwkv::kMaxPageCopies && i < P.copies.size(); ++i, ++a.n_copies) {
-      a.src[a.n_copies] = P.copies[i].src;
-      a.dst[a.n_copies] = P.copies[i].dst;
-      a.at[a.n_copies] = P.copies[i].pto + P.copies[i].j;
-      a.rows[a.n_copies] = (uint8_t)P.copies[i].rows;
-    }
-    for (a.n_entries = 0; a.n_entries < hwkv::kMaxEntries && e < P.entries.size(); ++e, ++a.n_entries) {
-      a.idx[a.n_entries] = P.entries[e].first;
-      a.page[a.n_entries] = P.entries[e].second;
-    }
+    fill_page_copies(c, P, &i, &e, &a);
     const int rc = check_device(hwkv::launch_page_copy(a, s), "page copy launch");
     if (rc != HWKV_OK) return rc;
   }
@@ -3011,10 +3039,19 @@ int reorder_impl(hwkv_cache *c, const int32_t *parent, hipStream_t s) {
   for (int32_t l = 0; l < c->pol.n_layers; ++l)
     for (int32_t b = 0; b < c->batch; ++b)
       c->n[(size_t)l * c->batch + b] = parent[b] < 0 ? 0 : n[(size_t)l * c->batch + parent[b]];
-  rc = launch_page_copies(c, P, plan, s);
-  for (size_t i = 0; rc == HWKV_OK && i < plan.moves.size(); i += hwkv::kMaxMoves)
-    rc = launch_moves(c, plan, i, c->base, c->base, s);
-  return rc;
+  if (!P.copies.empty() || !P.entries.empty()) {
+    hwkv::FewMoves m;
+    if (P.copies.size() <= hwkv::kFewPages && P.entries.size() <= hwkv::kFewPages &&
+        few_moves(c, plan, c->base, c->base, &m)) {
+      hwkv::FewPageCopies a;
+      size_t i = 0, e = 0;
+      fill_page_copies(c, P, &i, &e, &a);
+      return check_device(hwkv::launch_few(m, a, s), "move launch");
+    }
+    rc = launch_page_copies(c, P, plan, s);
+    if (rc != HWKV_OK) return rc;
+  }
+  return launch_moves(c, plan, c->base, c->base, s);
 }
 
 // The cache in another buffer, with a pool of n_pages pages.
@@ -3074,27 +3111,37 @@ int move_impl(hwkv_cache *c, int64_t n_pages, void *dev_buf, size_t buf_bytes, h
     }
   }
   uint8_t *const base = static_cast<uint8_t *>(dev_buf);
-  hwkv::PageMoveArgs a;
-  std::memset(&a, 0, sizeof a);
-  a.from_pool = c->base + c->pool_off * c->elem;
-  a.to_pool = base + to.pool_off * c->elem;
-  a.from_table = device_page_table(c);
-  a.to_table = reinterpret_cast<int32_t *>(base + to.table_off);
-  a.row_bytes = row_bytes(c);
-  a.pair_bytes = (int32_t)row_scale_bytes(c->fmt);
-  for (size_t i = 0; rc == HWKV_OK && i < runs.size();) {
+  const auto fill_pages = [&](auto *a, size_t *i) {
+    constexpr int N = (int)(sizeof a->run / sizeof a->run[0]);
+    a->from_pool = c->base + c->pool_off * c->elem;
+    a->to_pool = base + to.pool_off * c->elem;
+    a->from_table = device_page_table(c);
+    a->to_table = reinterpret_cast<int32_t *>(base + to.table_off);
+    a->row_bytes = row_bytes(c);
+    a->pair_bytes = (int32_t)row_scale_bytes(c->fmt);
     int k = 0;
-    for (a.n_pages = 0; k < hwkv::kMaxRuns && i < runs.size() && a.n_pages < (1 << 19); ++i, ++k) {
-      const int32_t len = runs[i].begin;
-      a.run[k] = runs[i];
-      a.run[k].begin = a.n_pages;
-      a.n_pages += len;
+    for (a->n_pages = 0; k < N && *i < runs.size() && a->n_pages < (1 << 19); ++*i, ++k) {
+      const int32_t len = runs[*i].begin;
+      a->run[k] = runs[*i];
+      a->run[k].begin = a->n_pages;
+      a->n_pages += len;
     }
-    for (; k < hwkv::kMaxRuns; ++k) a.run[k].begin = INT32_MAX;
-    rc = check_device(hwkv::launch_page_move(a, s), "page move launch");
+    for (; k < N; ++k) a->run[k].begin = INT32_MAX;
+  };
+  hwkv::FewMoves m;
+  if (!runs.empty() && runs.size() <= hwkv::kFewPages && used < 1024 && few_moves(c, plan, c->base, base, &m)) {
+    hwkv::FewPageMoves a;
+    size_t i = 0;
+    fill_pages(&a, &i);
+    rc = check_device(hwkv::launch_few(m, a, s), "move launch");
+  } else {
+    hwkv::PageMoveArgs a;
+    for (size_t i = 0; rc == HWKV_OK && i < runs.size();) {
+      fill_pages(&a, &i);
+      rc = check_device(hwkv::launch_page_move(a, s), "page move launch");
+    }
+    if (rc == HWKV_OK) rc = launch_moves(c, plan, c->base, base, s);
   }
-  for (size_t i = 0; rc == HWKV_OK && i < plan.moves.size(); i += hwkv::kMaxMoves)
-    rc = launch_moves(c, plan, i, c->base, base, s);
   if (rc == HWKV_OK && c->owned) {
     rc = check_device(hipStreamSynchronize(s), "hipStreamSynchronize");
     if (rc == HWKV_OK) rc = check_device(hipFree(c->base), "hipFree");

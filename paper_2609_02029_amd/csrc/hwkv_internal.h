@@ -295,17 +295,19 @@ struct MoveUnit {
   int64_t k_off, v_off, s_off;   // byte offsets of sequence 0
   int32_t cap, cap_pad;          // rows holding data; rows allocated
 };
-struct MoveArgs {
+template <int N>
+struct MoveArgsOf {
   MoveUnit unit[kMaxItems];
   int32_t wg_begin[kMaxItems + 1];   // INT32_MAX past the last
-  int32_t n[kMaxMoves];          // rows of src below its capacity (0: no move)
-  uint16_t src[kMaxMoves], dst[kMaxMoves];
-  uint8_t part[kMaxRounds + 1];  // first round; [n_parts]: all
+  int32_t n[N];                  // rows of src below its capacity (0: no move)
+  uint16_t src[N], dst[N];
+  uint8_t part[N / kMoveRound + 1];  // first round; [n_parts]: all
   const uint8_t *from;           // cache bases
   uint8_t *to;
   int32_t n_parts, most;         // the most rows of any move
   int32_t row_bytes, pair_bytes; // of a K or V row, and of a row's scale pair (0: none)
 };
+using MoveArgs = MoveArgsOf<kMaxMoves>;
 hipError_t launch_move_rows(const MoveArgs &a, hipStream_t s);
 // Workgroups of a unit for `rows` rows.
 int64_t move_workgroups(int64_t rows, int32_t row_bytes, int32_t pair_bytes);
@@ -323,15 +325,17 @@ hipError_t launch_table_move(const TableMoveArgs &a, int n_units, hipStream_t s)
 
 // Pages copied within a pool, each with its table entry, and entries alone.
 constexpr int kMaxPageCopies = 192, kMaxEntries = 180;
-struct PageCopyArgs {
-  int32_t src[kMaxPageCopies], dst[kMaxPageCopies], at[kMaxPageCopies];
-  int32_t idx[kMaxEntries], page[kMaxEntries];
-  uint8_t rows[kMaxPageCopies];  // that src holds (< 256)
+template <int N, int E>
+struct PageCopyArgsOf {
+  int32_t src[N], dst[N], at[N];
+  int32_t idx[E], page[E];
+  uint8_t rows[N];               // that src holds (< 256)
   int32_t n_copies, n_entries;
   uint8_t *pool;
   int32_t *table;
   int32_t row_bytes, pair_bytes;
 };
+using PageCopyArgs = PageCopyArgsOf<kMaxPageCopies, kMaxEntries>;
 hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t s);
 
 // Pages that go from one pool into another: runs of consecutive pages of a
@@ -344,15 +348,25 @@ struct PageRun {
   int32_t begin;                 // pages of the launch's runs before it
   int32_t copy;
 };
-struct PageMoveArgs {
-  PageRun run[kMaxRuns];         // begin INT32_MAX past the last
+template <int N>
+struct PageMoveArgsOf {
+  PageRun run[N];                // begin INT32_MAX past the last
   const uint8_t *from_pool;
   uint8_t *to_pool;
   const int32_t *from_table;
   int32_t *to_table;
   int32_t n_pages, row_bytes, pair_bytes;
 };
+using PageMoveArgs = PageMoveArgsOf<kMaxRuns>;
 hipError_t launch_page_move(const PageMoveArgs &a, hipStream_t s);
+
+// Rows and pages in one launch, where there are few of both.
+constexpr int kFewMoves = 32, kFewPages = 32;
+using FewMoves = MoveArgsOf<kFewMoves>;
+using FewPageCopies = PageCopyArgsOf<kFewPages, kFewPages>;
+using FewPageMoves = PageMoveArgsOf<kFewPages>;
+hipError_t launch_few(const FewMoves &m, const FewPageCopies &p, hipStream_t s);
+hipError_t launch_few(const FewMoves &m, const FewPageMoves &p, hipStream_t s);
 
 // Beam search's selection (beam_kernels.hip).
 constexpr int kMaxBeams = 64, kMaxSelected = 64;
@@ -597,6 +611,9 @@ static_assert(sizeof(hwkv::AppendRopeArgs) <= 4096, "append rope kernarg too lar
 static_assert(sizeof(hwkv::PageUpdateArgs) <= 4096, "page update kernarg too large");
 static_assert(sizeof(hwkv::SharedArgs) <= 4096, "shared decode kernarg too large");
 static_assert(sizeof(hwkv::MoveArgs) <= 4096, "move kernarg too large");
+static_assert(sizeof(hwkv::FewMoves) + sizeof(hwkv::FewPageCopies) <= 4096 &&
+                  sizeof(hwkv::FewMoves) + sizeof(hwkv::FewPageMoves) <= 4096,
+              "kernarg of few moves too large");
 static_assert(sizeof(hwkv::TableMoveArgs) <= 4096, "table move kernarg too large");
 static_assert(sizeof(hwkv::PageCopyArgs) <= 4096, "page copy kernarg too large");
 static_assert(sizeof(hwkv::PageMoveArgs) <= 4096, "page move kernarg too large");

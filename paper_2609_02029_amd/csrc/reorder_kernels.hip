@@ -33,12 +33,13 @@ __host__ __device__ constexpr int64_t part_chunks(int part, int64_t rows, int ro
 // sequences of 5 rows, 7 rounds: 26.6 us in one part, 7.1 in seven).  384 sequences of
 // 1,500 to 6,000 tokens, windows of 1,024: 980 MB in 201 us, 4.9 TB/s, the rate of a
 // copy.
-__global__ __launch_bounds__(256) void move_rows(MoveArgs a) {
+template <bool ONE, int M>
+__device__ __forceinline__ void move_rows_of(const MoveArgsOf<M> &a, int block, int part_of_moves) {
   const int lane = threadIdx.x & 63;
-  const int u = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.wg_begin[lane] <= (int)blockIdx.x)) - 1);
+  const int u = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.wg_begin[lane] <= block)) - 1);
   const MoveUnit &unit = a.unit[u];
   // the part (K, V, pairs) of this workgroup, by the most rows any move has
-  int64_t wg = (int)blockIdx.x - a.wg_begin[u];
+  int64_t wg = block - a.wg_begin[u];
   int part = 0;
   for (; part < 2; ++part) {
     const int64_t wgs =
@@ -48,39 +49,49 @@ __global__ __launch_bounds__(256) void move_rows(MoveArgs a) {
   }
   const int64_t at = part == 0 ? unit.k_off : part == 1 ? unit.v_off : unit.s_off;
   const int64_t stride = (int64_t)unit.cap_pad * (part == 2 ? a.pair_bytes : a.row_bytes);
-  const int64_t c0 = wg * kWgChunks + threadIdx.x;
+  const int64_t first = wg * kWgChunks;
   chunk_t carry[kMoveChunks] = {};
-  for (int r = a.part[blockIdx.y] * kMoveRound; r < a.part[blockIdx.y + 1] * kMoveRound; r += kMoveRound) {
+  // (ONE: every part is one round, which needs no carry: 68 registers, not 87, and 203
+  // MB in 44 us, not 50)
+  const int r0 = a.part[part_of_moves] * kMoveRound;
+  const int r1 = ONE ? r0 + kMoveRound : a.part[part_of_moves + 1] * kMoveRound;
+  for (int r = r0; r < r1; r += kMoveRound) {
     chunk_t x[kMoveRound][kMoveChunks];
     bool has[kMoveRound][kMoveChunks];
 #pragma unroll
     for (int i = 0; i < kMoveRound; ++i) {
       const int src = a.src[r + i];
-      const int64_t n = part_chunks(part, min(a.n[r + i], unit.cap), a.row_bytes, a.pair_bytes);
-      const chunk_t *const from = reinterpret_cast<const chunk_t *>(a.from + at + src * stride);
+      // (uniform: the chunks that are left, and where they begin)
+      const int n = (int)min(part_chunks(part, min(a.n[r + i], unit.cap), a.row_bytes, a.pair_bytes) - first, kWgChunks);
+      const chunk_t *const from = reinterpret_cast<const chunk_t *>(a.from + at + src * stride) + first;
 #pragma unroll
       for (int j = 0; j < kMoveChunks; ++j) {
-        has[i][j] = c0 + j * 256 < n;
-        if (src == kMoveCarry)
+        has[i][j] = (int)threadIdx.x + j * 256 < n;
+        if (!ONE && src == kMoveCarry)
           x[i][j] = carry[j];
         else if (has[i][j])
-          x[i][j] = from[c0 + j * 256];
+          x[i][j] = from[threadIdx.x + j * 256];
       }
     }
 #pragma unroll
     for (int i = 0; i < kMoveRound; ++i) {
       const int dst = a.dst[r + i];
-      chunk_t *const to = reinterpret_cast<chunk_t *>(a.to + at + dst * stride);
+      chunk_t *const to = reinterpret_cast<chunk_t *>(a.to + at + dst * stride) + first;
 #pragma unroll
       for (int j = 0; j < kMoveChunks; ++j) {
         if (!has[i][j]) continue;
-        if (dst == kMoveCarry)
+        if (!ONE && dst == kMoveCarry)
           carry[j] = x[i][j];
         else
-          to[c0 + j * 256] = x[i][j];
+          to[threadIdx.x + j * 256] = x[i][j];
       }
     }
   }
+}
+
+template <bool ONE>
+__global__ __launch_bounds__(256) void move_rows(MoveArgs a) {
+  move_rows_of<ONE>(a, blockIdx.x, blockIdx.y);
 }
 
 // Part `part` of kPageParts of a page's first `rows` rows.
@@ -112,18 +123,20 @@ __host__ __device__ constexpr int64_t page_bytes(int row_bytes, int pair_bytes) 
   return (int64_t)kPageTokens * (2 * row_bytes + pair_bytes);
 }
 
-// Grid: kPageParts workgroups a copy, and one that installs the entries.
-__global__ __launch_bounds__(256) void page_copy(PageCopyArgs a) {
-  const int i = blockIdx.x / kPageParts;
+// kPageParts workgroups a copy, and one that installs the entries.
+template <int N, int E>
+__device__ __forceinline__ void pages_of(const PageCopyArgsOf<N, E> &a, int block) {
+  const int i = block / kPageParts;
   if (i == a.n_copies) {
     for (int e = threadIdx.x; e < a.n_entries; e += 256) a.table[a.idx[e]] = a.page[e];
     for (int e = threadIdx.x; e < a.n_copies; e += 256) a.table[a.at[e]] = a.dst[e];
     return;
   }
   const int64_t page = page_bytes(a.row_bytes, a.pair_bytes);
-  copy_page(a.pool + a.src[i] * page, a.pool + a.dst[i] * page, blockIdx.x % kPageParts, a.rows[i], a.row_bytes,
+  copy_page(a.pool + a.src[i] * page, a.pool + a.dst[i] * page, block % kPageParts, a.rows[i], a.row_bytes,
             a.pair_bytes);
 }
+__global__ __launch_bounds__(256) void page_copy(PageCopyArgs a) { pages_of(a, blockIdx.x); }
 
 // As move_rows, for the page table: a thread holds entry j of every row of a unit.  Grid:
 // (entries / 256, units, parts).
@@ -150,11 +163,12 @@ __global__ __launch_bounds__(256) void table_move(TableMoveArgs a) {
   }
 }
 
-// Grid: kPageParts workgroups a page.
-__global__ __launch_bounds__(256) void page_move(PageMoveArgs a) {
-  const int lane = threadIdx.x & 63, p = blockIdx.x / kPageParts, part = blockIdx.x % kPageParts;
+// kPageParts workgroups a page.
+template <int N>
+__device__ __forceinline__ void pages_of(const PageMoveArgsOf<N> &a, int block) {
+  const int lane = threadIdx.x & 63, p = block / kPageParts, part = block % kPageParts;
   int run = -1;
-  for (int i = 0; i < kMaxRuns; i += 64) run += __popcll(__ballot(a.run[i + lane].begin <= p));
+  for (int i = 0; i < N; i += 64) run += __popcll(__ballot(i + lane < N && a.run[min(i + lane, N - 1)].begin <= p));
   const PageRun r = a.run[__builtin_amdgcn_readfirstlane(run)];
   const int j = p - r.begin, dst = r.dst0 + j;
   const int src = a.from_table[r.pto + r.j0 + j];
@@ -162,6 +176,34 @@ __global__ __launch_bounds__(256) void page_move(PageMoveArgs a) {
   if (!r.copy) return;
   const int64_t page = page_bytes(a.row_bytes, a.pair_bytes);
   copy_page(a.from_pool + src * page, a.to_pool + dst * page, part, kPageTokens, a.row_bytes, a.pair_bytes);
+}
+__global__ __launch_bounds__(256) void page_move(PageMoveArgs a) { pages_of(a, blockIdx.x); }
+
+// Few moves and few pages: a launch of its own for the pages is 3 us of a call of 11.
+template <bool ONE, typename Pages>
+__global__ __launch_bounds__(256) void few(FewMoves m, Pages p, int wgs) {
+  const int rows = wgs * m.n_parts;
+  if ((int)blockIdx.x < rows) move_rows_of<ONE>(m, blockIdx.x % wgs, blockIdx.x / wgs);
+  else pages_of(p, blockIdx.x - rows);
+}
+
+int page_wgs(const FewPageCopies &p) { return p.n_copies * kPageParts + 1; }
+int page_wgs(const FewPageMoves &p) { return p.n_pages * kPageParts; }
+
+template <int N>
+int last_wg(const MoveArgsOf<N> &a) {
+  int n = 0;
+  while (n < kMaxItems && a.wg_begin[n + 1] != INT32_MAX) ++n;
+  return a.wg_begin[n];
+}
+
+template <typename Pages>
+hipError_t launch_few_of(const FewMoves &m, const Pages &p, hipStream_t s) {
+  const int wgs = last_wg(m);
+  const dim3 grid((unsigned)(wgs * m.n_parts + page_wgs(p)));
+  if (m.part[m.n_parts] == m.n_parts) hipLaunchKernelGGL((few<true, Pages>), grid, dim3(256), 0, s, m, p, wgs);
+  else hipLaunchKernelGGL((few<false, Pages>), grid, dim3(256), 0, s, m, p, wgs);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -174,12 +216,16 @@ int64_t move_workgroups(int64_t rows, int32_t row_bytes, int32_t pair_bytes) {
 }
 
 hipError_t launch_move_rows(const MoveArgs &a, hipStream_t s) {
-  int n = 0;
-  while (n < kMaxItems && a.wg_begin[n + 1] != INT32_MAX) ++n;
-  if (a.wg_begin[n] == 0) return hipSuccess;
-  hipLaunchKernelGGL(move_rows, dim3((unsigned)a.wg_begin[n], (unsigned)a.n_parts), dim3(256), 0, s, a);
+  const int n = last_wg(a);
+  if (n == 0) return hipSuccess;
+  const dim3 grid((unsigned)n, (unsigned)a.n_parts);
+  if (a.part[a.n_parts] == a.n_parts) hipLaunchKernelGGL(move_rows<true>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(move_rows<false>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
+
+hipError_t launch_few(const FewMoves &m, const FewPageCopies &p, hipStream_t s) { return launch_few_of(m, p, s); }
+hipError_t launch_few(const FewMoves &m, const FewPageMoves &p, hipStream_t s) { return launch_few_of(m, p, s); }
 
 hipError_t launch_table_move(const TableMoveArgs &a, int n_units, hipStream_t s) {
   hipLaunchKernelGGL(table_move, dim3((unsigned)((a.most + 255) / 256), (unsigned)n_units, (unsigned)a.n_parts),

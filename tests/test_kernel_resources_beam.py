@@ -57,7 +57,7 @@ def test_beam_selection(table):
 
 
 def test_copies(table):
-    names = [n for n in table if re.search("move_rows|table_move|page_copy|page_move", n)]
-    assert len(names) == 4
+    names = [n for n in table if re.search("move_rows|table_move|page_copy|page_move|few", n)]
+    assert len(names) == 9, names
     for n in names:
         assert table[n][1] == 0, n
