@@ -7,9 +7,16 @@ import re
 import pytest
 
 from paper_2609_02029_amd import build
-from test_kernel_resources import _compile, _demangle, _kernels
+from test_kernel_resources import _compile
 
 FORMATS = {"bf16": 0, "f16": 1, "fp8": 2, "i8": 4}
+
+
+def _short(name):
+    """kernel<integers>, or as it is mangled where a type is among its arguments."""
+    base = re.sub(r"^_ZN4hwkv12_GLOBAL__N_1\d+", "", name)
+    m = re.match(r"([a-z_]+)I((?:L[ib]\d+E)+)E", base)
+    return f"{m.group(1)}<{', '.join(re.findall(r'L[ib]([0-9]+)E', m.group(2)))}>" if m else base
 
 
 @pytest.fixture(scope="module")
@@ -23,14 +30,12 @@ def table(tmp_path_factory):
     out = {}
     for p in paths:
         text = open(p).read()
-        lds = {}
         for block in re.split(r"\n  - \.", text[text.index("amdhsa.kernels:"):])[1:]:
-            name = re.search(r"\.name:\s+(\S+)", block)
-            size = re.search(r"\.group_segment_fixed_size:\s+(\d+)", block)
-            if name and size:
-                lds[_demangle(name.group(1))] = int(size.group(1))
-        for name, vg, scratch in _kernels(p):
-            out[name] = (vg, scratch, lds[name])
+            at = [re.search(rf"\.{key}:\s+(\S+)", block) for key in
+                  ("name", "vgpr_count", "private_segment_fixed_size", "group_segment_fixed_size")]
+            if all(at):
+                name, *sizes = (m.group(1) for m in at)
+                out[_short(name)] = tuple(int(x) for x in sizes)
     return out
 
 
@@ -57,7 +62,7 @@ def test_beam_selection(table):
 
 
 def test_copies(table):
-    names = [n for n in table if re.search("move_rows|table_move|page_copy|page_move|few", n)]
+    names = [n for n in table if re.match("move_rows|table_move|page_copy|page_move|few", n)]
     assert len(names) == 9, names
     for n in names:
         assert table[n][1] == 0, n
