@@ -357,7 +357,77 @@ def test_on_another_stream():
     same(was, r.read(), [0, 0, 0])
 
 
-def test_beam_search():
+@pytest.mark.parametrize("fmt", ["bf16", "f16", "fp8", "i8"])
+def test_forked_sequences_under_every_call(fmt):
+    """Each call on sequences that share pages gives the bits that it gives on a twin
+    whose sequences were written one by one; a captured reorder moves what it moved."""
+    D, H, G, B = 64, 2, 2, 4
+    pol = hwkv.policy_set(1, H, H * G, D, 4, [70, 0], [[0, 1]])
+    g = torch.Generator(device=DEV).manual_seed(5)
+    rows = lambda n, h=H: torch.randn((n, h, D), generator=g, device=DEV).to(torch.bfloat16)   # noqa: E731
+    kw = dict(k_scale=0.03, v_scale=0.02) if fmt == "fp8" else {}
+    forked, twin = (hwkv.cache_alloc(pol, B, 1000, kv_format=fmt, n_pages=20, **kw) for _ in range(2))
+    k, v = rows(600), rows(600)
+    hwkv.prefill_write(forked, 0, 2, 0, k, v)
+    hwkv.cache_reorder(forked, [2, 2, 2, 2])
+    for b in range(B):
+        hwkv.prefill_write(twin, 0, b, 0, k, v)
+    assert hwkv.cache_pages(forked)[1] == 20 - 2 - B and hwkv.cache_pages(twin)[1] == 20 - 3 * B
+    ws = torch.empty(hwkv.decode_workspace_bytes(forked), dtype=torch.uint8, device=DEV)
+    rope = hwkv.rope_set(D, [0.5 ** i for i in range(16)])
+    pos = torch.arange(600, 600 + B, dtype=torch.int32, device=DEV)
+
+    def both(f):
+        a, b = f(forked), f(twin)
+        torch.cuda.synchronize()
+        assert torch.equal(a, b) and torch.isfinite(a).all()
+
+    def decode(c, q):
+        out = torch.empty((B, H * G, D), device=DEV)
+        hwkv.decode_attn(c, 0, q, 0.125, out, ws)
+        return out
+
+    for n in (1, 5, 300):
+        seq, q, ck, cv = n % B, rows(n, H * G), rows(n), rows(n)
+        pws = torch.empty(max(256, hwkv.prefill_attn_workspace_bytes(forked, n)), dtype=torch.uint8, device=DEV)
+
+        def prefill(c):
+            out = torch.empty((n, H * G, D), device=DEV)
+            at = hwkv.cache_seq_len(c, 0, seq)
+            hwkv.prefill_attn(c, 0, seq, at, q, ck, cv, 0.125, out, pws)
+            hwkv.prefill_write(c, 0, seq, at, ck, cv)
+            return out
+        both(prefill)
+        kn, vn, qn = rows(B), rows(B), rows(B, H * G)
+
+        def rotate(c):
+            qo = torch.empty_like(qn)
+            hwkv.append_rope(c, 0, rope, pos, kn, vn, qn, qo)
+            return decode(c, qo)
+        both(rotate)
+
+        def fused(c):
+            out = torch.empty((B, H * G, D), device=DEV)
+            hwkv.append_decode_attn(c, 0, kn, vn, qn, 0.125, out, ws)
+            return out
+        both(fused)
+        both(lambda c: decode(c, qn))
+    hwkv.cache_reorder(twin, [1, 0, 3, 2])
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        hwkv.cache_reorder(forked, [1, 0, 3, 2])
+    graph.replay()
+    torch.cuda.synchronize()
+    both(lambda c: decode(c, qn))
+    for b in range(B):
+        hwkv.cache_reset_seq(forked, b)
+    assert hwkv.cache_pages(forked) == (20, 20)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_beam_search(shared):
     """Selection, reordering, appends and decoding together: at every step the
     choice is that of 64-bit scores over the step's logits, and the outputs are
     attention over the tokens of each beam's own history."""
@@ -369,7 +439,8 @@ def test_beam_search():
     prompts = [torch.randint(0, V, (n,), generator=g, device=DEV) for n in (250, 300, 7)]
     pol = hwkv.policy_set(1, H, H * G, D, S, [w, 0], [[0, 1]])
     cache = hwkv.cache_alloc(pol, B, 512, n_pages=24)
-    ws = torch.empty(hwkv.decode_workspace_bytes(cache), dtype=torch.uint8, device=DEV)
+    decode = hwkv.decode_attn_shared if shared else hwkv.decode_attn
+    ws = torch.empty((hwkv.decode_shared_workspace_bytes if shared else hwkv.decode_workspace_bytes)(cache), dtype=torch.uint8, device=DEV)
     for i, p in enumerate(prompts):
         hwkv.prefill_write(cache, 0, i * beams, 0, emb["k"][p[:-1]].contiguous(), emb["v"][p[:-1]].contiguous())
     hwkv.cache_reorder(cache, [b // beams * beams for b in range(B)])
@@ -382,7 +453,7 @@ def test_beam_search():
     from test_gpu_beam import check
     for step in range(steps):
         hwkv.append(cache, 0, emb["k"][tokens].contiguous(), emb["v"][tokens].contiguous())
-        hwkv.decode_attn(cache, 0, emb["q"][tokens].contiguous(), 0.125, out, ws)
+        decode(cache, 0, emb["q"][tokens].contiguous(), 0.125, out, ws)
         if step % 7 == 0 or step == steps - 1:
             got = out.cpu().double()
             for b in range(B):
