@@ -293,6 +293,8 @@ struct Run {
   uint32_t beam, place;
   float bound;                       // below every logit that is asked for
   uint32_t unused;
+  double s, lse;                     // the beam's (lse NaN: one without candidates)
+  __device__ __forceinline__ double score(float x) const { return s + ((double)x - lse); }
 };
 
 // Grid: one workgroup a group.  Two searches for the n first of a list, in the order
@@ -313,16 +315,12 @@ struct Run {
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   constexpr int N = kPerChunk<T>, WAVES = kPickThreads / 64;
-  __shared__ double s_s[kMaxBeams], lse_s[kMaxBeams];        // lse NaN: a beam without candidates
-  __shared__ __attribute__((aligned(16))) Run run_s[kMaxBeams];
-  __shared__ float x_s[kListed];
-  __shared__ uint32_t beam_s[kListed], at_s[kListed];
+  __shared__ __attribute__((aligned(16))) Run run_s[2][kMaxBeams];   // of each search
+  __shared__ uint32_t at_s[kListed];
   __shared__ uint64_t key_s[kListed], kept_key[kListed];
   __shared__ uint32_t kept_at[kListed];
   __shared__ float lane_top[WAVES][64];
-  __shared__ uint64_t best_key[kMaxSelected];
-  __shared__ uint32_t best_at[kMaxSelected];
-  __shared__ float floor_s;
+  __shared__ double floor_s;
   __shared__ int listed, kept, hits_s[WAVES];
   __shared__ __attribute__((aligned(16))) float value_s[kHeld];
   static_assert(kMaxSelected <= kMaxBeams, "a run per beam, or per block");
@@ -364,14 +362,13 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     const double all = wave_sum(part_sum * exp(part_base - top));
     const bool some = all > 0.0 && all < __builtin_inf() && __builtin_fabs(part_s) < __builtin_inf();
     if (lane == 0) {
-      s_s[b] = some ? part_s : 0.0;
-      lse_s[b] = some ? top + log(all) : __builtin_nan("");
-      run_s[b].beam = b;
-      run_s[b].place = b * a.n_blocks;
+      run_s[0][b].s = some ? part_s : 0.0;
+      run_s[0][b].lse = some ? top + log(all) : __builtin_nan("");
+      run_s[0][b].beam = b;
+      run_s[0][b].place = b * a.n_blocks;
     }
   }
   __syncthreads();
-  const auto score_of = [&](int b, float x) { return s_s[b] + ((double)x - lse_s[b]); };
 
   // A score that n blocks reach, from fp32 roundings: the n-th largest of 64 sets'
   // largest (minus infinity: fewer have one).
@@ -382,7 +379,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
       const int r = i / quads;
       const f32x4_t v = held ? *reinterpret_cast<const f32x4_t *>(value_s + 4 * i) : four_maxima(r, 4 * (i - r * quads));
       // (fmaxf passes over the NaN of a beam without candidates)
-      top = fmaxf(top, (float)score_of(r, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))));
+      top = fmaxf(top, (float)run_s[0][r].score(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))));
     }
     lane_top[wave][lane] = top;
     __syncthreads();
@@ -394,24 +391,22 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
       for (int l = 0; l < 64; ++l)
         above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), l)) > top ? 1 : 0;
       const float least = over_wave(above < n ? top : kInf, [](float x, float y) { return fminf(x, y); });
-      if (lane == 0) floor_s = least;
+      // (rounded: less a step)
+      if (lane == 0) floor_s = (double)least - __builtin_fabs((double)least) * 0x1p-23;
     }
     __syncthreads();
   }
-  double floor = (double)floor_s;            // (rounded: less a step)
-  floor -= __builtin_fabs(floor) * 0x1p-23;
-
-  int found = 0;
   for (int search = 0;; ++search) {
+    const double floor = floor_s;
+    Run *const run_of = run_s[search];
     // score >= floor: x >= floor - s + lse, less what fp64 and fp32 round
     const auto set_bounds = [&](bool any) {
       if (threadIdx.x < runs) {
-        const int b = run_s[threadIdx.x].beam;
-        const double s = s_s[b], lse = lse_s[b], x = floor - s + lse;
+        const double s = run_of[threadIdx.x].s, lse = run_of[threadIdx.x].lse, x = floor - s + lse;
         const double off = (__builtin_fabs(floor) + __builtin_fabs(s) + __builtin_fabs(lse)) * 0x1p-48 +
                            __builtin_fabs(x) * 0x1p-22;
         // (of a beam without candidates nothing, of a floor of minus infinity all)
-        run_s[threadIdx.x].bound = lse != lse ? kInf : any || floor == -__builtin_inf() ? -__FLT_MAX__ : (float)(x - off);
+        run_of[threadIdx.x].bound = lse != lse ? kInf : any || floor == -__builtin_inf() ? -__FLT_MAX__ : (float)(x - off);
       }
       if (threadIdx.x == 0) listed = 0;
       __syncthreads();
@@ -428,28 +423,27 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
 #pragma unroll
           for (int k = 0; k < kAhead; ++k) {
             const int i = min(i0 + k * kPickThreads, all - 1), r = i / quads, j = 4 * (i - r * quads);
-            const uint32_t beam = run_s[r].beam;
+            const uint32_t beam = run_of[r].beam;
             v[k] = search == 0 ? four_maxima(r, j)
-                               : four_logits<T>(a, row0 + beam, run_s[r].place + j - beam * (uint32_t)a.vocab);
+                               : four_logits<T>(a, row0 + beam, run_of[r].place + j - beam * (uint32_t)a.vocab);
           }
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
           const int i = i0 + k * kPickThreads, r = i / quads;
           if (k > 0 && (held || i >= all)) break;
-          const Run run = run_s[r];
+          const Run run = run_of[r];
           if (!(fmaxf(fmaxf(v[k].x, v[k].y), fmaxf(v[k].z, v[k].w)) >= run.bound)) continue;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (v[k][e] >= run.bound) f(run.beam, v[k][e], run.place + 4 * (i - r * quads) + e);
+            if (v[k][e] >= run.bound) f(order_key(run.score(v[k][e])), run.place + 4 * (i - r * quads) + e);
         }
       }
     };
-    const auto list = [&](int b, float x, uint32_t at) {
+    const auto list = [&](uint64_t key, uint32_t at) {
       const int l = atomicAdd(&listed, 1);
       if (l < kListed) {
-        x_s[l] = x;
-        beam_s[l] = b;
+        key_s[l] = key;
         at_s[l] = at;
       }
     };
@@ -470,8 +464,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
         if (step < 64) over = (least | 1ull << (63 - step)) - 1;
         if (step > 64) over = ~0ull, equal = least, upto = last | 1u << (96 - step);
         int hits = 0;
-        visit([&](int b, float x, uint32_t at) {
-          const uint64_t key = order_key(score_of(b, x));
+        visit([&](uint64_t key, uint32_t at) {
           hits += key > over || (key == equal && at < upto) ? 1 : 0;
         });
         hits = over_wave(hits, [](int x, int y) { return x + y; });
@@ -484,15 +477,12 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
         else if (step == 64) more = n - hits;          // items at `least` that are taken
         else last = hits < more ? upto : last;
       }
-      visit([&](int b, float x, uint32_t at) {
-        const uint64_t key = order_key(score_of(b, x));
-        if (key > least || (key == least && at <= last)) list(b, x, at);
+      visit([&](uint64_t key, uint32_t at) {
+        if (key > least || (key == least && at <= last)) list(key, at);
       });
       __syncthreads();
     }
     int all = min(listed, kListed);
-    for (int i = threadIdx.x; i < all; i += kPickThreads) key_s[i] = order_key(score_of(beam_s[i], x_s[i]));
-    __syncthreads();
     const uint64_t *key = key_s;
     const uint32_t *place = at_s;
     if (all > kRanked) {
@@ -532,43 +522,43 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
         const uint32_t p = place[j];
         before += (k > mine) | ((k == mine) & (p < at));
       }
-      if (before < n) {
-        best_key[before] = mine;
-        best_at[before] = at;
+      if (before >= n) continue;
+      if (search == 0) {
+        // its block's logits are a run of the next list, from the n-th's largest on
+        const uint32_t b = at / (uint32_t)a.n_blocks;
+        run_s[1][before] = {b, b * (uint32_t)a.vocab + (at - b * (uint32_t)a.n_blocks) * kBlock, 0.f, 0u,
+                            run_s[0][b].s, run_s[0][b].lse};
+        if (before == n - 1) floor_s = key_score(mine);
+      } else {
+        const int64_t o = (int64_t)blockIdx.x * n + before;
+        a.out_scores[o] = (float)key_score(mine);
+        a.out_parents[o] = (int32_t)(row0 + at / a.vocab);
+        a.out_tokens[o] = (int32_t)(at % a.vocab);
       }
     }
+    const int found = min(all, n);
+    if (search == 1 || found == 0) {
+      if ((int)threadIdx.x >= found && (int)threadIdx.x < n) {
+        const int64_t o = (int64_t)blockIdx.x * n + threadIdx.x;
+        a.out_scores[o] = -kInf;
+        a.out_parents[o] = a.out_tokens[o] = -1;
+      }
+      return;
+    }
+    if (threadIdx.x == 0 && found < n) floor_s = -__builtin_inf();
     __syncthreads();
-    found = min(all, n);
-    if (search == 1 || found == 0) break;
-    // next: the logits of these blocks, from the last one's largest on
-    floor = found == n ? key_score(best_key[n - 1]) : -__builtin_inf();
     runs = found;
     quads = kBlock / 4;
     held = runs * kBlock <= kHeld;
-    if (threadIdx.x < runs) {
-      const int at = best_at[threadIdx.x], b = at / a.n_blocks;
-      run_s[threadIdx.x].beam = b;
-      run_s[threadIdx.x].place = (uint32_t)b * a.vocab + (at - b * a.n_blocks) * kBlock;
-    }
-    __syncthreads();
 #pragma unroll 4
     for (int i = threadIdx.x; i < runs * (kBlock / N) && held; i += kPickThreads) {
-      const Run run = run_s[i / (kBlock / N)];
+      const Run run = run_s[1][i / (kBlock / N)];
       const u32x4_t v = Row<T>(a, row0 + run.beam)
                             .load((int)(run.place - run.beam * (uint32_t)a.vocab) / N + i % (kBlock / N), a.vocab);
 #pragma unroll
       for (int e = 0; e < N; ++e) value_s[i * N + e] = element<T>(v, e);
     }
     __syncthreads();
-  }
-  if (threadIdx.x < n) {
-    const int i = threadIdx.x;
-    const int64_t o = (int64_t)blockIdx.x * n + i;
-    const bool some = i < found;
-    const uint32_t at = some ? best_at[i] : 0;
-    a.out_scores[o] = some ? (float)key_score(best_key[i]) : -kInf;
-    a.out_parents[o] = some ? (int32_t)(row0 + at / a.vocab) : -1;
-    a.out_tokens[o] = some ? (int32_t)(at % a.vocab) : -1;
   }
 }
 

@@ -2993,7 +2993,7 @@ void fill_page_copies(const hwkv_cache *c, const PagePlan &P, size_t *i, size_t 
 // Copies the pages of a reorder and brings the device's table in line: by its changed
 // entries, or, where these are many, row by row as the sequences move (a fork of 30,000
 // tokens, 128 full units, eight ways: 105,000 entries, 435 us against 1,784 as lists;
-// 384 sequences permuted, 4,600 entries: 217 us against 263).
+// 32 beams of 1,500 to 6,000 tokens, 16 full units: 217 us against 263).
 int launch_page_copies(const hwkv_cache *c, const PagePlan &P, const MovePlan &plan, hipStream_t s) {
   const std::vector<Move> &moves = plan.moves;
   size_t i = 0, e = 0;
@@ -3305,9 +3305,12 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
   });
   std::vector<Family> families;
   if (full(heads[0])) {
-    std::vector<int32_t> all(B);
-    for (int32_t b = 0; b < B; ++b) all[b] = b;
-    find_families(c, layer, layer * H + heads[0], all, &families);
+    std::vector<int32_t> some;                   // that share their first page
+    const int32_t u = layer * H + heads[0];
+    for (int32_t b = 0; b < B; ++b)
+      if (len(b) >= hwkv::kPageTokens && c->refs[(size_t)c->pt_host[(size_t)page_tab_off(c, u, b)]] > 1)
+        some.push_back(b);
+    find_families(c, layer, u, some, &families);
   }
   std::sort(families.begin(), families.end(),
             [](const Family &x, const Family &y) { return x.members[0] < y.members[0]; });

@@ -30,9 +30,9 @@ __host__ __device__ constexpr int64_t part_chunks(int part, int64_t rows, int ro
 // destinations is written, within a round by the registers, from round to round by
 // the order of the moves (host).  A round is a read and a write of memory in a row, about
 // 3.7 us: rounds that touch other sequences are parts of their own, side by side (56
-// sequences of 5 rows, 7 rounds: 26.6 us in one part, 7.1 in seven).  384 sequences of
-// 1,500 to 6,000 tokens, windows of 1,024: 980 MB in 201 us, 4.9 TB/s, the rate of a
-// copy.
+// sequences of 5 rows, 7 rounds: 26.6 us in one part, 7.1 in seven).  32 beams of 1,500
+// to 6,000 tokens, 48 units with windows of 1,024: 980 MB in 201 us, 4.9 TB/s, the rate
+// of a copy.
 template <bool ONE, int M>
 __device__ __forceinline__ void move_rows_of(const MoveArgsOf<M> &a, int block, int part_of_moves) {
   const int lane = threadIdx.x & 63;
