@@ -184,11 +184,11 @@ struct Sum {
 // Grid: n_splits workgroups a row.  Wave w of split i takes blocks 4 i + w, and so
 // on in steps of 4 n_splits, DEEP at a time.  What bounds it: HBM and the 64-bit sums
 // beside it, 22 vector instructions a logit in all.  512 rows of 131,072 fp32 logits (268
-// MB): 52 us, 5.2 TB/s; 528 rows of 161,840 bf16 logits (171 MB): 68 us, three quarters
-// of which the vector units are busy.  (Registers for eight workgroups a CU: spills.)
+// MB): 51 us, 5.2 TB/s; 528 rows of 161,840 bf16 logits (171 MB): 63 us, three quarters
+// of which the vector units are busy.  (Registers for eight workgroups a CU: spills; for
+// seven: as fast.)
 template <int T, int DEEP>
-__global__ __launch_bounds__(kScanWaves * 64) __attribute__((amdgpu_waves_per_eu(7)))
-void beam_scan(BeamArgs a) {
+__global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
   constexpr int N = kPerChunk<T>, C = kBlockChunks<T>;
   const int64_t row = blockIdx.x / a.n_splits;
   const int split = blockIdx.x % a.n_splits;
@@ -202,14 +202,25 @@ void beam_scan(BeamArgs a) {
   // whole shift, so that x log2 e needs no difference first; others a logit as their
   // base, from which they differ exactly.
   double sum = 0.0, base = kNone, shift = 0.0;
-  float lowest = 0.0f;                       // base - 690
+  float lowest = 0.0f, over = -__FLT_MAX__;  // base - 690, base + 600
+  double magic = 0.0;                        // 1.5 * 2^52 - shift: added, the low word is the
+                                             //   whole part less the shift
   bool near = true;
   for (int b0 = split * kScanWaves + wave; b0 < a.n_blocks; b0 += DEEP * step) {
     u32x4_t v[DEEP][C];
+    if ((b0 + (DEEP - 1) * step + 1) * kBlock <= a.vocab) {    // uniform: whole blocks
+      const uint8_t *const from = r.at + (int64_t)b0 * (kBlock * kBytes<T>);
 #pragma unroll
-    for (int i = 0; i < DEEP; ++i)
+      for (int i = 0; i < DEEP; ++i)
 #pragma unroll
-      for (int c = 0; c < C; ++c) v[i][c] = r.load(((b0 + i * step) * C + c) * 64 + lane, a.vocab);
+        for (int c = 0; c < C; ++c)
+          v[i][c] = reinterpret_cast<const chunk_t *>(from + (int64_t)i * step * (kBlock * kBytes<T>))[c * 64 + lane];
+    } else {
+#pragma unroll
+      for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+        for (int c = 0; c < C; ++c) v[i][c] = r.load(((b0 + i * step) * C + c) * 64 + lane, a.vocab);
+    }
 #pragma unroll
     for (int i = 0; i < DEEP; ++i) {
       const int b = b0 + i * step;
@@ -231,16 +242,16 @@ void beam_scan(BeamArgs a) {
         sum = __builtin_nan("");
         continue;
       }
-      if ((double)top > base + 600.0) {
+      if (top > over) {
         const double before = base;
         near = __builtin_fabsf(top) <= 0x1p16f;
         shift = rint((double)top * kLog2e);
         base = near ? shift * kLn2 : (double)top;
         lowest = (float)(base - 690.0);
+        over = (float)(base + 600.0);
+        magic = 0x1.8p52 - shift;
         sum *= exp(before - base);
       }
-      // with 1.5 * 2^52 - shift added, the low word is the whole part less the shift
-      const double magic = 0x1.8p52 - shift;
       const auto add = [&](float xe) {
         const double d = (double)xe, y = __builtin_fma(d, kLog2e, magic);
         const double p = exp2_small(__builtin_fma(d, kLog2e, -(y - magic)));
@@ -576,12 +587,18 @@ hipError_t launch(const BeamArgs &a, int64_t n_groups, hipStream_t s) {
 
 int32_t beam_blocks(int32_t vocab) { return (vocab + kBlock - 1) / kBlock; }
 
-// Workgroups a row: those of all rows run at once (seven fit a CU), each with a block or
-// more for every wave, and no fewer blocks for some waves than need be.
+// Workgroups a row: those of all rows run at once (six fit a CU), or, where every wave
+// still has eight blocks or more, in two rounds, which even the CUs out; each with a block
+// or more for every wave, and no fewer blocks for some waves than need be.  (One round
+// against two: 96 rows of 131,072 bf16 logits 12.3 and 14.8 us, of 232,019 20.5 and 19.9;
+// 528 of 161,840 73 and 63; four rounds 19.8, 23.5 and 62.8.)
 int32_t beam_splits(int64_t n_rows, int32_t n_blocks) {
   const int64_t quads = (n_blocks + kScanWaves - 1) / kScanWaves;
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(quads, 64), kScanTarget / n_rows));
-  const int64_t per_wave = (quads + most - 1) / most;
+  const auto most = [&](int64_t target) {
+    return std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(quads, 64), target / n_rows));
+  };
+  const int64_t splits = quads / most(2 * kScanTarget) >= 8 ? most(2 * kScanTarget) : most(kScanTarget);
+  const int64_t per_wave = (quads + splits - 1) / splits;
   return (int32_t)((quads + per_wave - 1) / per_wave);
 }
 

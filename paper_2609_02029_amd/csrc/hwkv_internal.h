@@ -370,7 +370,7 @@ hipError_t launch_few(const FewMoves &m, const FewPageMoves &p, hipStream_t s);
 
 // Beam search's selection (beam_kernels.hip).
 constexpr int kMaxBeams = 64, kMaxSelected = 64;
-constexpr int kScanTarget = 1792;  // most workgroups of the scan of all rows (if not one a row)
+constexpr int kScanTarget = 1536;  // workgroups of the scan that run at once
 struct BeamArgs {
   const void *logits;            // rows stride elements apart
   int64_t stride;

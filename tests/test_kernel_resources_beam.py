@@ -57,8 +57,8 @@ def test_beam_selection(table):
         assert scratch == 0 and vg <= 128 and lds <= 80 * 1024
         scan = [x for name, x in table.items() if name.startswith(f"beam_scan<{t}, ")]
         assert len(scan) == 1
-        # seven workgroups a CU
-        assert scan[0][0] <= 72 and scan[0][1] == 0
+        # six workgroups a CU
+        assert scan[0][0] <= 80 and scan[0][1] == 0
 
 
 def test_copies(table):
