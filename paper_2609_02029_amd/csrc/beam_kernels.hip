@@ -295,9 +295,9 @@ __device__ __forceinline__ double key_score(uint64_t key) {
 }
 
 constexpr int kPickThreads = 512, kListed = 1024;
-constexpr int kHeld = 8192;          // logits that a workgroup keeps in LDS
+constexpr int kHeld = 8192, kHeldMost = 32768;   // values that a workgroup keeps in LDS
+static_assert(kHeldMost >= kMaxSelected * kBlock, "the blocks of a second search");
 constexpr int kRanked = 96;          // listed items that are counted against each other as they are
-constexpr int kAhead = 6;            // reads in flight of a list that it does not keep
 
 // A run of a search's list: consecutive places of one beam.
 struct Run {
@@ -323,7 +323,7 @@ struct Run {
 // (about 1.5 us each) and some twenty steps through LDS.  24 groups of 4 beams, 131,072
 // logits: with keys formed for every logit and a visit's code for each purpose 15 us,
 // one visit for all purposes 13.6, a bound in front of the keys 7.6.
-template <int T>
+template <int T, int HELD>
 __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   constexpr int N = kPerChunk<T>, WAVES = kPickThreads / 64;
   __shared__ __attribute__((aligned(16))) Run run_s[2][kMaxBeams];   // of each search
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   __shared__ float lane_top[WAVES][64];
   __shared__ double floor_s;
   __shared__ int listed, kept, hits_s[WAVES];
-  __shared__ __attribute__((aligned(16))) float value_s[kHeld];
+  __shared__ __attribute__((aligned(16))) float value_s[HELD];
   static_assert(kMaxSelected <= kMaxBeams, "a run per beam, or per block");
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   // sums and block maxima
   int runs = a.n_beams, items = a.n_blocks;  // of the list, and the items of each
   int quads = (items + 3) / 4;
-  bool held = runs * quads * 4 <= kHeld;
+  bool held = runs * quads * 4 <= HELD;
   // an item of a list that is not held, or is to be
   const auto maximum = [&](int r, int j) {
     return j < a.n_blocks ? a.block_max[(row0 + r) * a.n_blocks + j] : -kInf;
@@ -353,31 +353,34 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     if (j + 4 <= a.n_blocks) return *reinterpret_cast<const any_t *>(a.block_max + (row0 + r) * a.n_blocks + j);
     return f32x4_t{maximum(r, j), maximum(r, j + 1), maximum(r, j + 2), maximum(r, j + 3)};
   };
-  double part_sum = 0.0, part_base = kNone, part_s = 0.0;
-  const auto load_parts = [&](int b) {
-    const double *const part = a.part + ((row0 + b) * a.n_splits + lane) * 2;
-    if (lane < a.n_splits) part_sum = part[0], part_base = part[1];
-    part_s = (double)a.scores[row0 + b];
+  struct Part {
+    double sum, base, s;
   };
-  if (wave < a.n_beams) load_parts(wave);
+  const auto load_part = [&](int b) -> Part {
+    Part p = {0.0, kNone, 0.0};
+    if (b >= a.n_beams) return p;
+    const double *const part = a.part + ((row0 + b) * a.n_splits + lane) * 2;
+    if (lane < a.n_splits) p.sum = part[0], p.base = part[1];
+    p.s = (double)a.scores[row0 + b];
+    return p;
+  };
+  Part next = load_part(wave);
   if (held) {
-#pragma unroll 2
+#pragma unroll 4
     for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
       const int r = i / quads, j = (i - r * quads) * 4;
       *reinterpret_cast<f32x4_t *>(value_s + 4 * i) = four_maxima(r, j);
     }
   }
   for (int b = wave; b < a.n_beams; b += WAVES) {
-    if (b != wave) load_parts(b);
-    const double top = over_wave(part_base, [](double x, double y) { return fmax(x, y); });
-    const double all = wave_sum(part_sum * exp(part_base - top));
-    const bool some = all > 0.0 && all < __builtin_inf() && __builtin_fabs(part_s) < __builtin_inf();
-    if (lane == 0) {
-      run_s[0][b].s = some ? part_s : 0.0;
-      run_s[0][b].lse = some ? top + log(all) : __builtin_nan("");
-      run_s[0][b].beam = b;
-      run_s[0][b].place = b * a.n_blocks;
-    }
+    const Part p = next;
+    next = load_part(b + WAVES);
+    const double top = over_wave(p.base, [](double x, double y) { return fmax(x, y); });
+    const double all = wave_sum(p.sum * exp(p.base - top));
+    const bool some = all > 0.0 && all < __builtin_inf() && __builtin_fabs(p.s) < __builtin_inf();
+    if (lane == 0)
+      run_s[0][b] = {(uint32_t)b, (uint32_t)(b * a.n_blocks), 0.f, 0u, some ? p.s : 0.0,
+                     some ? top + log(all) : __builtin_nan("")};
   }
   __syncthreads();
 
@@ -422,33 +425,19 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
       if (threadIdx.x == 0) listed = 0;
       __syncthreads();
     };
-    // every item that its run's bound lets pass (of lists that are not held several reads
-    // are under way at once)
+    // every item that its run's bound lets pass
     const auto visit = [&](auto f) {
-      const int all = runs * quads, step = held ? kPickThreads : kAhead * kPickThreads;
-      for (int i0 = threadIdx.x; i0 < all; i0 += step) {
-        f32x4_t v[kAhead];
-        if (held) {
-          v[0] = *reinterpret_cast<const f32x4_t *>(value_s + 4 * i0);
-        } else {
+      for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
+        const int r = search == 0 ? i / quads : i / (kBlock / 4), j = 4 * (i - r * quads);
+        const Run run = run_of[r];
+        f32x4_t v;
+        if (held) v = *reinterpret_cast<const f32x4_t *>(value_s + 4 * i);
+        else if (search == 0) v = four_maxima(r, j);
+        else v = four_logits<T>(a, row0 + run.beam, run.place + j - run.beam * (uint32_t)a.vocab);
+        if (!(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= run.bound)) continue;
 #pragma unroll
-          for (int k = 0; k < kAhead; ++k) {
-            const int i = min(i0 + k * kPickThreads, all - 1), r = i / quads, j = 4 * (i - r * quads);
-            const uint32_t beam = run_of[r].beam;
-            v[k] = search == 0 ? four_maxima(r, j)
-                               : four_logits<T>(a, row0 + beam, run_of[r].place + j - beam * (uint32_t)a.vocab);
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const int i = i0 + k * kPickThreads, r = i / quads;
-          if (k > 0 && (held || i >= all)) break;
-          const Run run = run_of[r];
-          if (!(fmaxf(fmaxf(v[k].x, v[k].y), fmaxf(v[k].z, v[k].w)) >= run.bound)) continue;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (v[k][e] >= run.bound) f(order_key(run.score(v[k][e])), run.place + 4 * (i - r * quads) + e);
-        }
+        for (int e = 0; e < 4; ++e)
+          if (v[e] >= run.bound) f(order_key(run.score(v[e])), run.place + j + e);
       }
     };
     const auto list = [&](uint64_t key, uint32_t at) {
@@ -560,7 +549,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     __syncthreads();
     runs = found;
     quads = kBlock / 4;
-    held = runs * kBlock <= kHeld;
+    held = runs * kBlock <= HELD;
 #pragma unroll 4
     for (int i = threadIdx.x; i < runs * (kBlock / N) && held; i += kPickThreads) {
       const Run run = run_s[1][i / (kBlock / N)];
@@ -579,7 +568,11 @@ hipError_t launch(const BeamArgs &a, int64_t n_groups, hipStream_t s) {
   hipLaunchKernelGGL((beam_scan<T, 4 / kBlockChunks<T>>), grid, threads, 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(beam_pick<T>, dim3((unsigned)n_groups), dim3(kPickThreads), 0, s, a);
+  // (with more in LDS one workgroup fits a CU, not two; without it 28 of 161,840 x 16 logits
+  // took 75.2 us for 33 groups, not 73.5, and 64 of 200,000 x 64 58.6, not 52.9)
+  const int64_t values = std::max<int64_t>((int64_t)a.n_beams * ((a.n_blocks + 3) / 4 * 4), a.n_out * kBlock);
+  if (values <= kHeld) hipLaunchKernelGGL((beam_pick<T, kHeld>), dim3((unsigned)n_groups), dim3(kPickThreads), 0, s, a);
+  else hipLaunchKernelGGL((beam_pick<T, kHeldMost>), dim3((unsigned)n_groups), dim3(kPickThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -53,8 +53,9 @@ def test_shared_decode(table):
 
 def test_beam_selection(table):
     for t in (0, 1, 2):
-        vg, scratch, lds = table[f"beam_pick<{t}>"]
-        assert scratch == 0 and vg <= 128 and lds <= 80 * 1024
+        for held, most in ((8192, 80), (32768, 160)):
+            vg, scratch, lds = table[f"beam_pick<{t}, {held}>"]
+            assert scratch == 0 and vg <= 128 and lds <= most * 1024
         scan = [x for name, x in table.items() if name.startswith(f"beam_scan<{t}, ")]
         assert len(scan) == 1
         # six workgroups a CU
