@@ -175,6 +175,8 @@ __device__ __forceinline__ double exp2_small(double f) {
   return __builtin_fma(p, f, 0x1.ffffffffa7135p-1);
 }
 
+__host__ __device__ constexpr int whole_quads(int n) { return (n + 3) & ~3; }
+
 // A sum of e^x as sum * e^base (base kNone where there is none).
 constexpr double kNone = -0x1p1000;
 struct Sum {
@@ -194,8 +196,10 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
   const int split = blockIdx.x % a.n_splits;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const Row<T> r(a, row);
-  float *const block_max = a.block_max + row * a.n_blocks;
+  float *const block_max = a.block_max + row * whole_quads(a.n_blocks);
   const int step = kScanWaves * a.n_splits;
+  // (rows of maxima are whole quads)
+  if (split == 0 && (int)threadIdx.x < whole_quads(a.n_blocks) - a.n_blocks) block_max[a.n_blocks + threadIdx.x] = -kInf;
   // e^(x - base), summed; the base is set by the largest logit of the first block that
   // has one, and of a block whose largest passes it by 600, and a logit more than 690
   // below it counts as that (e^-690).  Logits up to 2^16 take base = shift ln 2 with a
@@ -322,7 +326,7 @@ struct Run {
 // What bounds it: latency, of two reads of what other XCDs wrote or left in memory
 // (about 1.5 us each) and some twenty steps through LDS.  24 groups of 4 beams, 131,072
 // logits: with keys formed for every logit and a visit's code for each purpose 15 us,
-// one visit for all purposes 13.6, a bound in front of the keys 7.6.
+// one visit for all purposes 13.6, a bound in front of the keys 7.6, maxima in whole quads 7.
 template <int T, int HELD>
 __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   constexpr int N = kPerChunk<T>, WAVES = kPickThreads / 64;
@@ -341,18 +345,10 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   const int n = a.n_out;
 
   // sums and block maxima
-  int runs = a.n_beams, items = a.n_blocks;  // of the list, and the items of each
-  int quads = (items + 3) / 4;
+  int runs = a.n_beams;              // of the list,
+  int quads = whole_quads(a.n_blocks) / 4;   // and the quads of each
   bool held = runs * quads * 4 <= HELD;
-  // an item of a list that is not held, or is to be
-  const auto maximum = [&](int r, int j) {
-    return j < a.n_blocks ? a.block_max[(row0 + r) * a.n_blocks + j] : -kInf;
-  };
-  const auto four_maxima = [&](int r, int j) -> f32x4_t {
-    typedef f32x4_t __attribute__((aligned(4))) any_t;
-    if (j + 4 <= a.n_blocks) return *reinterpret_cast<const any_t *>(a.block_max + (row0 + r) * a.n_blocks + j);
-    return f32x4_t{maximum(r, j), maximum(r, j + 1), maximum(r, j + 2), maximum(r, j + 3)};
-  };
+  const f32x4_t *const maxima = reinterpret_cast<const f32x4_t *>(a.block_max) + row0 * quads;
   struct Part {
     double sum, base, s;
   };
@@ -367,10 +363,8 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   Part next = load_part(wave);
   if (held) {
 #pragma unroll 4
-    for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
-      const int r = i / quads, j = (i - r * quads) * 4;
-      *reinterpret_cast<f32x4_t *>(value_s + 4 * i) = four_maxima(r, j);
-    }
+    for (int i = threadIdx.x; i < runs * quads; i += kPickThreads)
+      reinterpret_cast<f32x4_t *>(value_s)[i] = maxima[i];
   }
   for (int b = wave; b < a.n_beams; b += WAVES) {
     const Part p = next;
@@ -379,7 +373,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     const double all = wave_sum(p.sum * exp(p.base - top));
     const bool some = all > 0.0 && all < __builtin_inf() && __builtin_fabs(p.s) < __builtin_inf();
     if (lane == 0)
-      run_s[0][b] = {(uint32_t)b, (uint32_t)(b * a.n_blocks), 0.f, 0u, some ? p.s : 0.0,
+      run_s[0][b] = {(uint32_t)b, (uint32_t)(b * quads * 4), 0.f, 0u, some ? p.s : 0.0,
                      some ? top + log(all) : __builtin_nan("")};
   }
   __syncthreads();
@@ -391,7 +385,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
 #pragma unroll 2
     for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
       const int r = i / quads;
-      const f32x4_t v = held ? *reinterpret_cast<const f32x4_t *>(value_s + 4 * i) : four_maxima(r, 4 * (i - r * quads));
+      const f32x4_t v = held ? reinterpret_cast<const f32x4_t *>(value_s)[i] : maxima[i];
       // (fmaxf passes over the NaN of a beam without candidates)
       top = fmaxf(top, (float)run_s[0][r].score(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))));
     }
@@ -431,8 +425,8 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
         const int r = search == 0 ? i / quads : i / (kBlock / 4), j = 4 * (i - r * quads);
         const Run run = run_of[r];
         f32x4_t v;
-        if (held) v = *reinterpret_cast<const f32x4_t *>(value_s + 4 * i);
-        else if (search == 0) v = four_maxima(r, j);
+        if (held) v = reinterpret_cast<const f32x4_t *>(value_s)[i];
+        else if (search == 0) v = maxima[i];
         else v = four_logits<T>(a, row0 + run.beam, run.place + j - run.beam * (uint32_t)a.vocab);
         if (!(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= run.bound)) continue;
 #pragma unroll
@@ -525,8 +519,8 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
       if (before >= n) continue;
       if (search == 0) {
         // its block's logits are a run of the next list, from the n-th's largest on
-        const uint32_t b = at / (uint32_t)a.n_blocks;
-        run_s[1][before] = {b, b * (uint32_t)a.vocab + (at - b * (uint32_t)a.n_blocks) * kBlock, 0.f, 0u,
+        const uint32_t row_items = 4 * quads, b = at / row_items;
+        run_s[1][before] = {b, b * (uint32_t)a.vocab + (at - b * row_items) * kBlock, 0.f, 0u,
                             run_s[0][b].s, run_s[0][b].lse};
         if (before == n - 1) floor_s = key_score(mine);
       } else {
@@ -569,8 +563,8 @@ hipError_t launch(const BeamArgs &a, int64_t n_groups, hipStream_t s) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // (with more in LDS one workgroup fits a CU, not two; without it 28 of 161,840 x 16 logits
-  // took 75.2 us for 33 groups, not 73.5, and 64 of 200,000 x 64 58.6, not 52.9)
-  const int64_t values = std::max<int64_t>((int64_t)a.n_beams * ((a.n_blocks + 3) / 4 * 4), a.n_out * kBlock);
+  // took 75.2 us for 33 groups, not 73.5, and 64 of 200,000 x 64 58.6, not 52.9.)
+  const int64_t values = std::max<int64_t>((int64_t)a.n_beams * whole_quads(a.n_blocks), a.n_out * kBlock);
   if (values <= kHeld) hipLaunchKernelGGL((beam_pick<T, kHeld>), dim3((unsigned)n_groups), dim3(kPickThreads), 0, s, a);
   else hipLaunchKernelGGL((beam_pick<T, kHeldMost>), dim3((unsigned)n_groups), dim3(kPickThreads), 0, s, a);
   return hipGetLastError();
@@ -579,6 +573,7 @@ hipError_t launch(const BeamArgs &a, int64_t n_groups, hipStream_t s) {
 }  // namespace
 
 int32_t beam_blocks(int32_t vocab) { return (vocab + kBlock - 1) / kBlock; }
+int64_t beam_maxima(int32_t n_blocks) { return whole_quads(n_blocks); }
 
 // Workgroups a row: those of all rows run at once (six fit a CU), or, where every wave
 // still has eight blocks or more, in two rounds, which even the CUs out; each with a block

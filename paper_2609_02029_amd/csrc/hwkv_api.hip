@@ -3535,7 +3535,7 @@ int beam_layout(int64_t n_groups, int32_t n_beams, int32_t vocab, int32_t type, 
   a->n_blocks = hwkv::beam_blocks(vocab);
   a->n_splits = hwkv::beam_splits(std::max<int64_t>(1, rows), a->n_blocks);
   *part_bytes = (size_t)rows * a->n_splits * 16;
-  *bytes = *part_bytes + (size_t)rows * a->n_blocks * 4;
+  *bytes = *part_bytes + (size_t)rows * hwkv::beam_maxima(a->n_blocks) * 4;
   return HWKV_OK;
 }
 

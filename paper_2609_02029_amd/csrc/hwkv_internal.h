@@ -376,12 +376,13 @@ struct BeamArgs {
   int64_t stride;
   const float *scores;           // [rows]
   double *part;                  // [rows][n_splits][2]: sums, and their powers of two
-  float *block_max;              // [rows][n_blocks]
+  float *block_max;              // [rows][n_blocks, and minus infinity up to whole quads]
   float *out_scores;             // [groups][n_out]
   int32_t *out_parents, *out_tokens;
   int32_t vocab, n_beams, n_out, n_blocks, n_splits;
 };
 int32_t beam_blocks(int32_t vocab);   // of a row
+int64_t beam_maxima(int32_t n_blocks);   // floats of a row's block_max
 int32_t beam_splits(int64_t n_rows, int32_t n_blocks);
 hipError_t launch_beam_select(int32_t type, const BeamArgs &a, int64_t n_groups, hipStream_t s);
 
