@@ -3466,7 +3466,9 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
     a.block_ml = a.own_acc + rows * D;
     a.own_ml = a.block_ml + cols * 2;
     int rc = check_device(hwkv::launch_decode_shared(c->fmt, (int)D, a, s), "shared decode launch");
-    if (rc == HWKV_OK) rc = check_device(hwkv::launch_shared_merge((int)D, a, s), "shared decode merge launch");
+    // (an item that is not split writes the output itself)
+    if (rc == HWKV_OK && (a.n_blocks > 0 || L.wgs > (int64_t)a.n_heads * a.n_seqs))
+      rc = check_device(hwkv::launch_shared_merge((int)D, a, s), "shared decode merge launch");
     if (rc != HWKV_OK) return rc;
   }
   return HWKV_OK;
