@@ -4,6 +4,8 @@ Scores are 64-bit sums rounded once to fp32: off by half a step, 2^-24 of the
 value, by the error of lse (5.5e-11 a term, so at most 1e-10 in all), and in rows far
 from zero by the reference's own rounding of lse (half a step of 2^-52 of it, and as
 much again in x - lse)."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -89,6 +91,24 @@ def test_many_beams_and_groups(t):
     for G, B, V, n in ((70, 4, 3001, 8), (1, 64, 40001, 64), (300, 8, 130, 16), (1, 1, 600001, 5)):
         x, s = inputs(G, B, V, t, seed=3)
         check(select(x, s, n), x, s, n)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_more_blocks_than_fit_a_workgroup(t):
+    """Searches whose maxima stay in memory, also where they are all alike."""
+    G, B, V, n = 1, 5, (1 << 22) + 3, 20
+    x, s = inputs(G, B, V, t, seed=6)
+    check(select(x, s, n), x, s, n)
+    x.fill_(0.5)
+    x[0, 3, 4000000:] = 0.75
+    out = select(x, s.zero_(), n)
+    lse = [math.log(V) + 0.5] * 5
+    lse[3] = math.log(4000000 * math.exp(0.5) + (V - 4000000) * math.exp(0.75))
+    assert out[1].tolist() == [[3] * n] and out[2].tolist() == [list(range(4000000, 4000000 + n))]
+    assert (out[0].double() - (0.75 - lse[3])).abs().max() < 2.0 ** -20    # fp32 of about 15
+    x.fill_(0.5)                                  # every score is -log V
+    out = select(x, s, n)
+    assert out[1].tolist() == [[0] * n] and out[2].tolist() == [list(range(n))]
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
