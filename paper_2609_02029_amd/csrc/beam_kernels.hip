@@ -315,13 +315,16 @@ struct Run {
 // Grid: one workgroup a group.  Two searches for the n first of a list, in the order
 // (score falling, place rising): of the beams' block maxima, then of the logits of the
 // n blocks found; each list goes into LDS, as far as it fits, in quads.  A score that n
-// items reach is known before a search (of 64 sets' largest maxima the n-th largest;
-// the n-th block's), so one comparison of logits with a bound keeps nearly all out,
+// items reach is known before a search (the n-th largest of 64 sets' largest maxima; the
+// n-th block's largest), so one comparison of logits with a bound keeps nearly all out,
 // and what passes is listed, given its 64-bit key, and counted against each other (of
 // many, those that a second such score leaves: 4 groups of 16 beams, 2,165 logits, 18
 // chosen, 302 listed: 19.5 us a call against 27.8).
-// Where the list does not hold them (long runs of equal or rising logits), the n-th
-// key, how many lie above it and then the n-th item's place are found bit by bit first.
+// Where the list of logits does not hold them (few blocks, whose n-th is far below the
+// best), it is made once more above the n-th of 64 sets' largest logits (2 groups of 16
+// beams, 1,100 logits, 30 chosen: 24 us, 380 without).  Where that does not hold them
+// either (long runs of equal or rising logits), the n-th key, how many lie above it and
+// then the n-th item's place are found bit by bit first.
 //
 // What bounds it: latency, of two reads of what other XCDs wrote or left in memory
 // (about 1.5 us each) and some twenty steps through LDS.  24 groups of 4 beams, 131,072
@@ -378,35 +381,41 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   }
   __syncthreads();
 
-  // A score that n blocks reach, from fp32 roundings: the n-th largest of 64 sets'
-  // largest (minus infinity: fewer have one).
-  {
-    float top = -kInf;
-#pragma unroll 2
-    for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
-      const int r = i / quads;
-      const f32x4_t v = held ? reinterpret_cast<const f32x4_t *>(value_s)[i] : maxima[i];
-      // (fmaxf passes over the NaN of a beam without candidates)
-      top = fmaxf(top, (float)run_s[0][r].score(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))));
-    }
-    lane_top[wave][lane] = top;
-    __syncthreads();
-    if (wave == 0) {
-#pragma unroll
-      for (int w = 1; w < WAVES; ++w) top = fmaxf(top, lane_top[w][lane]);
-      int above = 0;
-#pragma unroll
-      for (int l = 0; l < 64; ++l)
-        above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), l)) > top ? 1 : 0;
-      const float least = over_wave(above < n ? top : kInf, [](float x, float y) { return fminf(x, y); });
-      // (rounded: less a step)
-      if (lane == 0) floor_s = (double)least - __builtin_fabs((double)least) * 0x1p-23;
-    }
-    __syncthreads();
-  }
-  for (int search = 0;; ++search) {
-    const double floor = floor_s;
+  for (int search = 0, sets = 1;;) {
     Run *const run_of = run_s[search];
+    const auto quad = [&](int i, int r, int j) -> f32x4_t {
+      if (held) return reinterpret_cast<const f32x4_t *>(value_s)[i];
+      if (search == 0) return maxima[i];
+      return four_logits<T>(a, row0 + run_of[r].beam, run_of[r].place + j - run_of[r].beam * (uint32_t)a.vocab);
+    };
+    // A score that n items reach, from fp32 roundings: the n-th largest of 64 sets'
+    // largest (minus infinity: fewer have one).
+    if (sets) {
+      float top = -kInf;
+#pragma unroll 2
+      for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
+        const int r = i / quads;
+        const f32x4_t v = quad(i, r, 4 * (i - r * quads));
+        // (fmaxf passes over the NaN of a beam without candidates)
+        top = fmaxf(top, (float)run_of[r].score(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))));
+      }
+      lane_top[wave][lane] = top;
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, lane_top[w][lane]);
+        int above = 0;
+#pragma unroll
+        for (int l = 0; l < 64; ++l)
+          above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), l)) > top ? 1 : 0;
+        const float least = over_wave(above < n ? top : kInf, [](float x, float y) { return fminf(x, y); });
+        // (rounded: less a step)
+        const double reached = (double)least - __builtin_fabs((double)least) * 0x1p-23;
+        if (lane == 0) floor_s = search == 0 ? reached : fmax(reached, floor_s);
+      }
+      __syncthreads();
+    }
+    const double floor = floor_s;
     // score >= floor: x >= floor - s + lse, less what fp64 and fp32 round
     const auto set_bounds = [&](bool any) {
       if (threadIdx.x < runs) {
@@ -424,10 +433,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
       for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
         const int r = search == 0 ? i / quads : i / (kBlock / 4), j = 4 * (i - r * quads);
         const Run run = run_of[r];
-        f32x4_t v;
-        if (held) v = reinterpret_cast<const f32x4_t *>(value_s)[i];
-        else if (search == 0) v = maxima[i];
-        else v = four_logits<T>(a, row0 + run.beam, run.place + j - run.beam * (uint32_t)a.vocab);
+        const f32x4_t v = quad(i, r, j);
         if (!(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= run.bound)) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -444,6 +450,11 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     set_bounds(false);
     visit(list);
     __syncthreads();
+    if (listed > kListed && !sets) {
+      __syncthreads();
+      sets = 1;                        // once more, above the sets' bound
+      continue;
+    }
     if (listed > kListed) {
       // the n-th key `least`, then the place `last` of the n-th item
       __syncthreads();
@@ -541,6 +552,8 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     }
     if (threadIdx.x == 0 && found < n) floor_s = -__builtin_inf();
     __syncthreads();
+    search = 1;
+    sets = 0;
     runs = found;
     quads = kBlock / 4;
     held = runs * kBlock <= HELD;

@@ -88,7 +88,8 @@ def test_sizes(t, V):
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
 def test_many_beams_and_groups(t):
-    for G, B, V, n in ((70, 4, 3001, 8), (1, 64, 40001, 64), (300, 8, 130, 16), (1, 1, 600001, 5)):
+    for G, B, V, n in ((70, 4, 3001, 8), (1, 64, 40001, 64), (300, 8, 130, 16), (1, 1, 600001, 5),
+                       (2, 16, 1100, 30), (9, 16, 1500, 64), (3, 8, 1000, 16)):
         x, s = inputs(G, B, V, t, seed=3)
         check(select(x, s, n), x, s, n)
 
