@@ -2829,6 +2829,7 @@ struct PagePlan {
   std::vector<PageCopy> copies;
   std::vector<std::pair<int32_t, int32_t>> entries;   // (table index, page), copies apart
   int32_t n_full = 0;
+  bool by_row = false;           // many entries: the table's rows move instead
 };
 
 // The full units in order: f(unit index, layer, table offset of sequence 0).
@@ -2874,7 +2875,9 @@ int reorder_pages(hwkv_cache *c, const int32_t *parent, PagePlan *P) {
     most_old = std::max(most_old, old);
   });
   P->old.reserve(most_old);
-  P->entries.reserve(entries);
+  P->n_full = (int32_t)n_full;
+  P->by_row = entries > 2 * hwkv::kMaxEntries && n_full <= UINT16_MAX;
+  if (!P->by_row) P->entries.reserve(entries);
   P->freed.reserve(dropped);
   P->orphans.reserve(P->changed.size());
   P->copies.reserve(P->changed.size() * n_full);
@@ -2949,7 +2952,7 @@ int reorder_pages(hwkv_cache *c, const int32_t *parent, PagePlan *P) {
           }
           P->copies.push_back(copy);
           pg = copy.dst;
-        } else {
+        } else if (!P->by_row) {
           P->entries.push_back({pto + j, pg});
         }
         row(pto0, b)[j] = pg;
@@ -2967,7 +2970,6 @@ int reorder_pages(hwkv_cache *c, const int32_t *parent, PagePlan *P) {
     c->refs[(size_t)copy.dst] = 1;
     c->pt_host[(size_t)copy.pto + copy.j] = copy.dst;
   }
-  P->n_full = (int32_t)n_full;
   return HWKV_OK;
 }
 
@@ -2997,8 +2999,7 @@ void fill_page_copies(const hwkv_cache *c, const PagePlan &P, size_t *i, size_t 
 int launch_page_copies(const hwkv_cache *c, const PagePlan &P, const MovePlan &plan, hipStream_t s) {
   const std::vector<Move> &moves = plan.moves;
   size_t i = 0, e = 0;
-  if (P.entries.size() > 2 * hwkv::kMaxEntries && P.n_full <= UINT16_MAX) {
-    e = P.entries.size();
+  if (P.by_row) {
     hwkv::TableMoveArgs t;
     std::memset(&t, 0, sizeof t);
     t.table = device_page_table(c);
@@ -3039,9 +3040,9 @@ int reorder_impl(hwkv_cache *c, const int32_t *parent, hipStream_t s) {
   for (int32_t l = 0; l < c->pol.n_layers; ++l)
     for (int32_t b = 0; b < c->batch; ++b)
       c->n[(size_t)l * c->batch + b] = parent[b] < 0 ? 0 : n[(size_t)l * c->batch + parent[b]];
-  if (!P.copies.empty() || !P.entries.empty()) {
+  if (P.by_row || !P.copies.empty() || !P.entries.empty()) {
     hwkv::FewMoves m;
-    if (P.copies.size() <= hwkv::kFewPages && P.entries.size() <= hwkv::kFewPages &&
+    if (!P.by_row && P.copies.size() <= hwkv::kFewPages && P.entries.size() <= hwkv::kFewPages &&
         few_moves(c, plan, c->base, c->base, &m)) {
       hwkv::FewPageCopies a;
       size_t i = 0, e = 0;
@@ -3315,19 +3316,27 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
   std::sort(families.begin(), families.end(),
             [](const Family &x, const Family &y) { return x.members[0] < y.members[0]; });
   // blocks that a launch holds, and the sequences of none as one each
+  struct Part {
+    int32_t first, count, pages;
+  };
   std::vector<char> taken(B, 0);
-  std::vector<Family> blocks;
+  std::vector<int32_t> order;
+  std::vector<Part> blocks;
+  order.reserve(B);
+  blocks.reserve(B);
   for (const Family &f : families) {
     const int64_t n = (int64_t)f.members.size(), most = hwkv::kSharedSeqs;
     const int64_t parts = (n + most - 1) / most, per = (n + parts - 1) / parts;
-    for (int64_t i = 0; i < n; i += per) {
-      const auto at = f.members.begin() + i;
-      blocks.push_back({std::vector<int32_t>(at, at + std::min(per, n - i)), f.pages});
-    }
+    for (int64_t i = 0; i < n; i += per)
+      blocks.push_back({(int32_t)(order.size() + i), (int32_t)std::min(per, n - i), f.pages});
+    order.insert(order.end(), f.members.begin(), f.members.end());
     for (int32_t b : f.members) taken[b] = 1;
   }
-  for (int32_t b = 0; b < B; ++b)
-    if (!taken[b]) blocks.push_back({{b}, 0});
+  for (int32_t b = 0; b < B; ++b) {
+    if (taken[b]) continue;
+    blocks.push_back({(int32_t)order.size(), 1, 0});
+    order.push_back(b);
+  }
 
   struct Launch {
     hwkv::SharedArgs a;
@@ -3341,16 +3350,19 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
     std::vector<int64_t> turns;                  // of a block: workgroups that read a tile
     int64_t groups = 1;                          // most of a block's columns
     std::vector<int64_t> own;                    // tiles of a sequence's own rows in a full unit
-    while (next < blocks.size() && a.n_seqs + blocks[next].members.size() <= (size_t)hwkv::kSharedSeqs) {
-      const Family &f = blocks[next];
+    turns.reserve(hwkv::kSharedBlocks);
+    own.reserve(hwkv::kSharedSeqs);
+    while (next < blocks.size() && a.n_seqs + blocks[next].count <= hwkv::kSharedSeqs) {
+      const Part &f = blocks[next];
       if (f.pages > 0) {
         if (a.n_blocks == hwkv::kSharedBlocks) break;
         a.block_pages[a.n_blocks] = f.pages;
         a.block_first[a.n_blocks] = (uint8_t)a.n_seqs;
-        a.block_count[a.n_blocks] = (uint8_t)f.members.size();
-        groups = std::max(groups, column_groups((int64_t)f.members.size() * G));
+        a.block_count[a.n_blocks] = (uint8_t)f.count;
+        groups = std::max(groups, column_groups(f.count * G));
       }
-      for (int32_t b : f.members) {
+      for (int32_t i = 0; i < f.count; ++i) {
+        const int32_t b = order[f.first + i];
         a.seq[a.n_seqs] = (uint16_t)b;
         a.len[a.n_seqs] = (int32_t)len(b);
         a.seq_block[a.n_seqs++] = f.pages > 0 ? (uint8_t)a.n_blocks : hwkv::kNoBlock;

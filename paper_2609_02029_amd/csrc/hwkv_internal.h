@@ -361,7 +361,7 @@ using PageMoveArgs = PageMoveArgsOf<kMaxRuns>;
 hipError_t launch_page_move(const PageMoveArgs &a, hipStream_t s);
 
 // Rows and pages in one launch, where there are few of both.
-constexpr int kFewMoves = 32, kFewPages = 32;
+constexpr int kFewMoves = 64, kFewPages = 48;
 using FewMoves = MoveArgsOf<kFewMoves>;
 using FewPageCopies = PageCopyArgsOf<kFewPages, kFewPages>;
 using FewPageMoves = PageMoveArgsOf<kFewPages>;
