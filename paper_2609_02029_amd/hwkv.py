@@ -6,6 +6,7 @@ prefix.  Device arguments are torch tensors on the GPU (bf16 inputs, fp32
 outputs, contiguous); ``stream`` defaults to torch's current stream.  There is
 no fallback: if the library is missing, importing this module raises.
 """
+import array
 import ctypes
 import os
 
@@ -53,7 +54,7 @@ SYMBOLS = {
                                ctypes.c_int),
     "hwkv_cache_pages": ([_vp, _P(_i64), _P(_i64)], ctypes.c_int),
     "hwkv_cache_reset_seq": ([_vp, _i32], ctypes.c_int),
-    "hwkv_cache_reorder": ([_vp, _P(_i32), _vp], ctypes.c_int),
+    "hwkv_cache_reorder": ([_vp, _vp, _vp], ctypes.c_int),
     "hwkv_cache_move": ([_vp, _i64, _vp, _sz, _vp], ctypes.c_int),
     "hwkv_beam_workspace_bytes": ([_i64, _i32, _i32, _i32, _i32, _P(_sz)], ctypes.c_int),
     "hwkv_beam_select": ([_i64, _i32, _i32, _vp, _i32, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp],
@@ -293,10 +294,10 @@ def cache_reset_seq(cache, seq):
 def cache_reorder(cache, parents, stream=None):
     """Sequence b becomes what sequence ``parents[b]`` was (-1: empty), in every
     layer.  ``parents``: ``batch`` ints in host memory (a list, a CPU tensor)."""
-    p = [int(x) for x in (parents.tolist() if hasattr(parents, "tolist") else parents)]
+    p = array.array("i", parents.tolist() if hasattr(parents, "tolist") else parents)
     if len(p) != cache.batch:
         raise ValueError("parents must hold one entry per sequence")
-    _check(_lib.hwkv_cache_reorder(cache.handle, (_i32 * len(p))(*p), _stream(stream)))
+    _check(_lib.hwkv_cache_reorder(cache.handle, p.buffer_info()[0], _stream(stream)))
 
 
 def cache_move(cache, n_pages=None, dev_buf=None, stream=None):
