@@ -52,15 +52,6 @@ __device__ __forceinline__ float element(const u32x4_t &c, int e) {
   }
 }
 
-// Token t of a row.
-template <int T>
-__device__ __forceinline__ float logit(const BeamArgs &a, int64_t row, uint32_t t) {
-  const uint8_t *const at = static_cast<const uint8_t *>(a.logits) + (row * a.stride + t) * kBytes<T>;
-  if constexpr (T == HWKV_LOGITS_F32) return *reinterpret_cast<const float *>(at);
-  const u32x4_t v = {*reinterpret_cast<const uint16_t *>(at), 0u, 0u, 0u};
-  return element<T>(v, 0);
-}
-
 // A row's chunks of 16 bytes, from its first logit on.  (Rows of an odd vocabulary
 // start anywhere: the loads need not be aligned, and equal rows are then summed in
 // equal order wherever they lie, so that equal scores are equal in all their bits.)
@@ -93,30 +84,6 @@ struct Row {
     return v;
   }
 };
-
-// Logits t .. t + 3 of a row, minus infinity past its end.
-template <int T>
-__device__ __forceinline__ f32x4_t four_logits(const BeamArgs &a, int64_t row, uint32_t t) {
-  f32x4_t v = {-kInf, -kInf, -kInf, -kInf};
-  if (t + 4 <= (uint32_t)a.vocab) {
-    typedef uint32_t half_t __attribute__((ext_vector_type(2), aligned(2)));
-    const uint8_t *const at = static_cast<const uint8_t *>(a.logits) + (row * a.stride + t) * kBytes<T>;
-    u32x4_t x;
-    if constexpr (T == HWKV_LOGITS_F32) {
-      x = *reinterpret_cast<const chunk_t *>(at);
-    } else {
-      const half_t h = *reinterpret_cast<const half_t *>(at);
-      x = u32x4_t{h.x, h.y, 0u, 0u};
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = element<T>(x, e);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (t + e < (uint32_t)a.vocab) v[e] = logit<T>(a, row, t + e);
-  }
-  return v;
-}
 
 // op(x, y) over the wavefront, in every lane: lanes 1 and 2 apart, a half row's
 // mirror, a row's, and the rows, two and two (registers only, where a shuffle goes
@@ -383,11 +350,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
 
   for (int search = 0, sets = 1;;) {
     Run *const run_of = run_s[search];
-    const auto quad = [&](int i, int r, int j) -> f32x4_t {
-      if (held) return reinterpret_cast<const f32x4_t *>(value_s)[i];
-      if (search == 0) return maxima[i];
-      return four_logits<T>(a, row0 + run_of[r].beam, run_of[r].place + j - run_of[r].beam * (uint32_t)a.vocab);
-    };
+    const auto quad = [&](int i) -> f32x4_t { return held ? reinterpret_cast<const f32x4_t *>(value_s)[i] : maxima[i]; };
     // A score that n items reach, from fp32 roundings: the n-th largest of 64 sets'
     // largest (minus infinity: fewer have one).
     if (sets) {
@@ -395,7 +358,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
 #pragma unroll 2
       for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
         const int r = i / quads;
-        const f32x4_t v = quad(i, r, 4 * (i - r * quads));
+        const f32x4_t v = quad(i);
         // (fmaxf passes over the NaN of a beam without candidates)
         top = fmaxf(top, (float)run_of[r].score(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w))));
       }
@@ -433,7 +396,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
       for (int i = threadIdx.x; i < runs * quads; i += kPickThreads) {
         const int r = search == 0 ? i / quads : i / (kBlock / 4), j = 4 * (i - r * quads);
         const Run run = run_of[r];
-        const f32x4_t v = quad(i, r, j);
+        const f32x4_t v = quad(i);
         if (!(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= run.bound)) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -556,9 +519,9 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     sets = 0;
     runs = found;
     quads = kBlock / 4;
-    held = runs * kBlock <= HELD;
+    held = true;                       // (n_out blocks at most: launch)
 #pragma unroll 4
-    for (int i = threadIdx.x; i < runs * (kBlock / N) && held; i += kPickThreads) {
+    for (int i = threadIdx.x; i < runs * (kBlock / N); i += kPickThreads) {
       const Run run = run_s[1][i / (kBlock / N)];
       const u32x4_t v = Row<T>(a, row0 + run.beam)
                             .load((int)(run.place - run.beam * (uint32_t)a.vocab) / N + i % (kBlock / N), a.vocab);
