@@ -285,12 +285,12 @@ struct Run {
 // items reach is known before a search (the n-th largest of 64 sets' largest maxima; the
 // n-th block's largest), so one comparison of logits with a bound keeps nearly all out,
 // and what passes is listed, given its 64-bit key, and counted against each other (of
-// many, those that a second such score leaves: 4 groups of 16 beams, 2,165 logits, 18
-// chosen, 302 listed: 19.5 us a call against 27.8).
-// Where the list of logits does not hold them (few blocks, whose n-th is far below the
-// best), it is made once more above the n-th of 64 sets' largest logits (2 groups of 16
-// beams, 1,100 logits, 30 chosen: 24 us, 380 without).  Where that does not hold them
-// either (long runs of equal or rising logits), the n-th key, how many lie above it and
+// many, those that a second such score leaves).
+// Where a row has few blocks, the n-th is far below the best, and too many logits pass
+// it: with fewer blocks than are chosen, or where the list overflows, the bound is that
+// of 64 sets of logits (2 groups of 16 beams, 1,100 logits, 30 chosen: 19 us, after an
+// overflow 24, without it 380; 4 groups, 2,165 logits, 18 chosen: 16.5, not 19.3, and
+// 27.8 where 302 are counted against each other).  Where that does not hold them either (long runs of equal or rising logits), the n-th key, how many lie above it and
 // then the n-th item's place are found bit by bit first.
 //
 // What bounds it: latency, of two reads of what other XCDs wrote or left in memory
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     if (threadIdx.x == 0 && found < n) floor_s = -__builtin_inf();
     __syncthreads();
     search = 1;
-    sets = 0;
+    sets = a.n_blocks < n ? 1 : 0;     // (a beam's blocks alone do not reach the n-th)
     runs = found;
     quads = kBlock / 4;
     held = true;                       // (n_out blocks at most: launch)
