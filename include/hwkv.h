@@ -501,9 +501,8 @@ int hwkv_decode_attn(hwkv_cache *cache, int32_t layer, const void *q,
                      void *stream);
 
 /* hwkv_decode_attn where sequences share pages (hwkv_cache_reorder): whole pages
- * that several sequences hold are read once for all of them, with the query heads of
- * 16 columns at a time.  Right for every cache and every batch, forked or not;
- * where nothing is shared hwkv_decode_attn is as fast or faster.  Which pages are
+ * that several sequences hold are read once for every 48 of their query heads.  Right for every cache and every batch, forked or not;
+ * where nothing is shared it takes about as long as hwkv_decode_attn.  Which pages are
  * shared is known to the host: the call reads nothing back.
  *   ws, ws_bytes  device workspace of >= hwkv_decode_shared_workspace_bytes, 16-byte
  *                 aligned

@@ -290,8 +290,9 @@ struct Run {
 // it: with fewer blocks than are chosen, or where the list overflows, the bound is that
 // of 64 sets of logits (2 groups of 16 beams, 1,100 logits, 30 chosen: 19 us, after an
 // overflow 24, without it 380; 4 groups, 2,165 logits, 18 chosen: 16.5, not 19.3, and
-// 27.8 where 302 are counted against each other).  Where that does not hold them either (long runs of equal or rising logits), the n-th key, how many lie above it and
-// then the n-th item's place are found bit by bit first.
+// 27.8 where 302 are counted against each other).  Where that does not hold them either
+// (long runs of equal or rising logits), the n-th key, how many lie above it and then
+// the n-th item's place are found bit by bit first.
 //
 // What bounds it: latency, of two reads of what other XCDs wrote or left in memory
 // (about 1.5 us each) and some twenty steps through LDS.  24 groups of 4 beams, 131,072
