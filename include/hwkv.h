@@ -247,6 +247,8 @@ int hwkv_cache_reset_seq(hwkv_cache *cache, int32_t seq);
  * copies, in the page that a sequence without children leaves, or from the pool.
  * Every other call takes a sequence that shares pages like any other: shared
  * pages are full, and full pages are never written again.
+ * Nothing is allocated on the device.  Lengths and pages change when the call is made;
+ * where it is captured, a replay repeats the copies alone.
  * EINVAL on a bad parent, more than 65534 sequences, or a cycle (0 <- 1, 1 <- 2, ..,
  * n <- 0) of more than 191 sequences; ENOMEM if the pool has too few pages. */
 int hwkv_cache_reorder(hwkv_cache *cache, const int32_t *parents, void *stream);
