@@ -173,7 +173,8 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
   // whole shift, so that x log2 e needs no difference first; others a logit as their
   // base, from which they differ exactly.
   double sum = 0.0, base = kNone, shift = 0.0;
-  float lowest = 0.0f, over = -__FLT_MAX__;  // base - 690, base + 600
+  float lowest = 0.0f, over = -kInf;         // base - 690, base + 600 (no base yet: any logit
+                                             //   is over it, the lowest one too)
   double magic = 0.0;                        // 1.5 * 2^52 - shift: added, the low word is the
                                              //   whole part less the shift
   bool near = true;

@@ -1,0 +1,101 @@
+"""GPU tests of beam selection over rows that are masked whole, hold what is no
+number, or lie far from zero.
+
+Scores are 64-bit and rounded once to fp32: off by half a step, 2^-24 of the value,
+and by the error of a row's sum, 1e-10."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_02029_amd import hwkv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+
+
+def select(x, s, n):
+    G = x.shape[0]
+    out = [torch.full((G, n), 7, dtype=d, device=DEV) for d in (torch.float32, torch.int32, torch.int32)]
+    ws = torch.full((hwkv.beam_workspace_bytes(x, n),), 0xff, dtype=torch.uint8, device=DEV)
+    hwkv.beam_select(x, s, *out, ws)
+    return [t.cpu() for t in out]
+
+
+def reference(x, s, n):
+    """Scores, parents and tokens from each row's distances to its largest logit,
+    which keep log sum e^(x - top) however far the row lies from zero.  (The order is
+    by that in steps of 2^-34, with which a running score is summed exactly: equal
+    scores of equal rows are equal bits.)"""
+    G, B, V = x.shape
+    x, s = x.double().cpu().numpy(), s.double().cpu().numpy()
+    score, key = np.full((2, G, B, V), -np.inf)
+    for g in range(G):
+        for b in range(B):
+            row = x[g, b]
+            top = row.max()
+            if math.isfinite(s[g, b]) and math.isfinite(top):        # (NaN if any logit is)
+                rest = math.log(np.exp(row - top).sum())
+                score[g, b] = (s[g, b] - rest) + (row - top)
+                key[g, b] = (s[g, b] - round(rest * 2.0 ** 34) * 2.0 ** -34) + (row - top)
+    at = np.argsort(-key.reshape(G, B * V), axis=1, kind="stable")[:, :n]
+    at = np.pad(at, ((0, 0), (0, n - at.shape[1])))
+    val = np.take_along_axis(score.reshape(G, B * V), at, 1)
+    val[:, B * V:] = -np.inf
+    none = val == -np.inf
+    return val, np.where(none, -1, np.arange(G)[:, None] * B + at // V), np.where(none, -1, at % V)
+
+
+def check(x, s, n):
+    val, par, tok = reference(x, s, n)
+    got = [t.numpy() for t in select(x, s, n)]
+    assert np.array_equal(got[1], par), (got[1], par)
+    assert np.array_equal(got[2], tok), (got[2], tok)
+    some = par >= 0
+    assert np.all(got[0][~some] == -np.inf)
+    assert np.all(np.abs(got[0][some] - val[some]) <= 2.0 ** -24 * np.abs(val[some]) + 1e-10)
+    return got
+
+
+def logits(G, B, V, t, seed=1):
+    g = torch.Generator(device=DEV).manual_seed(seed + V)
+    return (torch.randn((G, B, V), generator=g, device=DEV) * 2.5).to(TYPES[t])
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [1, 300, 1000, 40000])
+def test_a_row_at_the_lowest_value_beside_others(t, V):
+    """A mask of the type's lowest value over a whole row (no token of it is a better
+    choice than those of a live row), over a row's end, and over all but its end."""
+    low = torch.finfo(TYPES[t]).min
+    x, s = logits(2, 4, V, t), torch.tensor([[0.0, -40.0, -0.5, -1.0], [-40.0, -1.0, -0.25, -30.0]], device=DEV)
+    x[0, 1] = x[1, 0] = x[1, 3] = low
+    x[0, 2, V // 3:] = low
+    x[1, 1, :V - V // 3 - 1] = low
+    n = min(3, V)
+    got = select(x, s, n)
+    _, par, tok = reference(x, s, n)
+    assert np.array_equal(got[1].numpy(), par) and np.array_equal(got[2].numpy(), tok)
+    assert torch.isfinite(got[0]).all()
+    assert set(got[1][0].tolist()) <= {0, 2, 3} and set(got[1][1].tolist()) <= {5, 6}
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [1, 1000, 40000])
+def test_rows_at_the_lowest_value_alone(t, V):
+    """Every row is masked whole: the lowest tokens of the best running score."""
+    x = torch.full((1, 3, V), torch.finfo(TYPES[t]).min, dtype=TYPES[t], device=DEV)
+    s = torch.tensor([[-2.0, -1.0, -3.0]], device=DEV)
+    n = min(V, 9)
+    out = select(x, s, n)
+    assert out[1].tolist() == [[1] * n] and out[2].tolist() == [list(range(n))]
+    assert torch.isfinite(out[0]).all()
