@@ -257,10 +257,10 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
   a.part[(row * a.n_splits + split) * 2 + 1] = top;
 }
 
-// Scores as whole numbers in their order; 0: no candidate.
+// Scores as whole numbers in their order; above 0.
 __device__ __forceinline__ uint64_t order_key(double score) {
   const uint64_t u = __double_as_longlong(score + 0.0);
-  return score > -__builtin_inf() ? u ^ (u >> 63 ? ~0ull : 1ull << 63) : 0;
+  return u ^ (u >> 63 ? ~0ull : 1ull << 63);
 }
 __device__ __forceinline__ double key_score(uint64_t key) {
   return __longlong_as_double(key >> 63 ? key ^ 1ull << 63 : ~key);
@@ -274,7 +274,7 @@ constexpr int kRanked = 96;          // listed items that are counted against ea
 // A run of a search's list: consecutive places of one beam.
 struct Run {
   uint32_t beam, place;
-  float bound;                       // below every logit that is asked for
+  float bound;                       // below every logit that is asked for (NaN: none is)
   uint32_t unused;
   double s, lse;                     // the beam's (lse NaN: one without candidates)
   __device__ __forceinline__ double score(float x) const { return s + ((double)x - lse); }
@@ -387,8 +387,11 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
         const double s = run_of[threadIdx.x].s, lse = run_of[threadIdx.x].lse, x = floor - s + lse;
         const double off = (__builtin_fabs(floor) + __builtin_fabs(s) + __builtin_fabs(lse)) * 0x1p-48 +
                            __builtin_fabs(x) * 0x1p-22;
-        // (of a beam without candidates nothing, of a floor of minus infinity all)
-        run_of[threadIdx.x].bound = lse != lse ? kInf : any || floor == -__builtin_inf() ? -__FLT_MAX__ : (float)(x - off);
+        // Of a beam without candidates nothing passes (a NaN: its logits may be +infinity),
+        // of a floor of minus infinity all, but never a logit of minus infinity: every
+        // item that is listed has a score.
+        const float least = any || floor == -__builtin_inf() ? -__FLT_MAX__ : fmaxf((float)(x - off), -__FLT_MAX__);
+        run_of[threadIdx.x].bound = lse != lse ? __builtin_nanf("") : least;
       }
       if (threadIdx.x == 0) listed = 0;
       __syncthreads();

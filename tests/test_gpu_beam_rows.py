@@ -99,3 +99,45 @@ def test_rows_at_the_lowest_value_alone(t, V):
     out = select(x, s, n)
     assert out[1].tolist() == [[1] * n] and out[2].tolist() == [list(range(n))]
     assert torch.isfinite(out[0]).all()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_no_row_without_a_sum_is_chosen_from(t, bad):
+    """A row that holds a NaN or +infinity has no continuations, also where nothing
+    else is left to choose."""
+    for V, at, n in ((1000, slice(7, 8), 2), (1000, slice(None), 5), (5, slice(4, 5), 4), (40000, slice(39999, None), 64)):
+        x = logits(1, 1, V, t)
+        x[0, 0, at] = bad
+        out = select(x, torch.zeros((1, 1), device=DEV), n)
+        assert out[1].tolist() == out[2].tolist() == [[-1] * n] and (out[0] == -math.inf).all()
+    x = logits(1, 3, 1000, t)
+    x[0, :2, 500] = bad
+    x[0, 2] = -math.inf
+    assert select(x, torch.zeros((1, 3), device=DEV), 4)[1].tolist() == [[-1] * 4]
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_row_without_a_sum_beside_few_continuations(t, bad):
+    """Live rows with fewer allowed tokens, and blocks that hold one, than are chosen,
+    beside rows that hold a NaN or +infinity at one place, at their allowed tokens, or
+    everywhere; and beside a beam that is not alive."""
+    for V, B, n, allowed in ((3000, 2, 4, (5, 900)), (32000, 2, 4, (3, 16000, 31999)), (3000, 4, 30, (5, 6, 900)),
+                             (40001, 64, 64, (17, 40000)), (131072, 5, 10, (0, 1, 2, 70000, 131071))):
+        for where in ("one", "allowed", "all"):
+            x = torch.full((2, B, V), -math.inf, dtype=TYPES[t], device=DEV)
+            live = 0 if where == "one" else B - 1
+            for b in range(B):
+                x[:, b, list(allowed)] = torch.arange(len(allowed), device=DEV).to(TYPES[t]) / 4
+                if b != live:
+                    if where == "all":
+                        x[:, b] = bad
+                    else:
+                        x[:, b, list(allowed) if where == "allowed" else allowed[0]] = bad
+            s = -torch.arange(2 * B, device=DEV, dtype=torch.float32).view(2, B) / 8
+            got = check(x, s, n)
+            some = min(n, len(allowed))
+            assert (got[1][:, :some] == [[live], [B + live]]).all() and (got[1][:, some:] == -1).all()
+            s[1, live] = -math.inf
+            check(x, s, n)
