@@ -168,12 +168,12 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
   // (rows of maxima are whole quads)
   if (split == 0 && (int)threadIdx.x < whole_quads(a.n_blocks) - a.n_blocks) block_max[a.n_blocks + threadIdx.x] = -kInf;
   // e^(x - base), summed; the base is set by the largest logit of the first block that
-  // has one, and of a block whose largest passes it by 600, and a logit more than 690
+  // has one, and of a block whose largest passes it by 500, and a logit more than 690
   // below it counts as that (e^-690).  Logits up to 2^16 take base = shift ln 2 with a
   // whole shift, so that x log2 e needs no difference first; others a logit as their
   // base, from which they differ exactly.
   double sum = 0.0, base = kNone, shift = 0.0;
-  float lowest = 0.0f, over = -kInf;         // base - 690, base + 600 (no base yet: any logit
+  float lowest = 0.0f, over = -kInf;         // base - 690, base + 500 (no base yet: any logit
                                              //   is over it, the lowest one too)
   double magic = 0.0;                        // 1.5 * 2^52 - shift: added, the low word is the
                                              //   whole part less the shift
@@ -220,7 +220,8 @@ __global__ __launch_bounds__(kScanWaves * 64) void beam_scan(BeamArgs a) {
         shift = rint((double)top * kLog2e);
         base = near ? shift * kLn2 : (double)top;
         lowest = (float)(base - 690.0);
-        over = (float)(base + 600.0);
+        // (in fp32's steps 512 above a large base at most: half a step of 1,024 is not reached)
+        over = (float)(base + 500.0);
         magic = 0x1.8p52 - shift;
         sum *= exp(before - base);
       }

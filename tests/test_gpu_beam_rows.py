@@ -141,3 +141,15 @@ def test_a_row_without_a_sum_beside_few_continuations(t, bad):
             assert (got[1][:, :some] == [[live], [B + live]]).all() and (got[1][:, some:] == -1).all()
             s[1, live] = -math.inf
             check(x, s, n)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_a_later_block_one_step_above(sign):
+    """Logits whose neighbours in fp32 lie 512, 1,024 and 2,048 apart, and the last one a
+    step above them all: its row's sum is its own."""
+    for value in (5e9, 8.7e9, 2.0 ** 33, 2.0 ** 34 - 1024, 1.8e10):
+        x = torch.full((1, 1, 400000), sign * value, device=DEV)
+        x[0, 0, -1] = torch.nextafter(x[0, 0, -1], torch.tensor(math.inf, device=DEV))
+        got = check(x, torch.zeros((1, 1), device=DEV), 3)
+        # (the row's sum is one term, e^0, which its polynomial gives to 5.5e-11)
+        assert abs(got[0][0, 0]) <= 1e-10 and got[2].tolist() == [[399999, 0, 1]]
