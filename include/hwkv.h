@@ -565,8 +565,9 @@ int hwkv_beam_workspace_bytes(int64_t n_groups, int32_t n_beams, int32_t vocab,
  * of row r = group * n_beams + beam and its running score s,
  *   lse[r] = log sum_t e^x[r][t],  score(r, t) = s[r] + (x[r][t] - lse[r]):
  * the n_out largest scores of the group's rows and tokens, falling; equal ones go
- * to the lowest (r, t).  Sums and scores are formed in 64 bits (lse to 1e-10) and
- * order by these; the outputs are rounded to fp32.
+ * to the lowest (r, t).  Sums and scores are formed in 64 bits (log sum_t e^(x - the
+ * row's largest) to 1e-10, wherever the row lies) and order by these; the outputs are
+ * rounded to fp32.
  *   logits       device, n_groups * n_beams rows of vocab elements of `type`,
  *                `stride` elements apart, aligned to their elements
  *   scores       device fp32 [n_groups][n_beams]; -infinity: the beam has no

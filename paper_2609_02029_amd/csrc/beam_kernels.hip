@@ -277,7 +277,8 @@ struct Run {
   uint32_t beam, place;
   float bound;                       // below every logit that is asked for (NaN: none is)
   uint32_t unused;
-  double s, lse;                     // the beam's (lse NaN: one without candidates)
+  double s, lse;                     // the beam's (lse NaN: one without candidates), or, where
+                                     //   lse would lose log sum e^(x - base), s less that, and base
   __device__ __forceinline__ double score(float x) const { return s + ((double)x - lse); }
 };
 
@@ -343,11 +344,16 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
     const Part p = next;
     next = load_part(b + WAVES);
     const double top = over_wave(p.base, [](double x, double y) { return fmax(x, y); });
-    const double all = wave_sum(p.sum * exp(p.base - top));
+    const double all = wave_sum(p.sum * exp(p.base - top)), rest = log(all);
     const bool some = all > 0.0 && all < __builtin_inf() && __builtin_fabs(p.s) < __builtin_inf();
+    // A row at a type's lowest value, -3.4e38, is uniform: in top + rest nothing of rest is
+    // left.  So rows from 2^19 on keep them apart, rest in the steps that lse has there, 2^-34
+    // (3e-11 off): s less that is exact, and scores of two beams that are equal stay so.
+    const bool near = __builtin_fabs(top) < 0x1p19;
     if (lane == 0)
-      run_s[0][b] = {(uint32_t)b, (uint32_t)(b * quads * 4), 0.f, 0u, some ? p.s : 0.0,
-                     some ? top + log(all) : __builtin_nan("")};
+      run_s[0][b] = {(uint32_t)b, (uint32_t)(b * quads * 4), 0.f, 0u,
+                     !some ? 0.0 : near ? p.s : p.s - rint(rest * 0x1p34) * 0x1p-34,
+                     !some ? __builtin_nan("") : near ? top + rest : top};
   }
   __syncthreads();
 

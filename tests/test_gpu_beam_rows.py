@@ -153,3 +153,32 @@ def test_a_later_block_one_step_above(sign):
         got = check(x, torch.zeros((1, 1), device=DEV), 3)
         # (the row's sum is one term, e^0, which its polynomial gives to 5.5e-11)
         assert abs(got[0][0, 0]) <= 1e-10 and got[2].tolist() == [[399999, 0, 1]]
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [1, 1000, 40000])
+def test_scores_of_rows_far_from_zero(t, V):
+    """A row at the type's lowest value is uniform: each token has the running score
+    less log V, and goes behind those of live rows that are likelier.  So for rows
+    anywhere in the type's range."""
+    fi = torch.finfo(TYPES[t])
+    s = torch.tensor([[0.0, -1.0, -0.5]], device=DEV)
+    for far in (fi.min, fi.max, fi.min / 2, fi.max / 8, 60000.0, -60000.0):
+        x = torch.full((1, 3, V), far, dtype=TYPES[t], device=DEV)
+        x[0, 2, V // 2] = -math.inf if V > 1 else far
+        check(x, s, min(V, 20))
+        x[0, 0] = logits(1, 1, V, t)[0, 0]
+        check(x, s, min(V, 20))
+        x[0, 2, V // 3:] = torch.nextafter(torch.tensor(far, dtype=TYPES[t]), torch.tensor(0.0, dtype=TYPES[t])).to(DEV)
+        check(x, s, min(V, 5))
+
+
+def test_equal_scores_of_rows_far_from_zero():
+    """Three equal rows, whose running scores differ by a step of their logits: scores
+    of one are equal to those of another, and go to the lowest row."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for far, step in ((4e5, 2.0 ** -5), (-4e5, 2.0 ** -5), (2e6, 0.125), (-3e8, 32.0)):
+        x = (torch.randint(-40, 1, (1, 1, 3000), generator=g, device=DEV) * step + far).repeat(1, 3, 1)
+        s = torch.tensor([[0.0, -step, -2 * step]], device=DEV)
+        check(x, s, 40)
+        check(x, s.flip(1), 40)
