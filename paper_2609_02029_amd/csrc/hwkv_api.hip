@@ -3413,7 +3413,8 @@ int shared_impl(hwkv_cache *c, int32_t layer, const void *q, float scale, void *
       };
       for (int32_t i = 0; i < a.n_blocks && a.n_full > 0; ++i) {
         total += (int64_t)a.block_pages[i] * 4 * weight / 16 * turns[i] * a.n_full;
-        longest = std::max<int64_t>(longest, (int64_t)a.block_pages[i] * 4 * weight / 16);
+        // (rounded up: with so many tiles a workgroup a block has one, and no second for the rest)
+        longest = std::max<int64_t>(longest, ((int64_t)a.block_pages[i] * 4 * weight + 15) / 16);
       }
       for (int64_t t : own) {
         total += a.n_full > 0 ? t * a.n_full : 0;
