@@ -3012,7 +3012,8 @@ int launch_page_copies(const hwkv_cache *c, const PagePlan &P, const MovePlan &p
       for (size_t k = 0; k < hwkv::kMaxMoves; ++k) {
         t.src[k] = k < n ? (uint16_t)moves[m + k].src : 0;
         t.dst[k] = k < n ? (uint16_t)moves[m + k].dst : 0;
-        t.pages[k] = k < n ? (int32_t)pages_for(moves[m + k].rows) : 0;
+        // (a sequence may be longer in a layer of windows alone than a table row is)
+        t.pages[k] = k < n ? (int32_t)std::min(pages_for(moves[m + k].rows), c->max_pages) : 0;
         t.most = std::max(t.most, t.pages[k]);
       }
       if (t.most == 0) continue;

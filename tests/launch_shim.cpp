@@ -1,12 +1,13 @@
 // Stands between the library and the HIP runtime in a process without a GPU: kernel
-// launches succeed and do nothing, and are counted.  Preloaded by
-// test_host_launches.py.
+// launches succeed and do nothing; they are counted, and the arguments of
+// some are looked at.  Preloaded by test_host_launches.py.
 #include <dlfcn.h>
 
+#include <algorithm>
 #include <map>
 #include <string>
 
-#include <hip/hip_runtime.h>
+#include "hwkv_internal.h"
 
 namespace {
 std::map<const void *, std::string> &names() {
@@ -22,6 +23,20 @@ struct {
   size_t shared;
   hipStream_t stream;
 } launch;
+std::string fault;
+
+// Every entry that the kernel would touch lies in the row of its sequence.
+void check_table_move(const hwkv::TableMoveArgs &a, dim3 grid) {
+  for (int r = 0; r < a.part[a.n_parts] * hwkv::kMoveRound; ++r) {
+    if (a.pages[r] == 0) continue;
+    const bool rows = (a.src[r] == hwkv::kMoveCarry || a.src[r] < a.batch) &&
+                      (a.dst[r] == hwkv::kMoveCarry || a.dst[r] < a.batch);
+    // (a thread an entry, as many as the grid has)
+    const int64_t pages = std::min<int64_t>(a.pages[r], (int64_t)grid.x * 256);
+    if (!rows || pages > a.max_pages)
+      fault = "table_move: " + std::to_string(a.pages[r]) + " entries of rows of " + std::to_string(a.max_pages);
+  }
+}
 }  // namespace
 
 extern "C" {
@@ -32,6 +47,7 @@ int shim_launches(const char *kernel) {
     if (c.first.find(kernel) != std::string::npos) n += c.second;
   return n;
 }
+const char *shim_fault() { return fault.c_str(); }
 
 void __hipRegisterFunction(void **modules, const void *host, char *device, const char *name, unsigned limit, void *tid,
                            void *bid, void *block, void *grid, int *size) {
@@ -52,8 +68,11 @@ hipError_t __hipPopCallConfiguration(dim3 *grid, dim3 *block, size_t *shared, hi
   *stream = launch.stream;
   return hipSuccess;
 }
-hipError_t hipLaunchKernel(const void *f, dim3, dim3, void **, size_t, hipStream_t) {
-  ++counts()[names()[f]];
+hipError_t hipLaunchKernel(const void *f, dim3 grid, dim3, void **args, size_t, hipStream_t) {
+  const std::string &name = names()[f];
+  ++counts()[name];
+  if (name.find("table_move") != std::string::npos)
+    check_table_move(*static_cast<const hwkv::TableMoveArgs *>(args[0]), grid);
   return hipSuccess;
 }
 hipError_t hipGetLastError() { return hipSuccess; }

@@ -1,5 +1,5 @@
-"""CPU tests of what the host hands to the kernels of shared decode: the
-library as it is, in a process whose kernel launches are counted and not made
+"""CPU tests of what the host hands to the kernels of shared decode and reordering: the
+library as it is, in a process whose kernel launches are looked at and not made
 (``launch_shim.cpp``), so that caches can be filled, forked and decoded without a GPU."""
 import os
 import subprocess
@@ -32,6 +32,10 @@ def run(tmp_path_factory):
 
 def test_shared_decode_takes_no_more_than_its_workspace(run):
     run("workspace")
+
+
+def test_a_reorder_moves_no_more_entries_than_a_table_row_has(run):
+    run("table")
 
 
 # ---- in the process of the shim
@@ -117,9 +121,28 @@ def workspace(hw, shim):
     assert shim.shim_launches(b"decode_shared") >= made + len(cases)
 
 
+def table(hw, shim):
+    """Sequences that are longer in a layer of windows alone than any full unit may be:
+    forked and permuted, with more table entries than lists of them hold."""
+    import ctypes
+    L, H, B, max_ctx = 2, 6, 10, 2800
+    pol = hw.policy_set(L, H, H, 64, 4, [100, 0], [[1] * H, [0] * H])
+    for parents in ([0] * B, [B - 1 - b for b in range(B)], [(b + 1) % B for b in range(B)]):
+        h, made = ctypes.c_void_p(), shim.shim_launches(b"table_move")
+        assert hw._lib.hwkv_cache_alloc_paged(ctypes.byref(h), pol.handle, B, max_ctx, 0, None, None, 1000, FAKE, BUF) == hw.OK
+        for b in range(B):
+            for layer, n in ((0, max_ctx - b), (1, 9000 + b)):
+                assert hw._lib.hwkv_prefill_write(h, layer, b, 0, n, FAKE + 2 * BUF, FAKE + 3 * BUF, None) == hw.OK
+        assert hw._lib.hwkv_cache_reorder(h, (ctypes.c_int32 * B)(*parents), None) == hw.OK, hw.last_error()
+        assert shim.shim_launches(b"table_move") > made
+        assert shim.shim_fault() == b"", shim.shim_fault()
+        hw._lib.hwkv_cache_free(h)
+
+
 if __name__ == "__main__":
     import ctypes
     sys.path.insert(0, ROOT)
     shim = ctypes.CDLL(os.environ["SHIM"])
+    shim.shim_fault.restype = ctypes.c_char_p
     from paper_2609_02029_amd import hwkv
-    {"workspace": workspace}[sys.argv[1]](hwkv, shim)
+    {"workspace": workspace, "table": table}[sys.argv[1]](hwkv, shim)
