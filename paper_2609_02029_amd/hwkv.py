@@ -138,6 +138,14 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _stream_object(stream):
+    if stream is None:
+        return torch.cuda.current_stream()
+    if isinstance(stream, int):
+        return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return stream
+
+
 def _dev(t, dtype_name, what):
     if t is None:
         return None
@@ -173,6 +181,8 @@ class Cache:
         self.handle = handle
         self.n_layers, self.n_kv_heads, self.n_q_heads = n_layers, n_kv_heads, n_q_heads
         self.head_dim, self.batch = head_dim, batch
+        self.dev_buf = None   # the caller's buffer that the cache lies in
+        self.left = []        # buffers that captured moves read
 
     def free(self):
         if getattr(self, "handle", None):
@@ -303,12 +313,20 @@ def cache_reorder(cache, parents, stream=None):
 def cache_move(cache, n_pages=None, dev_buf=None, stream=None):
     """Moves the cache into ``dev_buf`` (uint8 device tensor, kept alive; None: the
     library allocates), with a pool of ``n_pages`` pages (None: not a paged
-    cache).  The buffer that it leaves must live until the stream's work is done."""
+    cache).  The buffer that it leaves (``dev_buf`` of cache_alloc or of an earlier move)
+    is not used again for other tensors before the stream's work is done; where the
+    call is captured, the cache keeps it, since replays read it."""
     _on_current_device(dev_buf)
     ptr = _dev(dev_buf, "uint8", "dev_buf")
     _check(_lib.hwkv_cache_move(cache.handle, 0 if n_pages is None else n_pages, ptr,
                                 0 if dev_buf is None else dev_buf.numel(), _stream(stream)))
-    cache.dev_buf = dev_buf
+    left, cache.dev_buf = cache.dev_buf, dev_buf
+    if left is None:
+        return
+    if torch.cuda.is_current_stream_capturing():
+        cache.left.append(left)
+    else:
+        left.record_stream(_stream_object(stream))
 
 
 def cache_format(cache):
