@@ -138,12 +138,15 @@ def _stream(stream):
     return stream.cuda_stream
 
 
-def _stream_object(stream):
-    if stream is None:
-        return torch.cuda.current_stream()
-    if isinstance(stream, int):
-        return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-    return stream
+_stream_objects = {}
+
+
+def _stream_object(raw):
+    """torch's object for a stream of the current device (made once each: 3 us)."""
+    key = torch._C._cuda_getDevice(), raw
+    if key not in _stream_objects:
+        _stream_objects[key] = torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
+    return _stream_objects[key]
 
 
 def _dev(t, dtype_name, what):
@@ -318,15 +321,16 @@ def cache_move(cache, n_pages=None, dev_buf=None, stream=None):
     call is captured, the cache keeps it, since replays read it."""
     _on_current_device(dev_buf)
     ptr = _dev(dev_buf, "uint8", "dev_buf")
+    raw = _stream(stream)
     _check(_lib.hwkv_cache_move(cache.handle, 0 if n_pages is None else n_pages, ptr,
-                                0 if dev_buf is None else dev_buf.numel(), _stream(stream)))
+                                0 if dev_buf is None else dev_buf.numel(), raw))
     left, cache.dev_buf = cache.dev_buf, dev_buf
     if left is None:
         return
-    if torch.cuda.is_current_stream_capturing():
+    if torch._C._cuda_isCurrentStreamCapturing():
         cache.left.append(left)
     else:
-        left.record_stream(_stream_object(stream))
+        left.record_stream(_stream_object(raw))
 
 
 def cache_format(cache):

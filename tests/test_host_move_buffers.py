@@ -27,10 +27,11 @@ def hw(monkeypatch):
     monkeypatch.setattr(hwkv, "_on_current_device", lambda *a: None)
     monkeypatch.setattr(hwkv, "_dev", lambda *a: None)
     capturing = []
-    monkeypatch.setattr(hwkv.torch.cuda, "is_current_stream_capturing", lambda: bool(capturing))
+    monkeypatch.setattr(hwkv.torch._C, "_cuda_isCurrentStreamCapturing", lambda: bool(capturing), raising=False)
     monkeypatch.setattr(hwkv.torch.cuda, "ExternalStream", lambda s: ("external", s))
     monkeypatch.setattr(hwkv.torch.cuda, "default_stream", lambda: "default")
-    monkeypatch.setattr(hwkv.torch.cuda, "current_stream", lambda: "current")
+    monkeypatch.setattr(hwkv.torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(hwkv, "_stream_objects", {})
     monkeypatch.setattr(hwkv, "_stream", lambda s: 77 if s is None else s if isinstance(s, int) else s.cuda_stream)
     return types.SimpleNamespace(hwkv=hwkv, calls=calls, capturing=capturing)
 
@@ -38,7 +39,7 @@ def hw(monkeypatch):
 def test_the_left_buffer_waits_for_the_move(hw):
     cache = hw.hwkv.Cache(None, 1, 1, 1, 64, 1)
     side = types.SimpleNamespace(cuda_stream=5)
-    for stream, seen, raw in ((side, side, 5), (None, "current", 77), (9, ("external", 9), 9), (0, "default", 0)):
+    for stream, seen, raw in ((side, ("external", 5), 5), (None, ("external", 77), 77), (9, ("external", 9), 9), (0, "default", 0)):
         left = cache.dev_buf = Buffer()
         hw.hwkv.cache_move(cache, 4, None, stream=stream)
         assert left.streams == [seen] and hw.calls[-1] == raw and cache.dev_buf is None
