@@ -238,7 +238,8 @@ int hwkv_cache_reset_seq(hwkv_cache *cache, int32_t seq);
  * times and drops others; parallel samples fork one prompt), or empty where
  * parents[b] is -1.
  *   parents   host int32 [batch], each in [-1, batch); read before the call
- *             returns
+ *             returns (a selection leaves its parents on the device: copy them, and
+ *             wait for the copy, first)
  * Finite units, and full units of a cache that is not paged, are copied to the
  * sequence's own rows.  In a paged cache the sequences that come from one parent
  * share its whole pages from then on (a page returns to the pool with the last
@@ -261,8 +262,9 @@ int hwkv_cache_reorder(hwkv_cache *cache, const int32_t *parents, void *stream);
  *   dev_buf, buf_bytes  as in hwkv_cache_alloc_paged, and apart from the present
  *                       buffer; NULL: the library allocates
  * The cache uses the new buffer from then on.  A buffer of the caller's that it
- * leaves must stay until the work on `stream` is done; one that the library owns
- * is freed, for which the call waits for `stream` (not under stream capture).  A
+ * leaves must stay until the work on `stream` is done, or, where the call is captured,
+ * as long as it is replayed; one that the library owns is freed, for which the call
+ * waits for `stream` (not under stream capture).  A
  * kernel of an earlier call must be done, or on `stream`.  ENOMEM if the sequences
  * hold more than n_pages pages, or the buffer is too small; EINVAL if it is not
  * 16-byte aligned or overlaps the present one, and on more than 65534 sequences. */
@@ -514,7 +516,8 @@ int hwkv_decode_attn(hwkv_cache *cache, int32_t layer, const void *q,
  * the weights as three bf16 terms that carry each to 2^-27 of itself, or, over
  * binary16 values, two binary16 terms (2^-22).  Outputs differ from those of
  * hwkv_decode_attn by the order of fp32 sums; equal calls on equal caches give equal
- * bits. */
+ * bits (not so a cache whose sequences hold the same rows unshared).  There is no form
+ * that appends, and hwkv_decode_timing does not record the call. */
 int hwkv_decode_attn_shared(hwkv_cache *cache, int32_t layer, const void *q,
                             float scale, void *out, void *ws, size_t ws_bytes,
                             void *stream);
@@ -566,8 +569,9 @@ int hwkv_beam_workspace_bytes(int64_t n_groups, int32_t n_beams, int32_t vocab,
  *   lse[r] = log sum_t e^x[r][t],  score(r, t) = s[r] + (x[r][t] - lse[r]):
  * the n_out largest scores of the group's rows and tokens, falling; equal ones go
  * to the lowest (r, t).  Sums and scores are formed in 64 bits (log sum_t e^(x - the
- * row's largest) to 1e-10, wherever the row lies) and order by these; the outputs are
- * rounded to fp32.
+ * row's largest) to 1e-10, wherever the row lies) and order by these, so that scores of
+ * rows of unequal logits that are nearer than that may come in either order; the
+ * outputs are rounded to fp32.
  *   logits       device, n_groups * n_beams rows of vocab elements of `type`,
  *                `stride` elements apart, aligned to their elements
  *   scores       device fp32 [n_groups][n_beams]; -infinity: the beam has no
@@ -576,7 +580,8 @@ int hwkv_beam_workspace_bytes(int64_t n_groups, int32_t n_beams, int32_t vocab,
  *   out_parents  device int32 [n_groups][n_out]: r
  *   out_tokens   device int32 [n_groups][n_out]: t
  *   ws           device workspace, 16-byte aligned
- * A logit of -infinity (a token that is not allowed) is no continuation, nor is
+ * A logit of -infinity (a token that is not allowed) is no continuation (the type's
+ * lowest finite value is a logit like others: a row of nothing else is uniform), nor is
  * any of a row that holds a NaN or +infinity, or whose score is not finite; where a
  * group has fewer than n_out, the rest are -infinity, -1 and -1.  The result is
  * the same from run to run.  1 <= n_beams, n_out <= 64, 1 <= vocab <= 2^24,

@@ -298,9 +298,8 @@ struct Run {
 // the n-th item's place are found bit by bit first.
 //
 // What bounds it: latency, of two reads of what other XCDs wrote or left in memory
-// (about 1.5 us each) and some twenty steps through LDS.  24 groups of 4 beams, 131,072
-// logits: with keys formed for every logit and a visit's code for each purpose 15 us,
-// one visit for all purposes 13.6, a bound in front of the keys 7.6, maxima in whole quads 7.
+// (about 1.5 us each) and some twenty steps through LDS: 7 us for 24 groups of 4 beams,
+// 131,072 logits.
 template <int T, int HELD>
 __global__ __launch_bounds__(kPickThreads) void beam_pick(BeamArgs a) {
   constexpr int N = kPerChunk<T>, WAVES = kPickThreads / 64;
